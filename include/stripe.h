@@ -286,6 +286,111 @@ stripe_status_t stripe_device_stream(const void* src, void* dst, size_t n_vector
 stripe_status_t stripe_device_mfma(const void* operands, void* out, int iters, int from_lds, int grid, void* hip_stream);
 
 /* ------------------------------------------------------------------------
+ * Layers: the operators of a transformer's feed-forward block that are no
+ * single Stripe block -- the linear layer with its epilogue, the same over
+ * rows sorted by expert (a data-dependent, hence not affine, index space), the
+ * layer norm -- each with its gradients.  Handles work like those of blocks:
+ * create() validates and plans on the host, run() / backward() enqueue on
+ * `hip_stream` of the current device and return, the workspace is the caller's
+ * (set_workspace) or the handle's.
+ *
+ * Common to all of them:
+ *  - buffers are DEVICE pointers, aligned to their element type; a pointer that
+ *    is not is refused (STRIPE_ERR_MISALIGNED).  16-byte aligned pointers,
+ *    strides and feature counts run faster kernels, nothing else depends on them;
+ *  - sums, statistics and totals are fp32 (or wider); a bf16 result is rounded to
+ *    nearest even once, on store; zeros, infinities and NaN go the way the formula sends them;
+ *  - outputs must not overlap inputs or one another, except where stated;
+ *  - the same call on the same inputs gives the same bits (no atomics);
+ *  - a backward pass that needs a workspace and has none of the caller's allocates it on the
+ *    handle's first such call on a device, once per device, and frees it on destroy; under graph capture that first
+ *    call is refused with STRIPE_ERR_NOMEM before anything is launched.  Calls (or
+ *    graph replays) of one handle that overlap race on the workspace unless each was
+ *    recorded with a workspace of its own; calls that need none may overlap.
+ */
+typedef enum {
+  STRIPE_ACT_NONE = 0,       /* z */
+  STRIPE_ACT_RELU = 1,       /* max(z, 0); its derivative at 0 is 0 */
+  STRIPE_ACT_GELU = 2,       /* z Phi(z), Phi the normal distribution function */
+  STRIPE_ACT_GELU_TANH = 3,  /* z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) */
+  STRIPE_ACT_SILU = 4        /* z / (1 + exp(-z)) */
+} stripe_activation_t;
+
+/*
+ * Linear layer:  z = x W^T + b,  y = act(z) + r,  and its gradients for a given dy
+ *   dz = dy act'(z),  dx = dz W,  dW = dz^T x,  db = sum of dz over the rows      (dr = dy).
+ * x [rows][in_features], W [out_features][in_features], y and r [rows][out_features], b [out_features] in fp32.
+ * groups > 0: rows sorted by expert.  W [groups][out_features][in_features], b [groups][out_features], and `offsets`,
+ * groups + 1 int32 values on the DEVICE: rows offsets[g] .. offsets[g+1] - 1 meet W[g] and b[g].  Rows outside
+ * every group keep what y, pre and dx hold there; a group without rows gets dW[g] = 0, db[g] = 0.  Values
+ * are read as their running maximum, limited to 0 .. rows, so that no sequence of them leads outside the buffers.
+ */
+typedef struct {
+  int64_t rows;                        /* 0 .. 2^28 */
+  int64_t in_features, out_features;   /* 1 .. 2^24 */
+  int32_t groups;                      /* 0: one matrix for all rows; else 1 .. 4096 matrices */
+  stripe_dtype_t dtype;                /* of x, W, r, y, pre, dy, dx, dW: STRIPE_BF16 or STRIPE_F32 */
+  stripe_activation_t activation;
+  /* Strides in elements, 0 = dense.  x_row: rows of x and dx; w_row, w_group: rows and matrices of W and dW;
+   * y_row: rows of y, r, pre and dy. */
+  int64_t x_row, w_row, w_group, y_row;
+} stripe_linear_desc_t;
+
+typedef struct stripe_linear stripe_linear_t;
+
+typedef struct {
+  char forward[96], input_grad[96], weight_grad[96];   /* kernels that 16-byte aligned buffers run on */
+  int64_t workspace_bytes;
+} stripe_linear_info_t;
+
+stripe_status_t stripe_linear_create(const stripe_linear_desc_t* desc, stripe_linear_t** out);
+
+/* bias, residual, pre may be NULL (no b, no r, z not stored); pre receives z in `dtype`, for a later backward pass.
+ * offsets: NULL without groups.  residual may be y itself. */
+stripe_status_t stripe_linear_run(stripe_linear_t* lin, const void* x, const void* w, const float* bias, const void* residual, const int32_t* offsets,
+                                  void* y, void* pre, void* hip_stream);
+
+/* dx, dw, dbias: any of them may be NULL (not computed), then x, w may be NULL where only that gradient reads them.
+ * pre: z as run() stored it; NULL only with STRIPE_ACT_NONE. */
+stripe_status_t stripe_linear_backward(stripe_linear_t* lin, const void* dy, const void* x, const void* w, const void* pre, const int32_t* offsets, void* dx,
+                                       void* dw, float* dbias, void* hip_stream);
+
+stripe_status_t stripe_linear_workspace_size(const stripe_linear_t* lin, size_t* bytes);
+stripe_status_t stripe_linear_set_workspace(stripe_linear_t* lin, void* device_ptr, size_t bytes);   /* as stripe_block_set_workspace */
+stripe_status_t stripe_linear_query(const stripe_linear_t* lin, stripe_linear_info_t* info);
+void stripe_linear_destroy(stripe_linear_t* lin);
+
+/*
+ * Layer norm over the features of a row:  m = mean(x),  s = (mean((x - m)^2) + eps)^(-1/2),  h = (x - m) s,
+ *   y = h gamma + beta;   with g = dy gamma:  dx = s (g - mean(g) - h mean(g h)),  dgamma = sum of dy h over the rows,
+ *   dbeta = sum of dy.
+ * gamma, beta, their gradients, m and s are fp32.
+ */
+typedef struct {
+  int64_t rows;             /* 0 .. 2^30 */
+  int64_t features;         /* 1 .. 2^24 */
+  stripe_dtype_t dtype;     /* of x, y, dy, dx: STRIPE_BF16 or STRIPE_F32 */
+  double eps;               /* >= 0 and finite */
+  int64_t x_row, y_row;     /* strides in elements, 0 = dense: rows of x and dx, rows of y and dy */
+} stripe_norm_desc_t;
+
+typedef struct stripe_norm stripe_norm_t;
+
+stripe_status_t stripe_norm_create(const stripe_norm_desc_t* desc, stripe_norm_t** out);
+
+/* gamma, beta may be NULL (1, 0); mean, rstd [rows] may be NULL (not stored).  y may be x itself where the row strides agree. */
+stripe_status_t stripe_norm_run(stripe_norm_t* norm, const void* x, const float* gamma, const float* beta, void* y, float* mean, float* rstd,
+                                void* hip_stream);
+
+/* mean, rstd: as run() stored them.  dx, dgamma, dbeta: any of them may be NULL. */
+stripe_status_t stripe_norm_backward(stripe_norm_t* norm, const void* dy, const void* x, const float* gamma, const float* mean, const float* rstd, void* dx,
+                                     float* dgamma, float* dbeta, void* hip_stream);
+
+stripe_status_t stripe_norm_workspace_size(const stripe_norm_t* norm, size_t* bytes);
+stripe_status_t stripe_norm_set_workspace(stripe_norm_t* norm, void* device_ptr, size_t bytes);
+void stripe_norm_destroy(stripe_norm_t* norm);
+
+/* ------------------------------------------------------------------------
  * Autotiling (paper Section 3.3, Figures 4 and 5): host-only integer code.
  *
  * All three calls take the FLAT form of a block: the declaring root (no

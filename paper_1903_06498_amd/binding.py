@@ -27,11 +27,15 @@ _DIR = {"in": 0, "out": 1, "temp": 2}
 _DTYPE = {"i8": 0, "i32": 1, "bf16": 2, "f32": 3}
 _AGG = {"assign": 0, "add": 1, "max": 2, "min": 3, "mul": 4}
 _INTR = {"mul": 0, "copy": 1, "add": 2, "add_relu": 3}
+_ACT = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 EXPORTS = ("stripe_block_create", "stripe_block_create_for_path", "stripe_block_run", "stripe_block_run_static", "stripe_block_query",
            "stripe_block_workspace_size", "stripe_block_set_workspace",
            "stripe_block_destroy", "stripe_status_string", "stripe_last_error", "stripe_device_copy", "stripe_device_stream", "stripe_device_mfma",
-           "stripe_tile_cost", "stripe_tile_search", "stripe_block_tile", "stripe_desc_free")
+           "stripe_tile_cost", "stripe_tile_search", "stripe_block_tile", "stripe_desc_free",
+           "stripe_linear_create", "stripe_linear_run", "stripe_linear_backward", "stripe_linear_workspace_size", "stripe_linear_set_workspace",
+           "stripe_linear_query", "stripe_linear_destroy", "stripe_norm_create", "stripe_norm_run", "stripe_norm_backward",
+           "stripe_norm_workspace_size", "stripe_norm_set_workspace", "stripe_norm_destroy")
 
 
 class stripe_refinement_t(C.Structure):
@@ -71,6 +75,19 @@ class stripe_tile_model_t(C.Structure):
 class stripe_tile_cost_t(C.Structure):
     _fields_ = [("tiles", C.c_int64), ("lines_per_tile", C.c_int64), ("footprint_elems", C.c_int64),
                 ("work", C.c_int64), ("cost", C.c_double), ("admissible", C.c_int32)]
+
+
+class stripe_linear_desc_t(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("in_features", C.c_int64), ("out_features", C.c_int64), ("groups", C.c_int32), ("dtype", C.c_int),
+                ("activation", C.c_int), ("x_row", C.c_int64), ("w_row", C.c_int64), ("w_group", C.c_int64), ("y_row", C.c_int64)]
+
+
+class stripe_linear_info_t(C.Structure):
+    _fields_ = [("forward", C.c_char * 96), ("input_grad", C.c_char * 96), ("weight_grad", C.c_char * 96), ("workspace_bytes", C.c_int64)]
+
+
+class stripe_norm_desc_t(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("features", C.c_int64), ("dtype", C.c_int), ("eps", C.c_double), ("x_row", C.c_int64), ("y_row", C.c_int64)]
 
 
 class StripeError(RuntimeError):
@@ -130,6 +147,14 @@ def _load():
                                       C.POINTER(C.POINTER(stripe_block_desc_t))]
     lib.stripe_desc_free.restype = None
     lib.stripe_desc_free.argtypes = [C.POINTER(stripe_block_desc_t)]
+    ptr = C.c_void_p
+    for name, desc, run, backward in (("linear", stripe_linear_desc_t, 8, 9), ("norm", stripe_norm_desc_t, 7, 9)):
+        for call, args in (("create", [C.POINTER(desc), C.POINTER(handle)]), ("run", [handle] + [ptr] * run), ("backward", [handle] + [ptr] * backward),
+                           ("workspace_size", [handle, C.POINTER(C.c_size_t)]), ("set_workspace", [handle, ptr, C.c_size_t]), ("destroy", [handle])):
+            f = getattr(lib, f"stripe_{name}_{call}")
+            f.restype, f.argtypes = None if call == "destroy" else C.c_int, args
+    lib.stripe_linear_query.restype = C.c_int
+    lib.stripe_linear_query.argtypes = [handle, C.POINTER(stripe_linear_info_t)]
     return lib
 
 
@@ -410,3 +435,153 @@ class StripeBlock:
             self.close()
         except Exception:
             pass
+
+
+# ---- layers: the linear layer (dense, or rows sorted by expert) and the layer norm ------------
+def stripe_linear_create(rows: int, in_features: int, out_features: int, dtype: str, activation: str = "none", groups: int = 0, x_row: int = 0,
+                         w_row: int = 0, w_group: int = 0, y_row: int = 0) -> C.c_void_p:
+    d = stripe_linear_desc_t(int(rows), int(in_features), int(out_features), int(groups), _DTYPE[dtype], _ACT[activation], int(x_row), int(w_row),
+                             int(w_group), int(y_row))
+    h = C.c_void_p()
+    _check(lib.stripe_linear_create(C.byref(d), C.byref(h)))
+    return h
+
+
+def stripe_linear_query(handle) -> dict:
+    info = stripe_linear_info_t()
+    _check(lib.stripe_linear_query(handle, C.byref(info)))
+    return {"forward": info.forward.decode(), "input_grad": info.input_grad.decode(), "weight_grad": info.weight_grad.decode(),
+            "workspace_bytes": info.workspace_bytes}
+
+
+def stripe_norm_create(rows: int, features: int, dtype: str, eps: float = 1e-5, x_row: int = 0, y_row: int = 0) -> C.c_void_p:
+    d = stripe_norm_desc_t(int(rows), int(features), _DTYPE[dtype], float(eps), int(x_row), int(y_row))
+    h = C.c_void_p()
+    _check(lib.stripe_norm_create(C.byref(d), C.byref(h)))
+    return h
+
+
+class _Layer:
+    """What the layers' wrappers share: the handle, its workspace, the checks of a call's tensors.
+
+    Tensors are checked before anything is launched: element type, shape, strides as the handle was made for, device.  Every tensor
+    has to be on the current device, whose current stream the call runs on unless it is given one.
+    """
+
+    _name = ""
+
+    def _open(self, handle, dtype):
+        import torch
+        self.handle = handle
+        self._ws = None
+        n = C.c_size_t(0)
+        _check(getattr(lib, f"stripe_{self._name}_workspace_size")(handle, C.byref(n)))
+        self.workspace_bytes = int(n.value)
+        self._dtype = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+        self._f32, self._i32, self._device = torch.float32, torch.int32, torch.cuda.current_device
+
+    def set_workspace(self, tensor) -> None:
+        """Hand the handle a caller-owned device workspace (a contiguous torch CUDA tensor, kept alive here), or None."""
+        if tensor is not None and not (tensor.is_cuda and tensor.is_contiguous()):
+            raise ValueError("the workspace is a contiguous CUDA tensor")
+        ptr, size = (0, 0) if tensor is None else (tensor.data_ptr(), tensor.numel() * tensor.element_size())
+        _check(getattr(lib, f"stripe_{self._name}_set_workspace")(self.handle, ptr, size))
+        self._ws = tensor
+
+    def _ptr(self, what, t, dtype, shape, strides, device):
+        """The tensor's address; None (NULL) for None."""
+        if t is None:
+            return None
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+            raise ValueError(f"{what}: expected {dtype} of shape {tuple(shape)} on the current device (cuda:{device}), got {t.dtype} of shape "
+                             f"{tuple(t.shape)} on {t.device}")
+        if t.stride() != strides and any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), strides)):
+            raise ValueError(f"{what}: expected strides {strides}, got {t.stride()}")
+        return t.data_ptr()
+
+    def close(self) -> None:
+        if self.handle is not None:
+            getattr(lib, f"stripe_{self._name}_destroy")(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class StripeLinear(_Layer):
+    """Linear layer y = act(x W^T + b) + r and its gradients (see include/stripe.h); owns one handle.
+
+    groups > 0: rows sorted by expert, w [groups][out][in], bias [groups][out], offsets int32 [groups + 1].  Strides (x_row, w_row, w_group,
+    y_row; 0 = dense) are in elements: x_row of x and dx, w_row and w_group of w and dw, y_row of y, residual, pre and dy.
+    """
+
+    _name = "linear"
+
+    def __init__(self, rows: int, in_features: int, out_features: int, dtype: str = "bf16", activation: str = "none", groups: int = 0, x_row: int = 0,
+                 w_row: int = 0, w_group: int = 0, y_row: int = 0):
+        self.handle = None
+        self._open(stripe_linear_create(rows, in_features, out_features, dtype, activation, groups, x_row, w_row, w_group, y_row), dtype)
+        self.info = stripe_linear_query(self.handle)
+        w_row = w_row or in_features
+        lead, lead_stride = ((groups,), (w_group or out_features * w_row,)) if groups else ((), ())
+        self._x = ((rows, in_features), (x_row or in_features, 1))
+        self._y = ((rows, out_features), (y_row or out_features, 1))
+        self._w = (lead + (out_features, in_features), lead_stride + (w_row, 1))
+        self._b = (lead + (out_features,), (out_features, 1) if groups else (1,))
+        self._o = ((groups + 1,), (1,))
+
+    def run(self, x, w, y, bias=None, residual=None, offsets=None, pre=None, stream: Optional[int] = None) -> None:
+        """y = act(x W^T + bias) + residual; pre (optional) receives x W^T + bias for a backward pass."""
+        dev, p, t = self._device(), self._ptr, self._dtype
+        st = lib.stripe_linear_run(self.handle, p("x", x, t, *self._x, dev), p("w", w, t, *self._w, dev), p("bias", bias, self._f32, *self._b, dev),
+                                   p("residual", residual, t, *self._y, dev), p("offsets", offsets, self._i32, *self._o, dev), p("y", y, t, *self._y, dev),
+                                   p("pre", pre, t, *self._y, dev), current_stream() if stream is None else stream)
+        if st != STRIPE_OK:
+            raise StripeError(st, stripe_last_error())
+
+    def backward(self, dy, x, w, pre=None, offsets=None, dx=None, dw=None, dbias=None, stream: Optional[int] = None) -> None:
+        """The gradients that are given a tensor: dx, dw, dbias (that of the residual is dy itself)."""
+        dev, p, t = self._device(), self._ptr, self._dtype
+        st = lib.stripe_linear_backward(self.handle, p("dy", dy, t, *self._y, dev), p("x", x, t, *self._x, dev), p("w", w, t, *self._w, dev),
+                                        p("pre", pre, t, *self._y, dev), p("offsets", offsets, self._i32, *self._o, dev), p("dx", dx, t, *self._x, dev),
+                                        p("dw", dw, t, *self._w, dev), p("dbias", dbias, self._f32, *self._b, dev),
+                                        current_stream() if stream is None else stream)
+        if st != STRIPE_OK:
+            raise StripeError(st, stripe_last_error())
+
+
+class StripeNorm(_Layer):
+    """Layer norm over the features of a row and its gradients (see include/stripe.h); owns one handle.
+
+    x_row: stride of the rows of x and dx, y_row: of y and dy (elements, 0 = dense).
+    """
+
+    _name = "norm"
+
+    def __init__(self, rows: int, features: int, dtype: str = "bf16", eps: float = 1e-5, x_row: int = 0, y_row: int = 0):
+        self.handle = None
+        self._open(stripe_norm_create(rows, features, dtype, eps, x_row, y_row), dtype)
+        self._x, self._y = ((rows, features), (x_row or features, 1)), ((rows, features), (y_row or features, 1))
+        self._c, self._r = ((features,), (1,)), ((rows,), (1,))
+
+    def run(self, x, y, gamma=None, beta=None, mean=None, rstd=None, stream: Optional[int] = None) -> None:
+        """y = (x - mean) rstd gamma + beta; mean and rstd (optional) are stored for a backward pass."""
+        dev, p, f = self._device(), self._ptr, self._f32
+        st = lib.stripe_norm_run(self.handle, p("x", x, self._dtype, *self._x, dev), p("gamma", gamma, f, *self._c, dev), p("beta", beta, f, *self._c, dev),
+                                 p("y", y, self._dtype, *self._y, dev), p("mean", mean, f, *self._r, dev), p("rstd", rstd, f, *self._r, dev),
+                                 current_stream() if stream is None else stream)
+        if st != STRIPE_OK:
+            raise StripeError(st, stripe_last_error())
+
+    def backward(self, dy, x, mean, rstd, gamma=None, dx=None, dgamma=None, dbeta=None, stream: Optional[int] = None) -> None:
+        """The gradients that are given a tensor: dx, dgamma, dbeta."""
+        dev, p, f = self._device(), self._ptr, self._f32
+        st = lib.stripe_norm_backward(self.handle, p("dy", dy, self._dtype, *self._y, dev), p("x", x, self._dtype, *self._x, dev),
+                                      p("gamma", gamma, f, *self._c, dev), p("mean", mean, f, *self._r, dev), p("rstd", rstd, f, *self._r, dev),
+                                      p("dx", dx, self._dtype, *self._x, dev), p("dgamma", dgamma, f, *self._c, dev), p("dbeta", dbeta, f, *self._c, dev),
+                                      current_stream() if stream is None else stream)
+        if st != STRIPE_OK:
+            raise StripeError(st, stripe_last_error())
