@@ -149,7 +149,7 @@ stripe_status_t linear_run(stripe_linear_t* lin, const void* x, const void* w, c
   const stripe_linear_desc_t& d = lin->d;
   if (d.rows && (!x || !w || !y)) return api_fail(STRIPE_ERR_NULL, "x, w or y is NULL");
   if (const stripe_status_t st = check_offsets(lin, offsets); st != STRIPE_OK) return st;
-  const int64_t e = elem_size(d.dtype);
+  const int64_t e = elem_size(d.dtype), v = 16 / e;
   if (misaligned(x, e) || misaligned(w, e) || misaligned(residual, e) || misaligned(y, e) || misaligned(pre, e) || misaligned(bias, 4))
     return api_fail(STRIPE_ERR_MISALIGNED, "a buffer is not aligned to its element type");
   if (!d.rows) return STRIPE_OK;
@@ -164,7 +164,7 @@ stripe_status_t linear_run(stripe_linear_t* lin, const void* x, const void* w, c
   p.a_ld = d.x_row; p.b_ld = d.w_row; p.c_ld = d.y_row; p.b_group = d.w_group;
   p.rows = p.M = (int32_t)d.rows; p.N = (int32_t)d.out_features; p.K = (int32_t)d.in_features;
   p.groups = d.groups; p.act = d.activation;
-  p.vec = d.out_features % 4 == 0 && d.y_row % 4 == 0 && !misaligned(y, 4 * e) && !misaligned(residual, 4 * e) && !misaligned(pre, 4 * e);
+  p.vec = d.y_row % v == 0 && !misaligned(y, 16) && !misaligned(residual, 16) && !misaligned(pre, 16);
   return launched(launch_product(kForward, d.dtype, plan, aligned, p, (hipStream_t)hip_stream));
 }
 
@@ -206,14 +206,14 @@ stripe_status_t linear_backward(stripe_linear_t* lin, const void* dy, const void
     p.b = w; p.b_ld = d.w_row; p.b_group = d.w_group;
     p.c = dx; p.c_ld = d.x_row;
     p.M = (int32_t)d.rows; p.N = (int32_t)d.in_features; p.K = (int32_t)d.out_features;
-    p.vec = d.in_features % 4 == 0 && d.x_row % 4 == 0 && !misaligned(dx, 4 * e);
+    p.vec = d.x_row % v == 0 && !misaligned(dx, 16);
     if (const stripe_status_t st = launched(launch_product(kInputGrad, d.dtype, in_plan, aligned_w, p, stream)); st != STRIPE_OK) return st;
   }
   if (dw) {
     p.b = x; p.b_ld = d.x_row; p.b_group = 0;
     p.c = dw; p.c_ld = d.w_row; p.c_group = d.w_group;
     p.M = (int32_t)d.out_features; p.N = (int32_t)d.in_features; p.K = (int32_t)d.rows;
-    p.vec = d.in_features % 4 == 0 && d.w_row % 4 == 0 && (!d.groups || d.w_group % 4 == 0) && !misaligned(dw, 4 * e);
+    p.vec = d.w_row % v == 0 && (!d.groups || d.w_group % v == 0) && !misaligned(dw, 16);
     if (const stripe_status_t st = launched(launch_product(kWeightGrad, d.dtype, w_plan, aligned_x, p, stream)); st != STRIPE_OK) return st;
   }
   return STRIPE_OK;

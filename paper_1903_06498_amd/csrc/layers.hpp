@@ -54,7 +54,7 @@ struct ProductParams {
   int32_t tiles_m, tiles_n; // kForward, kInputGrad: tiles_m is an upper bound of the row tiles with groups
   int32_t splits;
   int32_t act;
-  int32_t vec;              // c, residual and pre take one store per row and four columns
+  int32_t vec;              // rows of c, residual and pre start at 16-byte boundaries
 };
 
 struct ProductPlan {

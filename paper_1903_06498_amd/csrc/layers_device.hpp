@@ -3,6 +3,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "layers.hpp"
 
 namespace stripe {
@@ -85,6 +87,21 @@ __device__ __forceinline__ float activate(float z, int act) {
     case STRIPE_ACT_GELU_TANH: return z * inv<T>(1.f + exp_of<T>(-2.f * kGeluA * (z + kGeluB * z * z * z)));
     case STRIPE_ACT_SILU: return z * inv<T>(1.f + exp_of<T>(-z));
     default: return z;
+  }
+}
+// Eight values: one branch for all of them.
+template <typename T>
+__device__ __forceinline__ void activate8(float (&v)[8], int act) {
+  auto each = [&](auto a) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = activate<T>(v[e], decltype(a)::value);
+  };
+  switch (act) {
+    case STRIPE_ACT_RELU: return each(std::integral_constant<int, STRIPE_ACT_RELU>{});
+    case STRIPE_ACT_GELU: return each(std::integral_constant<int, STRIPE_ACT_GELU>{});
+    case STRIPE_ACT_GELU_TANH: return each(std::integral_constant<int, STRIPE_ACT_GELU_TANH>{});
+    case STRIPE_ACT_SILU: return each(std::integral_constant<int, STRIPE_ACT_SILU>{});
+    default: return;
   }
 }
 template <typename T>

@@ -1,17 +1,18 @@
 // Products of the linear layer on the gfx950 matrix cores, dense or with rows sorted by group (see ProductKind for the three
 // layouts).
 //
-// A workgroup of four wavefronts (2 x 2) computes a tile of BM x BN outputs, in 32 x 32 fragments.  K tiles are 64 bytes deep (32 bf16 or
-// 16 fp32) and lie in a ring of four LDS stages:
-//   an operand whose reduction index is contiguous in memory ([row][k]): 64 bytes per row, 16-byte piece c of row r in slot
-//   c ^ ((r >> 2) & 3); a fragment is one 16-byte read;
+// A workgroup of four wavefronts (2 x 2) computes a tile of BM x BN outputs, in 32 x 32 fragments.  K tiles are 128 bytes deep (64 bf16 or
+// 32 fp32: whole cache lines of a row, where halves of them cost the L2 as much) and lie in two LDS stages:
+//   an operand whose reduction index is contiguous in memory ([row][k]): 128 bytes per row, 16-byte piece c of row r in slot
+//   c ^ ((r >> 1) & 7); a fragment is one 16-byte read;
 //   one whose row index is contiguous ([k][row]): as it lies in memory, a row of BM or BN elements per k, pieces swizzled by k; a bf16
 //   fragment is two transposing reads, an fp32 one four 4-byte reads.
 // Everything beyond the reduction's end is zero in both operands; rows and columns beyond the output repeat valid ones, whose sums are
 // never stored.
 #include <algorithm>
-#include <type_traits>
+#include <atomic>
 
+#include "kernels.hpp"
 #include "layers_device.hpp"
 
 namespace stripe {
@@ -20,7 +21,7 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kStages = 4, kDepthBytes = 64;
+constexpr int kStages = 2, kDepthBytes = 128, kSteps = kDepthBytes / 32;    // matrix-instruction steps of a K tile
 
 template <typename T>
 __device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
@@ -34,6 +35,20 @@ __device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
   }
 }
 
+// A wavefront's LDS-direct load: lane i's 16 bytes land at lds_off + 16 i.  Written as assembly because the compiler, which cannot tell a
+// load into one ring stage from fragment reads of another, would wait for all of them before every LDS read; the kernels
+// wait by count.  M0 is written here and nowhere else (no register array is indexed dynamically, nothing else reads M0).
+__device__ __forceinline__ void load_to_lds(const void* src, unsigned lds_off) {
+  const unsigned uniform = __builtin_amdgcn_readfirstlane(lds_off);
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(uniform) : "memory", "m0");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() {      // until at most N of the wavefront's loads are outstanding
+  static_assert(N >= 0 && N < 64, "the counter's range");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __attribute__((aligned(16))) uint32_t zero_piece[4];
+
 // One operand's part of a tile: WIDTH rows (or columns) of it.  STRIDED: stored [k][row].
 template <typename T, int WIDTH, bool STRIDED>
 struct Operand {
@@ -41,7 +56,7 @@ struct Operand {
   static constexpr int ROW = STRIDED ? WIDTH * (int)sizeof(T) : kDepthBytes;   // bytes of an LDS row
   static constexpr int STAGE = WIDTH * kDepthBytes, LOADS = STAGE / 4096;      // 16-byte pieces per lane and K tile
   static __device__ __forceinline__ int key(int r) {
-    if constexpr (!STRIDED) return (r >> 2) & 3;
+    if constexpr (!STRIDED) return (r >> 1) & 7;
     else if constexpr (sizeof(T) == 4) return 8 * ((r >> 2) & 1);              // the wavefront's halves read k and k + 4
     else return ROW >= 256 ? 4 * (r & 3) : 4 * ((r >> 1) & 1);                 // a transposing read takes four rows of k
   }
@@ -83,7 +98,18 @@ struct Operand {
 #pragma unroll
     for (int u = 0; u < LOADS; ++u) *(u32x4*)(stage + (u * 4 + wave) * 1024 + lane * 16) = from[u];
   }
-  // fragment of rows row0 .. row0 + 31 (row0 a multiple of 32), matrix-instruction step s (half a K tile): lane l holds row l & 31 and the
+  // Piece u of the next K tile as an LDS-direct load (whole pieces only); n: what is left of the reduction.  What does not exist is fetched
+  // from 16 zero bytes.
+  __device__ __forceinline__ void issue(int u, unsigned stage, int n, const void* zero) {
+    const bool in = k[u] < n && (!STRIDED || left[u] > 0);
+    load_to_lds(in ? (const void*)src[u] : zero, stage + (u * 4 + (threadIdx.x >> 6)) * 1024);
+    src[u] += step;
+  }
+  __device__ __forceinline__ void skip(int kt) {
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u) src[u] += (int64_t)kt * step;
+  }
+  // fragment of rows row0 .. row0 + 31 (row0 a multiple of 32), matrix-instruction step s: lane l holds row l & 31 and the
   // 16 bytes of k with number 2 s + (l >> 5)
   static __device__ __forceinline__ u32x4 fragment(const unsigned char* stage, int row0, int s) {
     const int lane = threadIdx.x & 63, fr = lane & 31, fh = lane >> 5;
@@ -151,54 +177,170 @@ __device__ __forceinline__ bool place(const ProductParams& p, Tile* t) {
   return true;
 }
 
-// Four neighbouring outputs of a row: the epilogue in fp32, then one rounding.
-template <typename T, int KIND>
-__device__ __forceinline__ void finish4(const ProductParams& p, int group, int64_t row, int col, f32x4 v) {
-  const int n = p.N - col < 4 ? p.N - col : 4;
-  const int64_t at = row * p.c_ld + col + (KIND == kWeightGrad ? group * p.c_group : 0);
-  T* c = (T*)p.c + at;
-  typedef T t4 __attribute__((ext_vector_type(4)));
-  if constexpr (KIND == kForward) {
-    if (p.bias) {
-      const float* b = p.bias + (int64_t)group * p.N + col;
+// Eight neighbouring outputs of a row: the epilogue in fp32, then one rounding.  at: their place in y, residual and pre (or dx, dW); n: how many of
+// them there are; r: the residual's, loaded before.
+template <typename T>
+struct Eight {
+  u32x4 v[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* q, int n, bool whole) {
+    if (whole) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (e < n) v[e] += b[e];
-    }
-    if (p.pre) {
-      T* z = (T*)p.pre + at;
-      if (p.vec) {
-        *(t4*)z = __builtin_convertvector(v, t4);
-      } else {
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = *(const u32x4*)(q + i * kVec<T>);
+    } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (e < n) z[e] = (T)v[e];
-      }
-    }
-    if (p.act != STRIPE_ACT_NONE) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = activate<T>(v[e], p.act);
-    }
-    if (p.residual) {
-      const T* r = (const T*)p.residual + at;
-      if (p.vec) {
-        v += __builtin_convertvector(*(const t4*)r, f32x4);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (e < n) v[e] += (float)r[e];
-      }
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = load_piece<T>(q + i * kVec<T>, n - i * kVec<T>);
     }
   }
-  if (p.vec) {
-    *(t4*)c = __builtin_convertvector(v, t4);
-  } else {
+  __device__ __forceinline__ void store(T* q, int n, bool whole) const {
+    if (whole) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (e < n) c[e] = (T)v[e];
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) *(u32x4*)(q + i * kVec<T>) = v[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) store_piece<T>(q + i * kVec<T>, v[i], n - i * kVec<T>);
+    }
+  }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+      float e[kVec<T>];
+      unpack<T>(v[i], e);
+#pragma unroll
+      for (int k = 0; k < kVec<T>; ++k) f[i * kVec<T> + k] = e[k];
+    }
+  }
+  __device__ __forceinline__ void set(const float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+      float e[kVec<T>];
+#pragma unroll
+      for (int k = 0; k < kVec<T>; ++k) e[k] = f[i * kVec<T> + k];
+      v[i] = pack<T>(e);
+    }
+  }
+};
+
+template <typename T, int KIND>
+__device__ __forceinline__ void finish(const ProductParams& p, int64_t at, int n, float (&v)[8], const float (&bias)[8], const Eight<T>& r) {
+  const bool whole = p.vec && n >= 8;
+  Eight<T> out;
+  if constexpr (KIND == kForward) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += bias[e];
+    if (p.pre) {
+      out.set(v);
+      out.store((T*)p.pre + at, n, whole);
+    }
+    activate8<T>(v, p.act);
+    if (p.residual) {
+      float f[8];
+      r.get(f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += f[e];
+    }
+  }
+  out.set(v);
+  out.store((T*)p.c + at, n, whole);
+}
+
+// Element v of lane l of a fragment is row 8 (v / 4) + 4 (l >> 5) + v % 4, column l & 31.  A wavefront lays 64 of its columns at a time into its
+// quarter of the idle ring (every wavefront is done with it), 256 bytes per row, 16-byte pieces swizzled by the row, and takes them out
+// again eight neighbouring columns per lane, eight rows at a time: 128 contiguous bytes of a bf16 row.  A loop and not 256 copies
+// of the epilogue: the residual's loads of four turns are on their way together, two sets of them.
+template <typename T, int KIND, int FM, int FN>
+__device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t, unsigned char* lds, const f32x16 (&acc)[FM][FN]) {
+  static_assert(FN % 2 == 0 && FM * 8192 * 4 <= kStages * 64 * (FM + FN) * kDepthBytes, "a wavefront's rows fit its quarter of the ring");
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
+  unsigned char* buf = lds + wave * (FM * 8192);
+  const int fr = lane & 31, fh = lane >> 5, sp = lane >> 3, sc = lane & 7;
+  const int64_t image = KIND == kWeightGrad ? (int64_t)t.group * p.M : 0;
+  const int64_t images = KIND == kWeightGrad && p.groups ? (int64_t)p.groups * p.M : p.M;
+  const int64_t base = (KIND == kWeightGrad ? t.group * p.c_group : 0) + (int64_t)t.m0 * p.c_ld;
+  auto key = [](int row) { return (row & 1) ^ (((row >> 2) & 1) << 3); };
+#pragma unroll
+  for (int jp = 0; jp < FN / 2; ++jp) {
+    const int col = t.n0 + (wn * FN + 2 * jp) * 32 + 8 * sc, n = p.N - col;
+    float bias[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bias[e] = 0.f;
+    const bool residual = KIND == kForward && p.residual && p.splits == 1;
+    if constexpr (KIND == kForward)
+      if (p.bias && p.splits == 1) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < n) bias[e] = p.bias[(int64_t)t.group * p.N + col + e];
+      }
+    auto load = [&](Eight<T> (&r)[4], int turn) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int row = wm * FM * 32 + (turn + q) * 8 + sp;
+        if (residual && row < t.m && n > 0) r[q].load((const T*)p.residual + base + (int64_t)row * p.c_ld + col, n, p.vec && n >= 8);
+      }
+    };
+    Eight<T> now[4], ahead[4];
+    load(now, 0);
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int row = 8 * (v / 4) + 4 * fh + v % 4;      // + 32 i: the key stays
+          *(float*)(buf + (32 * i + row) * 256 + (((8 * j + (fr >> 2)) ^ key(row)) << 4) + (fr & 3) * 4) = acc[i][2 * jp + j][v];
+        }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+    for (int turn = 0; turn < FM * 4; turn += 4) {
+      if (turn + 4 < FM * 4) load(ahead, turn + 4);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int local = (turn + q) * 8 + sp, row = wm * FM * 32 + local;
+        float v[8];
+        *(f32x4*)v = *(const f32x4*)(buf + local * 256 + (((2 * sc) ^ key(local)) << 4));
+        *(f32x4*)(v + 4) = *(const f32x4*)(buf + local * 256 + (((2 * sc + 1) ^ key(local)) << 4));
+        if (row < t.m && n > 0) {
+          if (p.splits > 1) {
+            float* to = p.partial + ((int64_t)blockIdx.y * images + image + t.m0 + row) * p.N + col;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (e < n) to[e] = v[e];
+          } else {
+            finish<T, KIND>(p, base + (int64_t)row * p.c_ld + col, n, v, bias, now[q]);
+          }
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) now[q] = ahead[q];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
+template <typename T, int KIND, int BM, int BN>
+__device__ __forceinline__ void init_operands(const ProductParams& p, const Tile& t, Operand<T, BM, KIND == kWeightGrad>& a, Operand<T, BN, KIND != kForward>& b) {
+  if constexpr (KIND == kWeightGrad) {
+    a.init((const T*)p.a + (int64_t)t.k0 * p.a_ld + t.m0, t.m, p.a_ld);
+    b.init((const T*)p.b + (int64_t)t.k0 * p.b_ld + t.n0, p.N - t.n0, p.b_ld);
+  } else {
+    const T* w = (const T*)p.b + (int64_t)t.group * p.b_group;
+    a.init((const T*)p.a + (int64_t)t.m0 * p.a_ld, t.m, p.a_ld);
+    b.init(KIND == kForward ? w + (int64_t)t.n0 * p.b_ld : w + t.n0, p.N - t.n0, p.b_ld);
+  }
+}
+// This workgroup's K tiles of `all`.
+__device__ __forceinline__ void own_k_tiles(const ProductParams& p, int all, int* kt0, int* kt1) {
+  *kt0 = 0;
+  *kt1 = all;
+  if (p.splits > 1) {
+    const int per = (all + p.splits - 1) / p.splits;
+    *kt0 = (int)blockIdx.y * per < all ? (int)blockIdx.y * per : all;
+    *kt1 = *kt0 + per < all ? *kt0 + per : all;
+  }
+}
+
+// Operands at any alignment: through registers, two stages of the ring, one K tile ahead.
 template <typename T, int KIND, int FM, int FN>
 __global__ __launch_bounds__(256) void product_kernel(const ProductParams p) {
   constexpr int BM = 64 * FM, BN = 64 * FN;
@@ -208,25 +350,13 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductParams p) {
   unsigned char *const lds_a = lds, *const lds_b = lds + kStages * A::STAGE;
   Tile t;
   if (!place<KIND, BM, BN>(p, &t)) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
+  const int wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
 
   A a;
   B b;
-  if constexpr (KIND == kWeightGrad) {
-    a.init((const T*)p.a + (int64_t)t.k0 * p.a_ld + t.m0, t.m, p.a_ld);
-    b.init((const T*)p.b + (int64_t)t.k0 * p.b_ld + t.n0, p.N - t.n0, p.b_ld);
-  } else {
-    const T* w = (const T*)p.b + (int64_t)t.group * p.b_group;
-    a.init((const T*)p.a + (int64_t)t.m0 * p.a_ld, t.m, p.a_ld);
-    b.init(KIND == kForward ? w + (int64_t)t.n0 * p.b_ld : w + t.n0, p.N - t.n0, p.b_ld);
-  }
-  // this workgroup's K tiles
-  int kt0 = 0, kt1 = (t.k + A::DEPTH - 1) / A::DEPTH;
-  if (p.splits > 1) {
-    const int per = (kt1 + p.splits - 1) / p.splits;
-    kt0 = (int)blockIdx.y * per < kt1 ? (int)blockIdx.y * per : kt1;
-    kt1 = kt0 + per < kt1 ? kt0 + per : kt1;
-  }
+  init_operands<T, KIND, BM, BN>(p, t, a, b);
+  int kt0, kt1;
+  own_k_tiles(p, (t.k + A::DEPTH - 1) / A::DEPTH, &kt0, &kt1);
 
   f32x16 acc[FM][FN];
 #pragma unroll
@@ -247,7 +377,7 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductParams p) {
     a.fetch(ra, kt + 1, t.k);
     b.fetch(rb, kt + 1, t.k);
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < kSteps; ++s) {
       u32x4 fa[FM], fb[FN];
 #pragma unroll
       for (int i = 0; i < FM; ++i) fa[i] = A::fragment(lds_a + stage * A::STAGE, (wm * FM + i) * 32, s);
@@ -260,41 +390,107 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductParams p) {
     }
   }
 
-  // Element v of lane l of a fragment is row 8 (v / 4) + 4 (l >> 5) + v % 4, column l & 31.  Each fragment goes through 4 KB of the idle ring
-  // that are the wavefront's own, pieces swizzled by the row, and leaves with four neighbouring columns per lane.
-  __syncthreads();
-  unsigned char* buf = lds + wave * 4096;
-  const int fr = lane & 31, fh = lane >> 5, sp = lane >> 3, sc = lane & 7;
-  const int64_t image = KIND == kWeightGrad ? (int64_t)t.group * p.M : 0;
-  const int64_t images = KIND == kWeightGrad && p.groups ? (int64_t)p.groups * p.M : p.M;
+  store_tile<T, KIND, FM, FN>(p, t, lds, acc);
+}
+
+// Operands in whole 16-byte pieces: LDS-direct loads, one barrier for each K tile, before its last step:
+//   steps 0 .. 2 of tile kt   + fragment reads one step ahead;  in step 0 the second half of tile kt + 1's loads,
+//   wait, barrier             tile kt + 1 is complete in LDS, and everybody has read the whole of tile kt,
+//   step 3 of tile kt         + fragment reads of tile kt + 1's step 0 + the first half of tile kt + 2's loads, into tile kt's stage.
+// Behind the last tile the loop loads zeros and reads fragments that nobody uses: the counts then never change.
+#define PRODUCT_FENCE() __builtin_amdgcn_sched_barrier(0)
+
+template <typename T, int KIND, int FM, int FN>
+__global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void product_stream_kernel(const ProductParams p) {
+  constexpr int BM = 64 * FM, BN = 64 * FN;
+  using A = Operand<T, BM, KIND == kWeightGrad>;
+  using B = Operand<T, BN, KIND != kForward>;
+  constexpr int LOADS = A::LOADS + B::LOADS, READS = FM + FN;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  unsigned char *const lds_a = lds, *const lds_b = lds + kStages * A::STAGE;
+  Tile t;
+  if (!place<KIND, BM, BN>(p, &t)) return;
+  const int wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
+  A a;
+  B b;
+  init_operands<T, KIND, BM, BN>(p, t, a, b);
+  int kt0, kt1;
+  own_k_tiles(p, (t.k + A::DEPTH - 1) / A::DEPTH, &kt0, &kt1);
+
+  f32x16 acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
+    for (int j = 0; j < FN; ++j)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int row = 8 * (v / 4) + 4 * fh + v % 4;
-        *(float*)(buf + row * 128 + (((fr >> 2) ^ (row & 7)) << 4) + (fr & 3) * 4) = acc[i][j][v];
-      }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+
+  if (kt0 < kt1) {
+    const void* zero = zero_piece;
+    asm volatile("" : "+s"(zero));       // held in registers
+    int left = (kt1 * A::DEPTH < t.k ? kt1 * A::DEPTH : t.k) - kt0 * A::DEPTH;      // of this workgroup's part of the reduction
+    a.skip(kt0);
+    b.skip(kt0);
+    auto load = [&](int first, int last, int stage) {
 #pragma unroll
-      for (int r8 = 0; r8 < 4; ++r8) {
-        const f32x4 v = *(const f32x4*)(buf + (8 * r8 + sp) * 128 + ((sc ^ sp) << 4));
-        const int row = (wm * FM + i) * 32 + 8 * r8 + sp, col = t.n0 + (wn * FN + j) * 32 + 4 * sc;
-        if (row >= t.m || col >= p.N) continue;
-        if (p.splits > 1) {
-          float* to = p.partial + ((int64_t)blockIdx.y * images + image + t.m0 + row) * p.N + col;
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (col + e < p.N) to[e] = v[e];
-        } else {
-          finish4<T, KIND>(p, t.group, (int64_t)t.m0 + row, col, v);
+      for (int u = 0; u < LOADS; ++u)
+        if (u >= first && u < last) {
+          if (u < A::LOADS) a.issue(u, stage * A::STAGE, left, zero);
+          else b.issue(u - A::LOADS, kStages * A::STAGE + stage * B::STAGE, left, zero);
         }
+    };
+    load(0, LOADS, 0);
+    left -= A::DEPTH;
+    load(0, LOADS / 2, 1);
+    wait_loads<LOADS / 2>();
+    asm volatile("s_barrier" ::: "memory");
+    u32x4 fa[2][FM], fb[2][FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) fb[0][j] = B::fragment(lds_b, (wn * FN + j) * 32, 0);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) fa[0][i] = A::fragment(lds_a, (wm * FM + i) * 32, 0);
+
+    const int tiles = kt1 - kt0;
+    for (int kt = 0; kt < tiles; ++kt) {
+      const int cur = kt & 1, nxt = cur ^ 1;
+      // fragment reads of one step, spread over its predecessor's rows of matrix instructions: B's and A's first before the others, none
+      // beside the last row, so that neither the barrier nor the next step meets a read that has only just begun
+      auto read = [&](int to, int stage, int st, int row) {
+        constexpr int GROUPS = FM > 1 ? FM - 1 : 1;
+#pragma unroll
+        for (int r = 0; r < READS; ++r)
+          if (r * GROUPS / READS == row) {
+            if (r < FN) fb[to][r] = B::fragment(lds_b + stage * B::STAGE, (wn * FN + r) * 32, st);
+            else fa[to][r - FN] = A::fragment(lds_a + stage * A::STAGE, (wm * FM + r - FN) * 32, st);
+          }
+      };
+#pragma unroll
+      for (int st = 0; st < kSteps; ++st) {
+        const int from = st & 1;
+        if (st == kSteps - 1) {
+          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+          asm volatile("s_barrier" ::: "memory");
+          PRODUCT_FENCE();
+        }
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+#pragma unroll
+          for (int j = 0; j < FN; ++j) {
+            const int jj = (i & 1) ? FN - 1 - j : j;      // one operand stays in place between two instructions
+            acc[i][jj] = mma<T>(fa[from][i], fb[from][jj], acc[i][jj]);
+          }
+          read(from ^ 1, st == kSteps - 1 ? nxt : cur, (st + 1) % kSteps, i);
+          if (st == 0) load(LOADS / 2 + i * (LOADS / 2) / FM, LOADS / 2 + (i + 1) * (LOADS / 2) / FM, nxt);
+          if (st == kSteps - 1) load(i * (LOADS / 2) / FM, (i + 1) * (LOADS / 2) / FM, cur);
+          PRODUCT_FENCE();
+        }
+        if (st == 0) left -= A::DEPTH;
       }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
     }
+    wait_loads<0>();
+  }
+  __syncthreads();
+  store_tile<T, KIND, FM, FN>(p, t, lds, acc);
 }
 
 // ---- dz = dy act'(z), and the bias gradient -------------------------------------
@@ -372,10 +568,33 @@ __global__ __launch_bounds__(256) void db_kernel(const DzParams p, int strips) {
 struct TileShape {
   int fm, fn;
 };
-constexpr TileShape kTiles[] = {{2, 2}};
+constexpr TileShape kTiles[] = {{2, 2}, {4, 4}};
+
+// A kernel's LDS beyond 64 KB has to be allowed once on each device.
+template <typename K>
+hipError_t allow_lds(K kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  if (const hipError_t e = hipGetDevice(&dev); e != hipSuccess) return e;
+  const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return hipSuccess;
+  const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
+template <typename T, int KIND, int FM, int FN>
+hipError_t launch_stream(const ProductParams& p, dim3 grid, hipStream_t stream) {
+  constexpr int bytes = kStages * 64 * (FM + FN) * kDepthBytes;
+  if constexpr (bytes > 65536) {
+    static std::atomic<uint64_t> done{0};
+    if (const hipError_t e = allow_lds(product_stream_kernel<T, KIND, FM, FN>, bytes, done); e != hipSuccess) return e;
+  }
+  product_stream_kernel<T, KIND, FM, FN><<<grid, dim3(256), bytes, stream>>>(p);
+  return hipGetLastError();
+}
 
 template <typename T, int KIND>
-hipError_t launch_kind(const ProductPlan& plan, ProductParams& p, hipStream_t stream) {
+hipError_t launch_kind(const ProductPlan& plan, bool aligned, ProductParams& p, hipStream_t stream) {
   const TileShape s = kTiles[plan.tile];
   const int bm = 64 * s.fm, bn = 64 * s.fn;
   p.tiles_n = (p.N + bn - 1) / bn;
@@ -388,36 +607,46 @@ hipError_t launch_kind(const ProductPlan& plan, ProductParams& p, hipStream_t st
     else total = ((int64_t)p.M / bm + std::min<int64_t>(p.groups, p.M)) * p.tiles_n;
   }
   const dim3 grid((unsigned)((total + 7) / 8 * 8), (unsigned)plan.splits);
+  if (aligned) {
+    if (plan.tile == 1) return launch_stream<T, KIND, 4, 4>(p, grid, stream);
+    return launch_stream<T, KIND, 2, 2>(p, grid, stream);
+  }
   product_kernel<T, KIND, 2, 2><<<grid, dim3(256), kStages * (bm + bn) * kDepthBytes, stream>>>(p);
   return hipGetLastError();
 }
 
 template <typename T>
-hipError_t launch_type(ProductKind kind, const ProductPlan& plan, ProductParams& p, hipStream_t stream) {
+hipError_t launch_type(ProductKind kind, const ProductPlan& plan, bool aligned, ProductParams& p, hipStream_t stream) {
   switch (kind) {
-    case kForward: return launch_kind<T, kForward>(plan, p, stream);
-    case kInputGrad: return launch_kind<T, kInputGrad>(plan, p, stream);
-    default: return launch_kind<T, kWeightGrad>(plan, p, stream);
+    case kForward: return launch_kind<T, kForward>(plan, aligned, p, stream);
+    case kInputGrad: return launch_kind<T, kInputGrad>(plan, aligned, p, stream);
+    default: return launch_kind<T, kWeightGrad>(plan, aligned, p, stream);
   }
 }
 
 }  // namespace
 
 ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, bool aligned) {
-  (void)kind, (void)dtype, (void)rows, (void)in, (void)out, (void)groups, (void)aligned;
-  return {};
+  (void)dtype;
+  ProductPlan plan;
+  const int64_t m = kind == kWeightGrad ? out : rows, n = kind == kForward ? out : in;
+  if (aligned) {
+    const int64_t row_tiles = kind == kWeightGrad ? (m + 255) / 256 * std::max(1, groups) : m / 256 + std::max(1, groups / 2);
+    if (row_tiles * ((n + 255) / 256) >= 192) plan.tile = 1;
+    const int forced = tune_int("product_tile", -1);
+    if (forced >= 0 && forced < (int)(sizeof kTiles / sizeof *kTiles)) plan.tile = forced;
+  }
+  return plan;
 }
 
 std::string product_name(ProductKind kind, int dtype, const ProductPlan& plan, bool aligned) {
-  (void)aligned;
   const TileShape s = kTiles[plan.tile];
-  return std::string("product_") + (kind == kForward ? "nt_" : kind == kInputGrad ? "nn_" : "tn_") + (dtype == STRIPE_F32 ? "f32_" : "bf16_") +
+  return std::string(aligned ? "product_stream_" : "product_") + (kind == kForward ? "nt_" : kind == kInputGrad ? "nn_" : "tn_") + (dtype == STRIPE_F32 ? "f32_" : "bf16_") +
          std::to_string(64 * s.fm) + "x" + std::to_string(64 * s.fn);
 }
 
 hipError_t launch_product(ProductKind kind, int dtype, const ProductPlan& plan, bool aligned, ProductParams p, hipStream_t stream) {
-  (void)aligned;
-  return dtype == STRIPE_F32 ? launch_type<float>(kind, plan, p, stream) : launch_type<__bf16>(kind, plan, p, stream);
+  return dtype == STRIPE_F32 ? launch_type<float>(kind, plan, aligned, p, stream) : launch_type<__bf16>(kind, plan, aligned, p, stream);
 }
 
 // (one more with groups: a single empty group's zeros come from db_kernel)
