@@ -302,9 +302,9 @@ stripe_status_t stripe_device_mfma(const void* operands, void* out, int iters, i
  *    nearest even once, on store; zeros, infinities and NaN go the way the formula sends them;
  *  - outputs must not overlap inputs or one another, except where stated;
  *  - the same call on the same inputs gives the same bits (no atomics);
- *  - a backward pass that needs a workspace and has none of the caller's allocates it on the
- *    handle's first such call on a device, once per device, and frees it on destroy; under graph capture that first
- *    call is refused with STRIPE_ERR_NOMEM before anything is launched.  Calls (or
+ *  - a call that needs a workspace and has none of the caller's allocates it, once per
+ *    device, and keeps it until the handle is destroyed; under graph capture such a first call
+ *    is refused with STRIPE_ERR_NOMEM before anything is launched.  Calls (or
  *    graph replays) of one handle that overlap race on the workspace unless each was
  *    recorded with a workspace of its own; calls that need none may overlap.
  */

@@ -60,12 +60,15 @@ struct ProductParams {
 struct ProductPlan {
   int tile = 0;             // index into the tile table
   int splits = 1;
+  int few = 0;              // kForward: the kernel for few rows, 16 times as many at a time (product_rows.hip)
   int64_t ws_bytes = 0;     // partial images
 };
 ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, bool aligned);
 std::string product_name(ProductKind kind, int dtype, const ProductPlan& plan, bool aligned);
 // aligned: operands and strides allow 16-byte fetches, the contiguous extents are whole 16-byte pieces
 hipError_t launch_product(ProductKind kind, int dtype, const ProductPlan& plan, bool aligned, ProductParams p, hipStream_t stream);
+
+hipError_t launch_product_rows(int dtype, int fm, ProductParams p, hipStream_t stream);
 
 // dz = dy act'(z) (dz == nullptr: not stored; act none: not needed) and db = sums of dz over each group's rows (db == nullptr: not
 // computed).  partial: fp32, dz_slots(rows, groups) x out, unused if db is nullptr or there is one slot.

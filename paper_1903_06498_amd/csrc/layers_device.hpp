@@ -206,6 +206,18 @@ __device__ __forceinline__ void group_rows(const int32_t* offsets, int groups, i
   }
 }
 
+// The group of a row, -1 where it is none's.
+__device__ __forceinline__ int group_of_row(const int32_t* offsets, int groups, int rows, int row) {
+  int end = limited(offsets[0], rows);
+  for (int base = 0; base < groups; base += 64) {
+    const GroupChunk c = group_chunk(offsets, groups, rows, base, end, 0, 1);
+    const uint64_t in = __ballot(c.start <= row && row < c.end);
+    if (in) return base + __builtin_ctzll(in);
+    end = lane_value(c.end, 63);
+  }
+  return -1;
+}
+
 // Logical number of workgroup b when `total` of the grid's workgroups (a multiple of 8, at least total) have work: hardware numbers
 // go round the 8 XCDs, each XCD gets a contiguous run of logical ones.  false: nothing to do.
 __device__ __forceinline__ bool logical_number(unsigned b, unsigned total, unsigned* l) {

@@ -2,7 +2,7 @@
 // layouts).
 //
 // A workgroup of four wavefronts (2 x 2) computes a tile of BM x BN outputs, in 32 x 32 fragments.  K tiles are 128 bytes deep (64 bf16 or
-// 32 fp32: whole cache lines of a row, where halves of them cost the L2 as much) and lie in two LDS stages:
+// 32 fp32: whole cache lines of a row, where halves of them cost the L2 as much) and lie in a ring of LDS stages:
 //   an operand whose reduction index is contiguous in memory ([row][k]): 128 bytes per row, 16-byte piece c of row r in slot
 //   c ^ ((r >> 1) & 7); a fragment is one 16-byte read;
 //   one whose row index is contiguous ([k][row]): as it lies in memory, a row of BM or BN elements per k, pieces swizzled by k; a bf16
@@ -11,6 +11,7 @@
 // never stored.
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 
 #include "kernels.hpp"
 #include "layers_device.hpp"
@@ -21,7 +22,7 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kStages = 2, kDepthBytes = 128, kSteps = kDepthBytes / 32;    // matrix-instruction steps of a K tile
+constexpr int kDepthBytes = 128, kSteps = kDepthBytes / 32;    // matrix-instruction steps of a K tile
 
 template <typename T>
 __device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
@@ -249,7 +250,7 @@ __device__ __forceinline__ void finish(const ProductParams& p, int64_t at, int n
 // of the epilogue: the residual's loads of four turns are on their way together, two sets of them.
 template <typename T, int KIND, int FM, int FN>
 __device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t, unsigned char* lds, const f32x16 (&acc)[FM][FN]) {
-  static_assert(FN % 2 == 0 && FM * 8192 * 4 <= kStages * 64 * (FM + FN) * kDepthBytes, "a wavefront's rows fit its quarter of the ring");
+  static_assert(FN % 2 == 0 && FM * 8192 * 4 <= 2 * 64 * (FM + FN) * kDepthBytes, "a wavefront's rows fit its quarter of two stages");
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
   unsigned char* buf = lds + wave * (FM * 8192);
   const int fr = lane & 31, fh = lane >> 5, sp = lane >> 3, sc = lane & 7;
@@ -301,10 +302,9 @@ __device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t
         *(f32x4*)(v + 4) = *(const f32x4*)(buf + local * 256 + (((2 * sc + 1) ^ key(local)) << 4));
         if (row < t.m && n > 0) {
           if (p.splits > 1) {
-            float* to = p.partial + ((int64_t)blockIdx.y * images + image + t.m0 + row) * p.N + col;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (e < n) to[e] = v[e];
+            Eight<float> out;
+            out.set(v);
+            out.store(p.partial + ((int64_t)blockIdx.y * images + image + t.m0 + row) * p.N + col, n, false);
           } else {
             finish<T, KIND>(p, base + (int64_t)row * p.c_ld + col, n, v, bias, now[q]);
           }
@@ -347,7 +347,7 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductParams p) {
   using A = Operand<T, BM, KIND == kWeightGrad>;
   using B = Operand<T, BN, KIND != kForward>;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  unsigned char *const lds_a = lds, *const lds_b = lds + kStages * A::STAGE;
+  unsigned char *const lds_a = lds, *const lds_b = lds + 2 * A::STAGE;
   Tile t;
   if (!place<KIND, BM, BN>(p, &t)) return;
   const int wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
@@ -394,20 +394,21 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductParams p) {
 }
 
 // Operands in whole 16-byte pieces: LDS-direct loads, one barrier for each K tile, before its last step:
-//   steps 0 .. 2 of tile kt   + fragment reads one step ahead;  in step 0 the second half of tile kt + 1's loads,
+//   steps 0 .. 2 of tile kt   + fragment reads one step ahead;  in step 0 the second half of a tile's loads,
 //   wait, barrier             tile kt + 1 is complete in LDS, and everybody has read the whole of tile kt,
-//   step 3 of tile kt         + fragment reads of tile kt + 1's step 0 + the first half of tile kt + 2's loads, into tile kt's stage.
+//   step 3 of tile kt         + fragment reads of tile kt + 1's step 0 + the first half of tile kt + S's loads, into tile kt's stage,
+// S the stages of the ring (step 0: tile kt + S - 1's second half).
 // Behind the last tile the loop loads zeros and reads fragments that nobody uses: the counts then never change.
 #define PRODUCT_FENCE() __builtin_amdgcn_sched_barrier(0)
 
-template <typename T, int KIND, int FM, int FN>
+template <typename T, int KIND, int FM, int FN, int S>
 __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void product_stream_kernel(const ProductParams p) {
   constexpr int BM = 64 * FM, BN = 64 * FN;
   using A = Operand<T, BM, KIND == kWeightGrad>;
   using B = Operand<T, BN, KIND != kForward>;
   constexpr int LOADS = A::LOADS + B::LOADS, READS = FM + FN;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  unsigned char *const lds_a = lds, *const lds_b = lds + kStages * A::STAGE;
+  unsigned char *const lds_a = lds, *const lds_b = lds + S * A::STAGE;
   Tile t;
   if (!place<KIND, BM, BN>(p, &t)) return;
   const int wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
@@ -436,13 +437,16 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void product_stream_ker
       for (int u = 0; u < LOADS; ++u)
         if (u >= first && u < last) {
           if (u < A::LOADS) a.issue(u, stage * A::STAGE, left, zero);
-          else b.issue(u - A::LOADS, kStages * A::STAGE + stage * B::STAGE, left, zero);
+          else b.issue(u - A::LOADS, S * A::STAGE + stage * B::STAGE, left, zero);
         }
     };
-    load(0, LOADS, 0);
-    left -= A::DEPTH;
-    load(0, LOADS / 2, 1);
-    wait_loads<LOADS / 2>();
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) {
+      load(0, LOADS, i);
+      left -= A::DEPTH;
+    }
+    load(0, LOADS / 2, S - 1);
+    wait_loads<LOADS / 2 + (S - 2) * LOADS>();
     asm volatile("s_barrier" ::: "memory");
     u32x4 fa[2][FM], fb[2][FN];
 #pragma unroll
@@ -451,8 +455,9 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void product_stream_ker
     for (int i = 0; i < FM; ++i) fa[0][i] = A::fragment(lds_a, (wm * FM + i) * 32, 0);
 
     const int tiles = kt1 - kt0;
+    int cur = 0, before = S - 1;      // stages of tile kt and of tile kt - 1
     for (int kt = 0; kt < tiles; ++kt) {
-      const int cur = kt & 1, nxt = cur ^ 1;
+      const int nxt = cur + 1 == S ? 0 : cur + 1;
       // fragment reads of one step, spread over its predecessor's rows of matrix instructions: B's and A's first before the others, none
       // beside the last row, so that neither the barrier nor the next step meets a read that has only just begun
       auto read = [&](int to, int stage, int st, int row) {
@@ -468,7 +473,7 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void product_stream_ker
       for (int st = 0; st < kSteps; ++st) {
         const int from = st & 1;
         if (st == kSteps - 1) {
-          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((S - 2) * LOADS) : "memory");
           asm volatile("s_barrier" ::: "memory");
           PRODUCT_FENCE();
         }
@@ -480,17 +485,59 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void product_stream_ker
             acc[i][jj] = mma<T>(fa[from][i], fb[from][jj], acc[i][jj]);
           }
           read(from ^ 1, st == kSteps - 1 ? nxt : cur, (st + 1) % kSteps, i);
-          if (st == 0) load(LOADS / 2 + i * (LOADS / 2) / FM, LOADS / 2 + (i + 1) * (LOADS / 2) / FM, nxt);
+          if (st == 0) load(LOADS / 2 + i * (LOADS / 2) / FM, LOADS / 2 + (i + 1) * (LOADS / 2) / FM, before);
           if (st == kSteps - 1) load(i * (LOADS / 2) / FM, (i + 1) * (LOADS / 2) / FM, cur);
           PRODUCT_FENCE();
         }
         if (st == 0) left -= A::DEPTH;
       }
+      before = cur;
+      cur = nxt;
     }
     wait_loads<0>();
   }
   __syncthreads();
   store_tile<T, KIND, FM, FN>(p, t, lds, acc);
+}
+
+// The slices of a split reduction, added in their order, and the epilogue: one row (blockIdx.x / strips), 2048 columns.
+template <typename T, int KIND>
+__global__ __launch_bounds__(256) void product_join_kernel(const ProductParams p, int strips) {
+  const int row = (int)(blockIdx.x / (unsigned)strips), col = ((int)(blockIdx.x % (unsigned)strips) * 256 + (int)threadIdx.x) * 8, n = p.N - col;
+  const int64_t images = KIND == kWeightGrad && p.groups ? (int64_t)p.groups * p.M : p.M;
+  int group = 0;
+  int64_t at = (int64_t)row * p.c_ld + col;
+  if (KIND == kWeightGrad) {
+    group = row / p.M;
+    at = group * p.c_group + (int64_t)(row % p.M) * p.c_ld + col;
+  } else if (p.groups) {
+    group = group_of_row(p.offsets, p.groups, p.rows, row);
+    if (group < 0) return;
+  }
+  if (n <= 0) return;
+  float v[8], bias[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = bias[e] = 0.f;
+  const float* from = p.partial + (int64_t)row * p.N + col;
+#pragma unroll 4
+  for (int s = 0; s < p.splits; ++s) {
+    Eight<float> part;
+    part.load(from + (int64_t)s * images * p.N, n, false);
+    float f[8];
+    part.get(f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += f[e];
+  }
+  Eight<T> r;
+  if constexpr (KIND == kForward) {
+    if (p.bias) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < n) bias[e] = p.bias[(int64_t)group * p.N + col + e];
+    }
+    if (p.residual) r.load((const T*)p.residual + at, n, p.vec && n >= 8);
+  }
+  finish<T, KIND>(p, at, n, v, bias, r);
 }
 
 // ---- dz = dy act'(z), and the bias gradient -------------------------------------
@@ -566,9 +613,11 @@ __global__ __launch_bounds__(256) void db_kernel(const DzParams p, int strips) {
 
 // ---- host ---------------------------------------------------------------------
 struct TileShape {
-  int fm, fn;
+  int fm, fn, stages, resident;      // resident: workgroups that fit a CU
 };
-constexpr TileShape kTiles[] = {{2, 2}, {4, 4}};
+// 3: the tile that fills the chip with few rows; 2: one workgroup for a CU, whose ring then holds three K tiles ahead
+constexpr TileShape kTiles[] = {{2, 2, 2, 2}, {4, 4, 2, 1}, {2, 2, 4, 1}, {1, 2, 3, 2}};
+constexpr int kTileCount = sizeof kTiles / sizeof *kTiles;
 
 // A kernel's LDS beyond 64 KB has to be allowed once on each device.
 template <typename K>
@@ -582,14 +631,15 @@ hipError_t allow_lds(K kernel, int bytes, std::atomic<uint64_t>& done) {
   return e;
 }
 
-template <typename T, int KIND, int FM, int FN>
+template <typename T, int KIND, int TILE>
 hipError_t launch_stream(const ProductParams& p, dim3 grid, hipStream_t stream) {
-  constexpr int bytes = kStages * 64 * (FM + FN) * kDepthBytes;
+  constexpr TileShape s = kTiles[TILE];
+  constexpr int bytes = s.stages * 64 * (s.fm + s.fn) * kDepthBytes;
   if constexpr (bytes > 65536) {
     static std::atomic<uint64_t> done{0};
-    if (const hipError_t e = allow_lds(product_stream_kernel<T, KIND, FM, FN>, bytes, done); e != hipSuccess) return e;
+    if (const hipError_t e = allow_lds(product_stream_kernel<T, KIND, s.fm, s.fn, s.stages>, bytes, done); e != hipSuccess) return e;
   }
-  product_stream_kernel<T, KIND, FM, FN><<<grid, dim3(256), bytes, stream>>>(p);
+  product_stream_kernel<T, KIND, s.fm, s.fn, s.stages><<<grid, dim3(256), bytes, stream>>>(p);
   return hipGetLastError();
 }
 
@@ -607,11 +657,20 @@ hipError_t launch_kind(const ProductPlan& plan, bool aligned, ProductParams& p, 
     else total = ((int64_t)p.M / bm + std::min<int64_t>(p.groups, p.M)) * p.tiles_n;
   }
   const dim3 grid((unsigned)((total + 7) / 8 * 8), (unsigned)plan.splits);
+  hipError_t e;
   if (aligned) {
-    if (plan.tile == 1) return launch_stream<T, KIND, 4, 4>(p, grid, stream);
-    return launch_stream<T, KIND, 2, 2>(p, grid, stream);
+    e = plan.tile == 0 ? launch_stream<T, KIND, 0>(p, grid, stream) : plan.tile == 1 ? launch_stream<T, KIND, 1>(p, grid, stream)
+      : plan.tile == 2 ? launch_stream<T, KIND, 2>(p, grid, stream) : launch_stream<T, KIND, 3>(p, grid, stream);
+  } else {
+    const int bytes = 2 * (bm + bn) * kDepthBytes;
+    if (plan.tile == 0) product_kernel<T, KIND, 2, 2><<<grid, dim3(256), bytes, stream>>>(p);
+    else product_kernel<T, KIND, 1, 2><<<grid, dim3(256), bytes, stream>>>(p);
+    e = hipGetLastError();
   }
-  product_kernel<T, KIND, 2, 2><<<grid, dim3(256), kStages * (bm + bn) * kDepthBytes, stream>>>(p);
+  if (e != hipSuccess || plan.splits == 1) return e;
+  const int strips = (p.N + 2047) / 2048;
+  const int64_t rows = KIND == kWeightGrad ? (int64_t)std::max(1, p.groups) * p.M : p.M;
+  product_join_kernel<T, KIND><<<dim3((unsigned)(rows * strips)), dim3(256), 0, stream>>>(p, strips);
   return hipGetLastError();
 }
 
@@ -626,26 +685,61 @@ hipError_t launch_type(ProductKind kind, const ProductPlan& plan, bool aligned, 
 
 }  // namespace
 
+// The tile and the slices of the reduction with the smallest estimated time, in us.  A K tile takes a workgroup its matrix instructions (of all
+// workgroups on its CU; at three quarters of the peak rate) or the way of its operands through the ring, whichever is longer.
 ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, bool aligned) {
-  (void)dtype;
   ProductPlan plan;
-  const int64_t m = kind == kWeightGrad ? out : rows, n = kind == kForward ? out : in;
-  if (aligned) {
-    const int64_t row_tiles = kind == kWeightGrad ? (m + 255) / 256 * std::max(1, groups) : m / 256 + std::max(1, groups / 2);
-    if (row_tiles * ((n + 255) / 256) >= 192) plan.tile = 1;
-    const int forced = tune_int("product_tile", -1);
-    if (forced >= 0 && forced < (int)(sizeof kTiles / sizeof *kTiles)) plan.tile = forced;
+  // few rows (of a group, on average): W is read once, whatever is computed with it.  4096 x 4096 bf16: 1 row 8.4 us, 16 10.5, 32 13.8 where 128 x 128
+  // tiles take 42; 64 groups of 2048 x 1024: 16 rows 14.2 against 25.1, 256 53 against 59, 512 67 against 60.
+  if (kind == kForward && (rows <= 32 || (groups && rows <= 4 * (int64_t)groups))) plan.few = rows <= 16 || groups ? 1 : 2;
+  if (const int forced = tune_int("product_few", -1); forced >= 0 && kind == kForward) plan.few = forced;
+  if (plan.few || !rows) return plan;
+  const int64_t m = kind == kWeightGrad ? out : rows, n = kind == kForward ? out : in, k = kind == kForward ? in : kind == kInputGrad ? out : rows;
+  const int64_t images = kind == kWeightGrad ? std::max(1, groups) : 1, depth = dtype == STRIPE_F32 ? 32 : 64;
+  const double latency = aligned ? 0.62 : 1.2, rate = dtype == STRIPE_F32 ? 0.55 : 7.0;      // us of a fetch; Mflop per us of a CU
+  double best = __builtin_huge_val();
+  const int forced_tile = tune_int("product_tile", -1), forced_splits = tune_int("product_splits", 0);
+  for (int tile = 0; tile < kTileCount; ++tile) {
+    const TileShape s = kTiles[tile];
+    if (!aligned && (tile == 1 || tile == 2)) continue;
+    if (forced_tile >= 0 && tile != forced_tile && (aligned || forced_tile == 0 || forced_tile == 3)) continue;
+    const int64_t bm = 64 * s.fm, bn = 64 * s.fn;
+    const double row_tiles = kind == kWeightGrad ? (double)((m + bm - 1) / bm * images)
+                             : groups            ? (double)m / bm + 0.5 * std::min<double>(groups, (double)m)
+                                                 : (double)((m + bm - 1) / bm);
+    const double tiles = row_tiles * (double)((n + bn - 1) / bn), depth_of = kind == kWeightGrad && groups ? (double)k / groups : (double)k;
+    const int64_t k_tiles = std::max<int64_t>(1, (int64_t)((depth_of + depth - 1) / depth));
+    for (int splits = 1; splits <= 16; ++splits) {
+      if (splits > 1 && (k_tiles < 2 * splits || (forced_splits && splits != forced_splits))) continue;
+      const int64_t bytes = splits > 1 ? splits * images * m * n * 4 : 0;
+      if (bytes > (64 << 20)) continue;
+      const double workgroups = std::max(1.0, tiles * splits), resident = s.resident;
+      const double rounds = std::ceil(workgroups / (256 * resident)), together = std::min(resident, std::ceil(workgroups / 256));
+      const double flop = 2e-6 * bm * bn * depth / rate;
+      const double each = std::max(latency / (s.stages - 1), together * flop), store = 1.0 + together * bm * bn / 20000.0;
+      double us = 3.0 + rounds * (std::ceil((double)k_tiles / splits) * each + store);
+      if (splits > 1) us += 2.5 + (double)bytes * 2 / 4e6;
+      if (us < best) {
+        best = us;
+        plan.tile = tile;
+        plan.splits = splits;
+        plan.ws_bytes = bytes;
+      }
+    }
   }
   return plan;
 }
 
 std::string product_name(ProductKind kind, int dtype, const ProductPlan& plan, bool aligned) {
+  if (plan.few) return std::string("product_rows_") + (dtype == STRIPE_F32 ? "f32_" : "bf16_") + std::to_string(16 * plan.few) + "x16";
   const TileShape s = kTiles[plan.tile];
   return std::string(aligned ? "product_stream_" : "product_") + (kind == kForward ? "nt_" : kind == kInputGrad ? "nn_" : "tn_") + (dtype == STRIPE_F32 ? "f32_" : "bf16_") +
-         std::to_string(64 * s.fm) + "x" + std::to_string(64 * s.fn);
+         std::to_string(64 * s.fm) + "x" + std::to_string(64 * s.fn) + (aligned ? "_s" + std::to_string(s.stages) : "") +
+         (plan.splits > 1 ? "_k" + std::to_string(plan.splits) : "");
 }
 
 hipError_t launch_product(ProductKind kind, int dtype, const ProductPlan& plan, bool aligned, ProductParams p, hipStream_t stream) {
+  if (plan.few) return launch_product_rows(dtype, plan.few, p, stream);
   return dtype == STRIPE_F32 ? launch_type<float>(kind, plan, aligned, p, stream) : launch_type<__bf16>(kind, plan, aligned, p, stream);
 }
 
