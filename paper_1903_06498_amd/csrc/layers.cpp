@@ -120,7 +120,9 @@ stripe_status_t linear_create(const stripe_linear_desc_t* desc, stripe_linear_t*
   auto lin = std::make_unique<stripe_linear>();
   lin->d = d;
   const int64_t v = 16 / elem_size(d.dtype);
-  lin->wide = d.in_features % v == 0 && d.out_features % v == 0 && d.x_row % v == 0 && d.w_row % v == 0 && d.y_row % v == 0 && (!d.groups || d.w_group % v == 0);
+  // (and a tile's rows, at most 256, span less than 2^31 bytes: the kernels that load them have 32-bit offsets)
+  const int64_t most = (int64_t)1 << 20;
+  lin->wide = d.x_row <= most && d.w_row <= most && d.y_row <= most && d.in_features % v == 0 && d.out_features % v == 0 && d.x_row % v == 0 && d.w_row % v == 0 && d.y_row % v == 0 && (!d.groups || d.w_group % v == 0);
   for (int aligned = 0; aligned < 2; ++aligned)
     for (int k = 0; k < 3; ++k) {
       lin->plan[aligned][k] = plan_product((ProductKind)k, d.dtype, d.rows, d.in_features, d.out_features, d.groups, aligned != 0);

@@ -1,8 +1,9 @@
 // Products of the linear layer on the gfx950 matrix cores, dense or with rows sorted by group (see ProductKind for the three
 // layouts).
 //
-// A workgroup of four wavefronts (2 x 2) computes a tile of BM x BN outputs, in 32 x 32 fragments.  K tiles are 128 bytes deep (64 bf16 or
-// 32 fp32: whole cache lines of a row, where halves of them cost the L2 as much) and lie in a ring of LDS stages:
+// A workgroup of four wavefronts (2 x 2) computes a tile of BM x BN outputs, in 16 x 16 fragments (32 x 32 ones do as many operations per cycle, but
+// draw more power for each: the chip's clock gives way, 4096^3 bf16 on N(0,1) 113 us where 16 x 16 take 9x).  K tiles are 128 bytes deep (64 bf16
+// or 32 fp32: whole cache lines of a row, where halves of them cost the L2 as much) and lie in a ring of LDS stages:
 //   an operand whose reduction index is contiguous in memory ([row][k]): 128 bytes per row, 16-byte piece c of row r in slot
 //   c ^ ((r >> 1) & 7); a fragment is one 16-byte read;
 //   one whose row index is contiguous ([k][row]): as it lies in memory, a row of BM or BN elements per k, pieces swizzled by k; a bf16
@@ -19,36 +20,39 @@
 namespace stripe {
 namespace {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kDepthBytes = 128, kSteps = kDepthBytes / 32;    // matrix-instruction steps of a K tile
+constexpr int kDepthBytes = 128;      // two matrix-instruction steps
 
-template <typename T>
-__device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
+// c[j] += b[j] a^T over 64 bytes of k: lane l holds row l & 15 of a and of b[j], 16-byte piece l >> 4; element v of its c[j] is row l & 15 of a's, row
+// 4 (l >> 4) + v of b[j]'s.  (In this order: neighbouring instructions add to different registers, each in place.)
+template <typename T, int C>
+__device__ __forceinline__ void mma_row(u32x4 a, const u32x4 (&b)[C], f32x4 (&c)[C]) {
   if constexpr (sizeof(T) == 2) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-  } else {
-    const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[i], c, 0, 0, 0);
-    return c;
+    for (int j = 0; j < C; ++j) c[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b[j]), __builtin_bit_cast(bf16x8, a), c[j], 0, 0, 0);
+  } else {
+    const f32x4 x = __builtin_bit_cast(f32x4, a);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < C; ++j) c[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(f32x4, b[j])[i], x[i], c[j], 0, 0, 0);
   }
 }
 
-// A wavefront's LDS-direct load: lane i's 16 bytes land at lds_off + 16 i.  Written as assembly because the compiler, which cannot tell a
-// load into one ring stage from fragment reads of another, would wait for all of them before every LDS read; the kernels
-// wait by count.  M0 is written here and nowhere else (no register array is indexed dynamically, nothing else reads M0).
-__device__ __forceinline__ void load_to_lds(const void* src, unsigned lds_off) {
-  const unsigned uniform = __builtin_amdgcn_readfirstlane(lds_off);
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(uniform) : "memory", "m0");
+// A wavefront's LDS-direct load: lane i's 16 bytes from offset `from` of the buffer land at lds_off + 16 i; beyond the buffer: zeros.  Written as
+// assembly because the compiler, which cannot tell a load into one ring stage from fragment reads of another, would wait for all of them
+// before every LDS read; the kernels wait by count.  M0 is written here and nowhere else (no register array is indexed dynamically,
+// nothing else reads M0).
+__device__ __forceinline__ void load_to_lds(u32x4 buffer, unsigned from, unsigned lds_off) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(from), "s"(buffer), "s"(lds_off) : "memory", "m0");
 }
 template <int N>
 __device__ __forceinline__ void wait_loads() {      // until at most N of the wavefront's loads are outstanding
   static_assert(N >= 0 && N < 64, "the counter's range");
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
-__device__ __attribute__((aligned(16))) uint32_t zero_piece[4];
+constexpr uint32_t kOutside = 0x80000000u, kRecords = 0x7fffffffu;      // an offset beyond the buffer, and its size
 
 // One operand's part of a tile: WIDTH rows (or columns) of it.  STRIDED: stored [k][row].
 template <typename T, int WIDTH, bool STRIDED>
@@ -58,10 +62,52 @@ struct Operand {
   static constexpr int STAGE = WIDTH * kDepthBytes, LOADS = STAGE / 4096;      // 16-byte pieces per lane and K tile
   static __device__ __forceinline__ int key(int r) {
     if constexpr (!STRIDED) return (r >> 1) & 7;
-    else if constexpr (sizeof(T) == 4) return 8 * ((r >> 2) & 1);              // the wavefront's halves read k and k + 4
-    else return ROW >= 256 ? 4 * (r & 3) : 4 * ((r >> 1) & 1);                 // a transposing read takes four rows of k
+    else if constexpr (sizeof(T) == 4) return 4 * ((r >> 2) & 3);              // the wavefront's quarters read k, k + 4, k + 8, k + 12
+    else if constexpr (ROW >= 256) return 2 * ((r & 3) | ((r >> 1) & 4));      // half a transposing read takes k = 0 .. 3 and 8 .. 11, 32 bytes of each
+    else return 2 * (((r >> 1) & 1) | ((r >> 2) & 2));
   }
-  // where piece `u` of this lane comes from
+  // Fragment i (rows row0 + 16 i .. + 15) of matrix-instruction step s: lane l holds row l & 15 and the 16 bytes of k with number 4 s + (l >> 4).  The
+  // swizzles only flip address bits that i and s set, so that one register, first(row0), serves all fragments of a wavefront's rows
+  // (row0 a multiple of their number).
+  static __device__ __forceinline__ unsigned first(int row0) {
+    const int lane = threadIdx.x & 63, fr = lane & 15, fq = lane >> 4;
+    if constexpr (!STRIDED) {
+      return (row0 + fr) * ROW + ((fq ^ key(fr)) << 4);
+    } else if constexpr (sizeof(T) == 2) {
+      // within 16 lanes, lane p points at 4 consecutive values of one k; lane i gets, for j = 0 .. 3, value i & 3 of what lane
+      // (i >> 2) + 4 j points at: four k of row i
+      const int kr = 8 * fq + (fr >> 2);
+      return kr * ROW + (((row0 / 8 + ((fr & 3) >> 1)) ^ key(kr)) << 4) + (fr & 1) * 8;
+    } else {
+      return 4 * fq * ROW + ((((row0 + fr) >> 2) ^ key(4 * fq)) << 4) + (fr & 3) * 4;
+    }
+  }
+  static __device__ __forceinline__ u32x4 fragment(const unsigned char* lds, unsigned first, int i, int s) {
+    if constexpr (!STRIDED) {
+      return *(const u32x4*)(lds + (first ^ (s << 6)) + i * 16 * ROW);
+    } else if constexpr (sizeof(T) == 2) {
+      typedef __attribute__((address_space(3))) s16x4* lptr;
+      const unsigned char* at = lds + (first ^ (i << 5)) + 32 * s * ROW;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(at + 4 * ROW));
+      return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      const unsigned char* at = lds + (first ^ (i << 6)) + 16 * s * ROW;
+      u32x4 v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = *(const uint32_t*)(at + j * ROW);
+      return v;
+    }
+  }
+};
+
+// Where the pieces of an operand come from, element by element at its rims: any alignment.
+template <typename T, int WIDTH, bool STRIDED>
+struct Fetch : Operand<T, WIDTH, STRIDED> {
+  using Operand<T, WIDTH, STRIDED>::VEC;
+  using Operand<T, WIDTH, STRIDED>::DEPTH;
+  using Operand<T, WIDTH, STRIDED>::ROW;
+  using Operand<T, WIDTH, STRIDED>::LOADS;
+  using Operand<T, WIDTH, STRIDED>::key;
   const T* src[LOADS];
   int k[LOADS], left[LOADS];      // its first k; elements of it inside the rows' range (strided) -- else a constant
   int64_t step;                   // elements from one K tile to the next
@@ -99,38 +145,41 @@ struct Operand {
 #pragma unroll
     for (int u = 0; u < LOADS; ++u) *(u32x4*)(stage + (u * 4 + wave) * 1024 + lane * 16) = from[u];
   }
-  // Piece u of the next K tile as an LDS-direct load (whole pieces only); n: what is left of the reduction.  What does not exist is fetched
-  // from 16 zero bytes.
-  __device__ __forceinline__ void issue(int u, unsigned stage, int n, const void* zero) {
-    const bool in = k[u] < n && (!STRIDED || left[u] > 0);
-    load_to_lds(in ? (const void*)src[u] : zero, stage + (u * 4 + (threadIdx.x >> 6)) * 1024);
-    src[u] += step;
-  }
-  __device__ __forceinline__ void skip(int kt) {
+};
+
+// The same in whole 16-byte pieces, as LDS-direct loads of consecutive K tiles.  The buffer's base moves from K tile to K tile (scalar additions); a
+// lane's offsets within it stay, 32 bits each (the host has checked that a tile's rows span less than 2^31 bytes).
+template <typename T, int WIDTH, bool STRIDED>
+struct Stream : Operand<T, WIDTH, STRIDED> {
+  using Operand<T, WIDTH, STRIDED>::VEC;
+  using Operand<T, WIDTH, STRIDED>::DEPTH;
+  using Operand<T, WIDTH, STRIDED>::ROW;
+  using Operand<T, WIDTH, STRIDED>::LOADS;
+  using Operand<T, WIDTH, STRIDED>::key;
+  uint64_t base, step;            // of the next K tile, bytes to the one after it
+  uint32_t from[LOADS];
+
+  __device__ __forceinline__ void init(const T* at0, int rows, int64_t ld) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
-    for (int u = 0; u < LOADS; ++u) src[u] += (int64_t)kt * step;
-  }
-  // fragment of rows row0 .. row0 + 31 (row0 a multiple of 32), matrix-instruction step s: lane l holds row l & 31 and the
-  // 16 bytes of k with number 2 s + (l >> 5)
-  static __device__ __forceinline__ u32x4 fragment(const unsigned char* stage, int row0, int s) {
-    const int lane = threadIdx.x & 63, fr = lane & 31, fh = lane >> 5;
-    if constexpr (!STRIDED) {
-      return *(const u32x4*)(stage + (row0 + fr) * ROW + (((2 * s + fh) ^ key(fr)) << 4));
-    } else if constexpr (sizeof(T) == 2) {
-      // within 16 lanes, lane p points at 4 consecutive values of one k; lane i gets, for j = 0 .. 3, value i & 3 of what lane
-      // (i >> 2) + 4 j points at: four k of row i
-      typedef __attribute__((address_space(3))) s16x4* lptr;
-      const int g = lane >> 4, q = lane & 15, kr = 8 * (g >> 1) + (q >> 2), piece = row0 / 8 + 2 * (g & 1) + ((q & 3) >> 1);
-      const unsigned char* at = stage + (16 * s + kr) * ROW + ((piece ^ key(kr)) << 4) + (q & 1) * 8;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(at + 4 * ROW));
-      return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    } else {
-      const unsigned char* at = stage + (8 * s + 4 * fh) * ROW + ((((row0 + fr) >> 2) ^ key(4 * fh)) << 4) + (fr & 3) * 4;
-      u32x4 v;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = *(const uint32_t*)(at + j * ROW);
-      return v;
+    for (int u = 0; u < LOADS; ++u) {
+      const int at = (u * 4 + wave) * 1024 + lane * 16, r = at / ROW, piece = (at % ROW / 16) ^ key(r);
+      const bool in = STRIDED ? piece * VEC < rows : r < rows;
+      from[u] = in ? (uint32_t)(r * (uint32_t)ld + piece * VEC) * (uint32_t)sizeof(T) : kOutside;
     }
+    const uint64_t b = (uint64_t)(uintptr_t)at0;
+    base = (uint64_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)b);
+    step = (STRIDED ? (uint64_t)DEPTH * (uint64_t)ld : (uint64_t)DEPTH) * sizeof(T);
+  }
+  // From here on only `left` (< DEPTH) of a K tile's depth exist: the reduction's last tile, or none of those behind it.
+  __device__ __forceinline__ void cut(int u, int left) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int at = (u * 4 + wave) * 1024 + lane * 16, r = at / ROW, piece = (at % ROW / 16) ^ key(r);
+    if ((STRIDED ? r : piece * VEC) >= left) from[u] = kOutside;
+  }
+  __device__ __forceinline__ void load(int u, unsigned stage) const {
+    const u32x4 buffer = {(uint32_t)base, (uint32_t)(base >> 32), kRecords, 0x00020000u};
+    load_to_lds(buffer, from[u], stage + u * 4096);
   }
 };
 
@@ -244,20 +293,19 @@ __device__ __forceinline__ void finish(const ProductParams& p, int64_t at, int n
   out.store((T*)p.c + at, n, whole);
 }
 
-// Element v of lane l of a fragment is row 8 (v / 4) + 4 (l >> 5) + v % 4, column l & 31.  A wavefront lays 64 of its columns at a time into its
-// quarter of the idle ring (every wavefront is done with it), 256 bytes per row, 16-byte pieces swizzled by the row, and takes them out
-// again eight neighbouring columns per lane, eight rows at a time: 128 contiguous bytes of a bf16 row.  A loop and not 256 copies
+// B's fragments are the matrix instruction's first operand, so that a lane holds four neighbouring columns of a row: 4 (l >> 4) .. + 3 of row l & 15.
+// A wavefront lays 64 of its columns at a time into its quarter of the idle ring (every wavefront is done with it), 256 bytes per row, 16-byte
+// pieces swizzled by the row, and takes them out again eight neighbouring columns per lane, eight rows at a time: 128 contiguous bytes of a bf16 row.  A loop and not 256 copies
 // of the epilogue: the residual's loads of four turns are on their way together, two sets of them.
 template <typename T, int KIND, int FM, int FN>
-__device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t, unsigned char* lds, const f32x16 (&acc)[FM][FN]) {
+__device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t, unsigned char* lds, const f32x4 (&acc)[2 * FM][2 * FN]) {
   static_assert(FN % 2 == 0 && FM * 8192 * 4 <= 2 * 64 * (FM + FN) * kDepthBytes, "a wavefront's rows fit its quarter of two stages");
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
   unsigned char* buf = lds + wave * (FM * 8192);
-  const int fr = lane & 31, fh = lane >> 5, sp = lane >> 3, sc = lane & 7;
+  const int fr = lane & 15, fq = lane >> 4, sp = lane >> 3, sc = lane & 7;
   const int64_t image = KIND == kWeightGrad ? (int64_t)t.group * p.M : 0;
   const int64_t images = KIND == kWeightGrad && p.groups ? (int64_t)p.groups * p.M : p.M;
   const int64_t base = (KIND == kWeightGrad ? t.group * p.c_group : 0) + (int64_t)t.m0 * p.c_ld;
-  auto key = [](int row) { return (row & 1) ^ (((row >> 2) & 1) << 3); };
 #pragma unroll
   for (int jp = 0; jp < FN / 2; ++jp) {
     const int col = t.n0 + (wn * FN + 2 * jp) * 32 + 8 * sc, n = p.N - col;
@@ -281,14 +329,9 @@ __device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t
     Eight<T> now[4], ahead[4];
     load(now, 0);
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+    for (int i = 0; i < 2 * FM; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int row = 8 * (v / 4) + 4 * fh + v % 4;      // + 32 i: the key stays
-          *(float*)(buf + (32 * i + row) * 256 + (((8 * j + (fr >> 2)) ^ key(row)) << 4) + (fr & 3) * 4) = acc[i][2 * jp + j][v];
-        }
+      for (int j = 0; j < 4; ++j) *(f32x4*)(buf + (16 * i + fr) * 256 + (((4 * j + fq) ^ fr) << 4)) = acc[i][4 * jp + j];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
@@ -298,8 +341,8 @@ __device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t
       for (int q = 0; q < 4; ++q) {
         const int local = (turn + q) * 8 + sp, row = wm * FM * 32 + local;
         float v[8];
-        *(f32x4*)v = *(const f32x4*)(buf + local * 256 + (((2 * sc) ^ key(local)) << 4));
-        *(f32x4*)(v + 4) = *(const f32x4*)(buf + local * 256 + (((2 * sc + 1) ^ key(local)) << 4));
+        *(f32x4*)v = *(const f32x4*)(buf + local * 256 + (((2 * sc) ^ (local & 15)) << 4));
+        *(f32x4*)(v + 4) = *(const f32x4*)(buf + local * 256 + (((2 * sc + 1) ^ (local & 15)) << 4));
         if (row < t.m && n > 0) {
           if (p.splits > 1) {
             Eight<float> out;
@@ -318,8 +361,8 @@ __device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t
   }
 }
 
-template <typename T, int KIND, int BM, int BN>
-__device__ __forceinline__ void init_operands(const ProductParams& p, const Tile& t, Operand<T, BM, KIND == kWeightGrad>& a, Operand<T, BN, KIND != kForward>& b) {
+template <typename T, int KIND, typename A, typename B>
+__device__ __forceinline__ void init_operands(const ProductParams& p, const Tile& t, A& a, B& b) {
   if constexpr (KIND == kWeightGrad) {
     a.init((const T*)p.a + (int64_t)t.k0 * p.a_ld + t.m0, t.m, p.a_ld);
     b.init((const T*)p.b + (int64_t)t.k0 * p.b_ld + t.n0, p.N - t.n0, p.b_ld);
@@ -343,9 +386,9 @@ __device__ __forceinline__ void own_k_tiles(const ProductParams& p, int all, int
 // Operands at any alignment: through registers, two stages of the ring, one K tile ahead.
 template <typename T, int KIND, int FM, int FN>
 __global__ __launch_bounds__(256) void product_kernel(const ProductParams p) {
-  constexpr int BM = 64 * FM, BN = 64 * FN;
-  using A = Operand<T, BM, KIND == kWeightGrad>;
-  using B = Operand<T, BN, KIND != kForward>;
+  constexpr int BM = 64 * FM, BN = 64 * FN, R = 2 * FM, C = 2 * FN;      // fragments of a wavefront
+  using A = Fetch<T, BM, KIND == kWeightGrad>;
+  using B = Fetch<T, BN, KIND != kForward>;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   unsigned char *const lds_a = lds, *const lds_b = lds + 2 * A::STAGE;
   Tile t;
@@ -354,18 +397,17 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductParams p) {
 
   A a;
   B b;
-  init_operands<T, KIND, BM, BN>(p, t, a, b);
+  init_operands<T, KIND>(p, t, a, b);
   int kt0, kt1;
   own_k_tiles(p, (t.k + A::DEPTH - 1) / A::DEPTH, &kt0, &kt1);
 
-  f32x16 acc[FM][FN];
+  f32x4 acc[R][C];
 #pragma unroll
-  for (int i = 0; i < FM; ++i)
+  for (int i = 0; i < R; ++i)
 #pragma unroll
-    for (int j = 0; j < FN; ++j)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+    for (int j = 0; j < C; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
 
+  const unsigned first_a = A::first(wm * R * 16), first_b = B::first(wn * C * 16);
   u32x4 ra[A::LOADS], rb[B::LOADS];
   a.fetch(ra, kt0, t.k);
   b.fetch(rb, kt0, t.k);
@@ -377,36 +419,36 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductParams p) {
     a.fetch(ra, kt + 1, t.k);
     b.fetch(rb, kt + 1, t.k);
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      u32x4 fa[FM], fb[FN];
+    for (int s = 0; s < 2; ++s) {
+      u32x4 fa[R], fb[C];
 #pragma unroll
-      for (int i = 0; i < FM; ++i) fa[i] = A::fragment(lds_a + stage * A::STAGE, (wm * FM + i) * 32, s);
+      for (int i = 0; i < R; ++i) fa[i] = A::fragment(lds_a + stage * A::STAGE, first_a, i, s);
 #pragma unroll
-      for (int j = 0; j < FN; ++j) fb[j] = B::fragment(lds_b + stage * B::STAGE, (wn * FN + j) * 32, s);
+      for (int j = 0; j < C; ++j) fb[j] = B::fragment(lds_b + stage * B::STAGE, first_b, j, s);
 #pragma unroll
-      for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = mma<T>(fa[i], fb[j], acc[i][j]);
+      for (int i = 0; i < R; ++i) mma_row<T, C>(fa[i], fb, acc[i]);
     }
   }
 
   store_tile<T, KIND, FM, FN>(p, t, lds, acc);
 }
 
-// Operands in whole 16-byte pieces: LDS-direct loads, one barrier for each K tile, before its last step:
-//   steps 0 .. 2 of tile kt   + fragment reads one step ahead;  in step 0 the second half of a tile's loads,
-//   wait, barrier             tile kt + 1 is complete in LDS, and everybody has read the whole of tile kt,
-//   step 3 of tile kt         + fragment reads of tile kt + 1's step 0 + the first half of tile kt + S's loads, into tile kt's stage,
-// S the stages of the ring (step 0: tile kt + S - 1's second half).
+// Operands in whole 16-byte pieces: LDS-direct loads into a ring of S stages, one barrier for each K tile.  A K tile is two matrix-instruction steps of R
+// fragment rows each, and beside the rows' matrix instructions go
+//   rows 0 .. R - 1             the fragment reads of step 1,
+//   rows 0 .. R/2 - 1           the second half of tile kt + S - 1's loads,
+//   behind row R + R/2 - 1      wait, barrier: tile kt + 1 is complete in LDS, and everybody has read the whole of tile kt,
+//   rows R + R/2 .. 2 R - 1     the fragment reads of tile kt + 1's step 0, and the first half of tile kt + S's loads, into tile kt's stage.
+// (All of a tile's loads behind the barrier: 4096^3 on zeros 94 us instead of 87; over three quarters of a tile: 90.)
 // Behind the last tile the loop loads zeros and reads fragments that nobody uses: the counts then never change.
 #define PRODUCT_FENCE() __builtin_amdgcn_sched_barrier(0)
 
 template <typename T, int KIND, int FM, int FN, int S>
 __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void product_stream_kernel(const ProductParams p) {
-  constexpr int BM = 64 * FM, BN = 64 * FN;
-  using A = Operand<T, BM, KIND == kWeightGrad>;
-  using B = Operand<T, BN, KIND != kForward>;
-  constexpr int LOADS = A::LOADS + B::LOADS, READS = FM + FN;
+  constexpr int BM = 64 * FM, BN = 64 * FN, R = 2 * FM, C = 2 * FN;      // fragments of a wavefront
+  using A = Stream<T, BM, KIND == kWeightGrad>;
+  using B = Stream<T, BN, KIND != kForward>;
+  constexpr int LOADS = A::LOADS + B::LOADS, READS = R + C, HALF = R / 2;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   unsigned char *const lds_a = lds, *const lds_b = lds + S * A::STAGE;
   Tile t;
@@ -414,82 +456,99 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void product_stream_ker
   const int wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
   A a;
   B b;
-  init_operands<T, KIND, BM, BN>(p, t, a, b);
+  init_operands<T, KIND>(p, t, a, b);
   int kt0, kt1;
   own_k_tiles(p, (t.k + A::DEPTH - 1) / A::DEPTH, &kt0, &kt1);
 
-  f32x16 acc[FM][FN];
+  f32x4 acc[R][C];
 #pragma unroll
-  for (int i = 0; i < FM; ++i)
+  for (int i = 0; i < R; ++i)
 #pragma unroll
-    for (int j = 0; j < FN; ++j)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+    for (int j = 0; j < C; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
 
   if (kt0 < kt1) {
-    const void* zero = zero_piece;
-    asm volatile("" : "+s"(zero));       // held in registers
-    int left = (kt1 * A::DEPTH < t.k ? kt1 * A::DEPTH : t.k) - kt0 * A::DEPTH;      // of this workgroup's part of the reduction
-    a.skip(kt0);
-    b.skip(kt0);
+    int left = (kt1 * A::DEPTH < t.k ? kt1 * A::DEPTH : t.k) - kt0 * A::DEPTH;      // of this workgroup's part of the reduction, from the next tile on
+    a.base += (uint64_t)kt0 * a.step;
+    b.base += (uint64_t)kt0 * b.step;
+    const unsigned own = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) * 1024;
     auto load = [&](int first, int last, int stage) {
 #pragma unroll
       for (int u = 0; u < LOADS; ++u)
         if (u >= first && u < last) {
-          if (u < A::LOADS) a.issue(u, stage * A::STAGE, left, zero);
-          else b.issue(u - A::LOADS, S * A::STAGE + stage * B::STAGE, left, zero);
+          if (u < A::LOADS) a.load(u, own + stage * A::STAGE);
+          else b.load(u - A::LOADS, own + S * A::STAGE + stage * B::STAGE);
         }
+    };
+    // pieces first .. last - 1 of a tile are about to be loaded, `depth` of whose k exist (the last one, or none behind it)
+    auto cut = [&](int first, int last, int depth) {
+      if (depth >= A::DEPTH) return;
+#pragma unroll
+      for (int u = 0; u < LOADS; ++u)
+        if (u >= first && u < last) {
+          if (u < A::LOADS) a.cut(u, depth);
+          else b.cut(u - A::LOADS, depth);
+        }
+    };
+    auto next = [&] {
+      left -= A::DEPTH;
+      a.base += a.step;
+      b.base += b.step;
     };
 #pragma unroll
     for (int i = 0; i < S - 1; ++i) {
+      cut(0, LOADS, left);
       load(0, LOADS, i);
-      left -= A::DEPTH;
+      next();
     }
+    cut(0, LOADS / 2, left);
     load(0, LOADS / 2, S - 1);
     wait_loads<LOADS / 2 + (S - 2) * LOADS>();
     asm volatile("s_barrier" ::: "memory");
-    u32x4 fa[2][FM], fb[2][FN];
+    const unsigned first_a = A::first(wm * R * 16), first_b = B::first(wn * C * 16);
+    u32x4 fa[2][R], fb[2][C];
 #pragma unroll
-    for (int j = 0; j < FN; ++j) fb[0][j] = B::fragment(lds_b, (wn * FN + j) * 32, 0);
+    for (int j = 0; j < C; ++j) fb[0][j] = B::fragment(lds_b, first_b, j, 0);
 #pragma unroll
-    for (int i = 0; i < FM; ++i) fa[0][i] = A::fragment(lds_a, (wm * FM + i) * 32, 0);
+    for (int i = 0; i < R; ++i) fa[0][i] = A::fragment(lds_a, first_a, i, 0);
 
     const int tiles = kt1 - kt0;
     int cur = 0, before = S - 1;      // stages of tile kt and of tile kt - 1
     for (int kt = 0; kt < tiles; ++kt) {
       const int nxt = cur + 1 == S ? 0 : cur + 1;
-      // fragment reads of one step, spread over its predecessor's rows of matrix instructions: B's and A's first before the others, none
-      // beside the last row, so that neither the barrier nor the next step meets a read that has only just begun
-      auto read = [&](int to, int stage, int st, int row) {
-        constexpr int GROUPS = FM > 1 ? FM - 1 : 1;
+      if (left < 2 * A::DEPTH) {      // (here and not beside the loads: the rest of the loop is one block)
+        cut(LOADS / 2, LOADS, left);
+        cut(0, LOADS / 2, left - A::DEPTH);
+      }
+      unsigned cur_a = first_a + cur * A::STAGE, cur_b = first_b + cur * B::STAGE, nxt_a = first_a + nxt * A::STAGE, nxt_b = first_b + nxt * B::STAGE;
+      // (opaque: else every fragment's address would be kept in a register of its own over the whole loop)
+      asm volatile("" : "+v"(cur_a), "+v"(cur_b), "+v"(nxt_a), "+v"(nxt_b));
+      // reads number first .. last - 1 of a step's fragments: all of B's, of which its first row needs every one, then A's
+      auto read = [&](int st, unsigned at_a, unsigned at_b, int first, int last) {
 #pragma unroll
         for (int r = 0; r < READS; ++r)
-          if (r * GROUPS / READS == row) {
-            if (r < FN) fb[to][r] = B::fragment(lds_b + stage * B::STAGE, (wn * FN + r) * 32, st);
-            else fa[to][r - FN] = A::fragment(lds_a + stage * A::STAGE, (wm * FM + r - FN) * 32, st);
+          if (r >= first && r < last) {
+            if (r < C) fb[st][r] = B::fragment(lds_b, at_b, r, st);
+            else fa[st][r - C] = A::fragment(lds_a, at_a, r - C, st);
           }
       };
 #pragma unroll
-      for (int st = 0; st < kSteps; ++st) {
-        const int from = st & 1;
-        if (st == kSteps - 1) {
+      for (int row = 0; row < 2 * R; ++row) {
+        const int st = row / R, i = row % R;
+        if (row == R + HALF) {
           asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((S - 2) * LOADS) : "memory");
           asm volatile("s_barrier" ::: "memory");
           PRODUCT_FENCE();
         }
-#pragma unroll
-        for (int i = 0; i < FM; ++i) {
-#pragma unroll
-          for (int j = 0; j < FN; ++j) {
-            const int jj = (i & 1) ? FN - 1 - j : j;      // one operand stays in place between two instructions
-            acc[i][jj] = mma<T>(fa[from][i], fb[from][jj], acc[i][jj]);
-          }
-          read(from ^ 1, st == kSteps - 1 ? nxt : cur, (st + 1) % kSteps, i);
-          if (st == 0) load(LOADS / 2 + i * (LOADS / 2) / FM, LOADS / 2 + (i + 1) * (LOADS / 2) / FM, before);
-          if (st == kSteps - 1) load(i * (LOADS / 2) / FM, (i + 1) * (LOADS / 2) / FM, cur);
-          PRODUCT_FENCE();
+        mma_row<T, C>(fa[st][i], fb[st], acc[i]);
+        if (row < R) read(1, cur_a, cur_b, row * READS / R, (row + 1) * READS / R);
+        if (row < HALF) load(LOADS / 2 + row * (LOADS / 2) / HALF, LOADS / 2 + (row + 1) * (LOADS / 2) / HALF, before);
+        if (row >= R + HALF) {
+          const int at = row - R - HALF;
+          read(0, nxt_a, nxt_b, at * READS / HALF, (at + 1) * READS / HALF);
+          load(at * (LOADS / 2) / HALF, (at + 1) * (LOADS / 2) / HALF, cur);
         }
-        if (st == 0) left -= A::DEPTH;
+        PRODUCT_FENCE();
+        if (row == HALF - 1) next();
       }
       before = cur;
       cur = nxt;
