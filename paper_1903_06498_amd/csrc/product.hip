@@ -55,11 +55,11 @@ __device__ __forceinline__ void wait_loads() {      // until at most N of the wa
 constexpr uint32_t kOutside = 0x80000000u, kRecords = 0x7fffffffu;      // an offset beyond the buffer, and its size
 
 // One operand's part of a tile: WIDTH rows (or columns) of it.  STRIDED: stored [k][row].
-template <typename T, int WIDTH, bool STRIDED>
+template <typename T, int WIDTH, bool STRIDED, int WAVES = 4>
 struct Operand {
   static constexpr int VEC = kVec<T>, DEPTH = kDepthBytes / (int)sizeof(T);
   static constexpr int ROW = STRIDED ? WIDTH * (int)sizeof(T) : kDepthBytes;   // bytes of an LDS row
-  static constexpr int STAGE = WIDTH * kDepthBytes, LOADS = STAGE / 4096;      // 16-byte pieces per lane and K tile
+  static constexpr int STAGE = WIDTH * kDepthBytes, LOADS = STAGE / (1024 * WAVES);   // 16-byte pieces per lane and K tile
   static __device__ __forceinline__ int key(int r) {
     if constexpr (!STRIDED) return (r >> 1) & 7;
     else if constexpr (sizeof(T) == 4) return 4 * ((r >> 2) & 3);              // the wavefront's quarters read k, k + 4, k + 8, k + 12
@@ -149,13 +149,13 @@ struct Fetch : Operand<T, WIDTH, STRIDED> {
 
 // The same in whole 16-byte pieces, as LDS-direct loads of consecutive K tiles.  The buffer's base moves from K tile to K tile (scalar additions); a
 // lane's offsets within it stay, 32 bits each (the host has checked that a tile's rows span less than 2^31 bytes).
-template <typename T, int WIDTH, bool STRIDED>
-struct Stream : Operand<T, WIDTH, STRIDED> {
-  using Operand<T, WIDTH, STRIDED>::VEC;
-  using Operand<T, WIDTH, STRIDED>::DEPTH;
-  using Operand<T, WIDTH, STRIDED>::ROW;
-  using Operand<T, WIDTH, STRIDED>::LOADS;
-  using Operand<T, WIDTH, STRIDED>::key;
+template <typename T, int WIDTH, bool STRIDED, int WAVES>
+struct Stream : Operand<T, WIDTH, STRIDED, WAVES> {
+  using Operand<T, WIDTH, STRIDED, WAVES>::VEC;
+  using Operand<T, WIDTH, STRIDED, WAVES>::DEPTH;
+  using Operand<T, WIDTH, STRIDED, WAVES>::ROW;
+  using Operand<T, WIDTH, STRIDED, WAVES>::LOADS;
+  using Operand<T, WIDTH, STRIDED, WAVES>::key;
   uint64_t base, step;            // of the next K tile, bytes to the one after it
   uint32_t from[LOADS];
 
@@ -163,7 +163,7 @@ struct Stream : Operand<T, WIDTH, STRIDED> {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int u = 0; u < LOADS; ++u) {
-      const int at = (u * 4 + wave) * 1024 + lane * 16, r = at / ROW, piece = (at % ROW / 16) ^ key(r);
+      const int at = (u * WAVES + wave) * 1024 + lane * 16, r = at / ROW, piece = (at % ROW / 16) ^ key(r);
       const bool in = STRIDED ? piece * VEC < rows : r < rows;
       from[u] = in ? (uint32_t)(r * (uint32_t)ld + piece * VEC) * (uint32_t)sizeof(T) : kOutside;
     }
@@ -174,12 +174,12 @@ struct Stream : Operand<T, WIDTH, STRIDED> {
   // From here on only `left` (< DEPTH) of a K tile's depth exist: the reduction's last tile, or none of those behind it.
   __device__ __forceinline__ void cut(int u, int left) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int at = (u * 4 + wave) * 1024 + lane * 16, r = at / ROW, piece = (at % ROW / 16) ^ key(r);
+    const int at = (u * WAVES + wave) * 1024 + lane * 16, r = at / ROW, piece = (at % ROW / 16) ^ key(r);
     if ((STRIDED ? r : piece * VEC) >= left) from[u] = kOutside;
   }
   __device__ __forceinline__ void load(int u, unsigned stage) const {
     const u32x4 buffer = {(uint32_t)base, (uint32_t)(base >> 32), kRecords, 0x00020000u};
-    load_to_lds(buffer, from[u], stage + u * 4096);
+    load_to_lds(buffer, from[u], stage + u * (1024 * WAVES));
   }
 };
 
@@ -297,18 +297,19 @@ __device__ __forceinline__ void finish(const ProductParams& p, int64_t at, int n
 // A wavefront lays 64 of its columns at a time into its quarter of the idle ring (every wavefront is done with it), 256 bytes per row, 16-byte
 // pieces swizzled by the row, and takes them out again eight neighbouring columns per lane, eight rows at a time: 128 contiguous bytes of a bf16 row.  A loop and not 256 copies
 // of the epilogue: the residual's loads of four turns are on their way together, two sets of them.
-template <typename T, int KIND, int FM, int FN>
-__device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t, unsigned char* lds, const f32x4 (&acc)[2 * FM][2 * FN]) {
-  static_assert(FN % 2 == 0 && FM * 8192 * 4 <= 2 * 64 * (FM + FN) * kDepthBytes, "a wavefront's rows fit its quarter of two stages");
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
-  unsigned char* buf = lds + wave * (FM * 8192);
+template <typename T, int KIND, int FM, int C, int WAVES>
+__device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t, unsigned char* lds, const f32x4 (&acc)[2 * FM][C]) {
+  constexpr int PARTS = WAVES / 4, ROWS = FM * 32 / PARTS;      // a wavefront's rows at a time
+  static_assert(C % 4 == 0 && ROWS % 32 == 0, "64 columns, four turns of eight rows");
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / (WAVES / 2), wn = wave % (WAVES / 2);
+  unsigned char* buf = lds + wave * (ROWS * 256);
   const int fr = lane & 15, fq = lane >> 4, sp = lane >> 3, sc = lane & 7;
   const int64_t image = KIND == kWeightGrad ? (int64_t)t.group * p.M : 0;
   const int64_t images = KIND == kWeightGrad && p.groups ? (int64_t)p.groups * p.M : p.M;
   const int64_t base = (KIND == kWeightGrad ? t.group * p.c_group : 0) + (int64_t)t.m0 * p.c_ld;
 #pragma unroll
-  for (int jp = 0; jp < FN / 2; ++jp) {
-    const int col = t.n0 + (wn * FN + 2 * jp) * 32 + 8 * sc, n = p.N - col;
+  for (int jp = 0; jp < C / 4; ++jp) {
+    const int col = t.n0 + (wn * C + 4 * jp) * 16 + 8 * sc, n = p.N - col;
     float bias[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) bias[e] = 0.f;
@@ -319,27 +320,29 @@ __device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t
         for (int e = 0; e < 8; ++e)
           if (e < n) bias[e] = p.bias[(int64_t)t.group * p.N + col + e];
       }
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) {
     auto load = [&](Eight<T> (&r)[4], int turn) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int row = wm * FM * 32 + (turn + q) * 8 + sp;
+        const int row = wm * FM * 32 + part * ROWS + (turn + q) * 8 + sp;
         if (residual && row < t.m && n > 0) r[q].load((const T*)p.residual + base + (int64_t)row * p.c_ld + col, n, p.vec && n >= 8);
       }
     };
     Eight<T> now[4], ahead[4];
     load(now, 0);
 #pragma unroll
-    for (int i = 0; i < 2 * FM; ++i)
+    for (int i = 0; i < ROWS / 16; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) *(f32x4*)(buf + (16 * i + fr) * 256 + (((4 * j + fq) ^ fr) << 4)) = acc[i][4 * jp + j];
+      for (int j = 0; j < 4; ++j) *(f32x4*)(buf + (16 * i + fr) * 256 + (((4 * j + fq) ^ fr) << 4)) = acc[part * (ROWS / 16) + i][4 * jp + j];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-    for (int turn = 0; turn < FM * 4; turn += 4) {
-      if (turn + 4 < FM * 4) load(ahead, turn + 4);
+    for (int turn = 0; turn < ROWS / 8; turn += 4) {
+      if (turn + 4 < ROWS / 8) load(ahead, turn + 4);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int local = (turn + q) * 8 + sp, row = wm * FM * 32 + local;
+        const int local = (turn + q) * 8 + sp, row = wm * FM * 32 + part * ROWS + local;
         float v[8];
         *(f32x4*)v = *(const f32x4*)(buf + local * 256 + (((2 * sc) ^ (local & 15)) << 4));
         *(f32x4*)(v + 4) = *(const f32x4*)(buf + local * 256 + (((2 * sc + 1) ^ (local & 15)) << 4));
@@ -358,6 +361,7 @@ __device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
+    }
   }
 }
 
@@ -430,7 +434,7 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductParams p) {
     }
   }
 
-  store_tile<T, KIND, FM, FN>(p, t, lds, acc);
+  store_tile<T, KIND, FM, C, 4>(p, t, lds, acc);
 }
 
 // Operands in whole 16-byte pieces: LDS-direct loads into a ring of S stages, one barrier for each K tile.  A K tile is two matrix-instruction steps of R
@@ -443,17 +447,17 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductParams p) {
 // Behind the last tile the loop loads zeros and reads fragments that nobody uses: the counts then never change.
 #define PRODUCT_FENCE() __builtin_amdgcn_sched_barrier(0)
 
-template <typename T, int KIND, int FM, int FN, int S>
-__global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void product_stream_kernel(const ProductParams p) {
-  constexpr int BM = 64 * FM, BN = 64 * FN, R = 2 * FM, C = 2 * FN;      // fragments of a wavefront
-  using A = Stream<T, BM, KIND == kWeightGrad>;
-  using B = Stream<T, BN, KIND != kForward>;
-  constexpr int LOADS = A::LOADS + B::LOADS, READS = R + C, HALF = R / 2;
+template <typename T, int KIND, int FM, int FN, int S, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, FM * FN >= 16 ? 1 : 2) void product_stream_kernel(const ProductParams p) {
+  constexpr int BM = 64 * FM, BN = 64 * FN, R = 2 * FM, C = 8 * FN / WAVES;      // fragments of a wavefront
+  using A = Stream<T, BM, KIND == kWeightGrad, WAVES>;
+  using B = Stream<T, BN, KIND != kForward, WAVES>;
+  constexpr int LOADS = A::LOADS + B::LOADS, HALF = R / 2;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   unsigned char *const lds_a = lds, *const lds_b = lds + S * A::STAGE;
   Tile t;
   if (!place<KIND, BM, BN>(p, &t)) return;
-  const int wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
+  const int wave = threadIdx.x >> 6, wm = wave / (WAVES / 2), wn = wave % (WAVES / 2);
   A a;
   B b;
   init_operands<T, KIND>(p, t, a, b);
@@ -505,11 +509,11 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void product_stream_ker
     wait_loads<LOADS / 2 + (S - 2) * LOADS>();
     asm volatile("s_barrier" ::: "memory");
     const unsigned first_a = A::first(wm * R * 16), first_b = B::first(wn * C * 16);
-    u32x4 fa[2][R], fb[2][C];
+    u32x4 fa[R], fb[2][C];
 #pragma unroll
     for (int j = 0; j < C; ++j) fb[0][j] = B::fragment(lds_b, first_b, j, 0);
 #pragma unroll
-    for (int i = 0; i < R; ++i) fa[0][i] = A::fragment(lds_a, first_a, i, 0);
+    for (int i = 0; i < R; ++i) fa[i] = A::fragment(lds_a, first_a, i, 0);
 
     const int tiles = kt1 - kt0;
     int cur = 0, before = S - 1;      // stages of tile kt and of tile kt - 1
@@ -522,14 +526,15 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void product_stream_ker
       unsigned cur_a = first_a + cur * A::STAGE, cur_b = first_b + cur * B::STAGE, nxt_a = first_a + nxt * A::STAGE, nxt_b = first_b + nxt * B::STAGE;
       // (opaque: else every fragment's address would be kept in a register of its own over the whole loop)
       asm volatile("" : "+v"(cur_a), "+v"(cur_b), "+v"(nxt_a), "+v"(nxt_b));
-      // reads number first .. last - 1 of a step's fragments: all of B's, of which its first row needs every one, then A's
-      auto read = [&](int st, unsigned at_a, unsigned at_b, int first, int last) {
+      auto read_b = [&](int st, unsigned at, int first, int last) {
 #pragma unroll
-        for (int r = 0; r < READS; ++r)
-          if (r >= first && r < last) {
-            if (r < C) fb[st][r] = B::fragment(lds_b, at_b, r, st);
-            else fa[st][r - C] = A::fragment(lds_a, at_a, r - C, st);
-          }
+        for (int j = 0; j < C; ++j)
+          if (j >= first && j < last) fb[st][j] = B::fragment(lds_b, at, j, st);
+      };
+      auto read_a = [&](int st, unsigned at, int first, int last) {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+          if (i >= first && i < last) fa[i] = A::fragment(lds_a, at, i, st);
       };
 #pragma unroll
       for (int row = 0; row < 2 * R; ++row) {
@@ -539,12 +544,18 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void product_stream_ker
           asm volatile("s_barrier" ::: "memory");
           PRODUCT_FENCE();
         }
-        mma_row<T, C>(fa[st][i], fb[st], acc[i]);
-        if (row < R) read(1, cur_a, cur_b, row * READS / R, (row + 1) * READS / R);
+        mma_row<T, C>(fa[i], fb[st], acc[i]);
+        if (row < R) {
+          read_a(1, cur_a, row, row + 1);
+          read_b(1, cur_b, row * C / R, (row + 1) * C / R);
+        }
         if (row < HALF) load(LOADS / 2 + row * (LOADS / 2) / HALF, LOADS / 2 + (row + 1) * (LOADS / 2) / HALF, before);
         if (row >= R + HALF) {
-          const int at = row - R - HALF;
-          read(0, nxt_a, nxt_b, at * READS / HALF, (at + 1) * READS / HALF);
+          // B's fragments and A's first ones, which were used before the barrier, in the first half of these rows; the others behind their use
+          const int at = row - R - HALF, early = HALF > 1 ? HALF / 2 : 1;
+          if (at < early) read_b(0, nxt_b, at * C / early, (at + 1) * C / early);
+          if (at < early) read_a(0, nxt_a, at * HALF / early, (at + 1) * HALF / early);
+          read_a(0, nxt_a, HALF + at, HALF + at + 1);
           load(at * (LOADS / 2) / HALF, (at + 1) * (LOADS / 2) / HALF, cur);
         }
         PRODUCT_FENCE();
@@ -556,7 +567,7 @@ __global__ __launch_bounds__(256, FM * FN >= 16 ? 1 : 2) void product_stream_ker
     wait_loads<0>();
   }
   __syncthreads();
-  store_tile<T, KIND, FM, FN>(p, t, lds, acc);
+  store_tile<T, KIND, FM, C, WAVES>(p, t, lds, acc);
 }
 
 // The slices of a split reduction, added in their order, and the epilogue: one row (blockIdx.x / strips), 2048 columns.
@@ -672,10 +683,10 @@ __global__ __launch_bounds__(256) void db_kernel(const DzParams p, int strips) {
 
 // ---- host ---------------------------------------------------------------------
 struct TileShape {
-  int fm, fn, stages, resident;      // resident: workgroups that fit a CU
+  int fm, fn, stages, resident, waves;      // resident: workgroups that fit a CU
 };
 // 3: the tile that fills the chip with few rows; 2: one workgroup for a CU, whose ring then holds three K tiles ahead
-constexpr TileShape kTiles[] = {{2, 2, 2, 2}, {4, 4, 2, 1}, {2, 2, 4, 1}, {1, 2, 3, 2}};
+constexpr TileShape kTiles[] = {{2, 2, 2, 2, 4}, {4, 4, 2, 1, 8}, {2, 2, 4, 1, 4}, {1, 2, 3, 2, 4}};
 constexpr int kTileCount = sizeof kTiles / sizeof *kTiles;
 
 // A kernel's LDS beyond 64 KB has to be allowed once on each device.
@@ -696,9 +707,9 @@ hipError_t launch_stream(const ProductParams& p, dim3 grid, hipStream_t stream) 
   constexpr int bytes = s.stages * 64 * (s.fm + s.fn) * kDepthBytes;
   if constexpr (bytes > 65536) {
     static std::atomic<uint64_t> done{0};
-    if (const hipError_t e = allow_lds(product_stream_kernel<T, KIND, s.fm, s.fn, s.stages>, bytes, done); e != hipSuccess) return e;
+    if (const hipError_t e = allow_lds(product_stream_kernel<T, KIND, s.fm, s.fn, s.stages, s.waves>, bytes, done); e != hipSuccess) return e;
   }
-  product_stream_kernel<T, KIND, s.fm, s.fn, s.stages><<<grid, dim3(256), bytes, stream>>>(p);
+  product_stream_kernel<T, KIND, s.fm, s.fn, s.stages, s.waves><<<grid, dim3(64 * s.waves), bytes, stream>>>(p);
   return hipGetLastError();
 }
 
