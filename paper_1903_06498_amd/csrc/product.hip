@@ -294,9 +294,9 @@ __device__ __forceinline__ void finish(const ProductParams& p, int64_t at, int n
 }
 
 // B's fragments are the matrix instruction's first operand, so that a lane holds four neighbouring columns of a row: 4 (l >> 4) .. + 3 of row l & 15.
-// A wavefront lays 64 of its columns at a time into its quarter of the idle ring (every wavefront is done with it), 256 bytes per row, 16-byte
-// pieces swizzled by the row, and takes them out again eight neighbouring columns per lane, eight rows at a time: 128 contiguous bytes of a bf16 row.  A loop and not 256 copies
-// of the epilogue: the residual's loads of four turns are on their way together, two sets of them.
+// A wavefront lays 64 of its columns at a time into a part of the idle ring, 256 bytes per row, 16-byte pieces swizzled by the row, and
+// takes them out again eight neighbouring columns per lane, eight rows at a time: 128 contiguous bytes of a bf16 row.  A loop and not
+// 256 copies of the epilogue: the residual's loads of four turns are on their way together, two sets of them.
 template <typename T, int KIND, int FM, int C, int WAVES>
 __device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t, unsigned char* lds, const f32x4 (&acc)[2 * FM][C]) {
   constexpr int PARTS = WAVES / 4, ROWS = FM * 32 / PARTS;      // a wavefront's rows at a time
@@ -320,47 +320,49 @@ __device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t
         for (int e = 0; e < 8; ++e)
           if (e < n) bias[e] = p.bias[(int64_t)t.group * p.N + col + e];
       }
-#pragma unroll
-    for (int part = 0; part < PARTS; ++part) {
-    auto load = [&](Eight<T> (&r)[4], int turn) {
+    auto load = [&](Eight<T> (&r)[4], int first) {      // the residual of four turns of eight rows, from the wavefront's row `first` on
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int row = wm * FM * 32 + part * ROWS + (turn + q) * 8 + sp;
+        const int row = wm * FM * 32 + first + q * 8 + sp;
         if (residual && row < t.m && n > 0) r[q].load((const T*)p.residual + base + (int64_t)row * p.c_ld + col, n, p.vec && n >= 8);
       }
     };
     Eight<T> now[4], ahead[4];
     load(now, 0);
+    if (jp == 0) __syncthreads();      // every wavefront is done with the ring
 #pragma unroll
-    for (int i = 0; i < ROWS / 16; ++i)
+    for (int part = 0; part < PARTS; ++part) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) *(f32x4*)(buf + (16 * i + fr) * 256 + (((4 * j + fq) ^ fr) << 4)) = acc[part * (ROWS / 16) + i][4 * jp + j];
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+      for (int i = 0; i < ROWS / 16; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) *(f32x4*)(buf + (16 * i + fr) * 256 + (((4 * j + fq) ^ fr) << 4)) = acc[part * (ROWS / 16) + i][4 * jp + j];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-    for (int turn = 0; turn < ROWS / 8; turn += 4) {
-      if (turn + 4 < ROWS / 8) load(ahead, turn + 4);
+      for (int turn = 0; turn < ROWS / 8; turn += 4) {
+        const int first = part * ROWS + turn * 8;
+        if (first + 32 < FM * 32) load(ahead, first + 32);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int local = (turn + q) * 8 + sp, row = wm * FM * 32 + part * ROWS + local;
-        float v[8];
-        *(f32x4*)v = *(const f32x4*)(buf + local * 256 + (((2 * sc) ^ (local & 15)) << 4));
-        *(f32x4*)(v + 4) = *(const f32x4*)(buf + local * 256 + (((2 * sc + 1) ^ (local & 15)) << 4));
-        if (row < t.m && n > 0) {
-          if (p.splits > 1) {
-            Eight<float> out;
-            out.set(v);
-            out.store(p.partial + ((int64_t)blockIdx.y * images + image + t.m0 + row) * p.N + col, n, false);
-          } else {
-            finish<T, KIND>(p, base + (int64_t)row * p.c_ld + col, n, v, bias, now[q]);
+        for (int q = 0; q < 4; ++q) {
+          const int local = (turn + q) * 8 + sp, row = wm * FM * 32 + part * ROWS + local;
+          float v[8];
+          *(f32x4*)v = *(const f32x4*)(buf + local * 256 + (((2 * sc) ^ (local & 15)) << 4));
+          *(f32x4*)(v + 4) = *(const f32x4*)(buf + local * 256 + (((2 * sc + 1) ^ (local & 15)) << 4));
+          if (row < t.m && n > 0) {
+            if (p.splits > 1) {
+              Eight<float> out;
+              out.set(v);
+              out.store(p.partial + ((int64_t)blockIdx.y * images + image + t.m0 + row) * p.N + col, n, false);
+            } else {
+              finish<T, KIND>(p, base + (int64_t)row * p.c_ld + col, n, v, bias, now[q]);
+            }
           }
         }
-      }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) now[q] = ahead[q];
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+        for (int q = 0; q < 4; ++q) now[q] = ahead[q];
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
     }
   }
 }
@@ -448,7 +450,7 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductParams p) {
 #define PRODUCT_FENCE() __builtin_amdgcn_sched_barrier(0)
 
 template <typename T, int KIND, int FM, int FN, int S, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, FM * FN >= 16 ? 1 : 2) void product_stream_kernel(const ProductParams p) {
+__global__ __launch_bounds__(64 * WAVES, S * 64 * (FM + FN) * kDepthBytes > 80 * 1024 ? 1 : 2) void product_stream_kernel(const ProductParams p) {
   constexpr int BM = 64 * FM, BN = 64 * FN, R = 2 * FM, C = 8 * FN / WAVES;      // fragments of a wavefront
   using A = Stream<T, BM, KIND == kWeightGrad, WAVES>;
   using B = Stream<T, BN, KIND != kForward, WAVES>;
@@ -566,7 +568,6 @@ __global__ __launch_bounds__(64 * WAVES, FM * FN >= 16 ? 1 : 2) void product_str
     }
     wait_loads<0>();
   }
-  __syncthreads();
   store_tile<T, KIND, FM, C, WAVES>(p, t, lds, acc);
 }
 
@@ -685,9 +686,23 @@ __global__ __launch_bounds__(256) void db_kernel(const DzParams p, int strips) {
 struct TileShape {
   int fm, fn, stages, resident, waves;      // resident: workgroups that fit a CU
 };
-// 3: the tile that fills the chip with few rows; 2: one workgroup for a CU, whose ring then holds three K tiles ahead
-constexpr TileShape kTiles[] = {{2, 2, 2, 2, 4}, {4, 4, 2, 1, 8}, {2, 2, 4, 1, 4}, {1, 2, 3, 2, 4}};
-constexpr int kTileCount = sizeof kTiles / sizeof *kTiles;
+// What each is for, bf16: 0 many outputs (4096^3: 100 us, 112 and 150 on the others); 1 half as many, or groups of a few hundred rows (8192 rows of 32
+// groups, 2048 -> 4096: 216, 199, 274; 2048 x 4096 x 4096: 83, 57, 76); 2 few of them, and fp32, whose matrix instructions take so long that nothing
+// else matters.  Operands that are no whole 16-byte pieces run on product_kernel in tile 2's shape.
+constexpr TileShape kTiles[] = {{4, 4, 2, 1, 8}, {2, 4, 3, 1, 8}, {1, 2, 3, 2, 4}};
+constexpr int kTileCount = 3, kSmallTile = 2;
+
+// Estimated times, in us: of a K tile where workgroups are alone on their CU and few on the chip; where they fill it; the same of what else
+// a workgroup does.
+struct TileTime {
+  double k_few, k_full, store_few, store_full;
+};
+TileTime tile_time(int tile, int dtype, bool aligned, bool strided) {
+  if (dtype == STRIPE_F32) return aligned ? TileTime{1.0, 1.95, 3, 5} : strided ? TileTime{2.4, 3.2, 3, 5} : TileTime{1.4, 2.4, 3, 5};
+  if (!aligned) return {0.75, 1.1, 3, 5};
+  constexpr TileTime t[] = {{1.1, 1.45, 6, 9}, {0.56, 0.76, 4, 5}, {0.28, 0.5, 3, 5}};
+  return t[tile];
+}
 
 // A kernel's LDS beyond 64 KB has to be allowed once on each device.
 template <typename K>
@@ -729,12 +744,13 @@ hipError_t launch_kind(const ProductPlan& plan, bool aligned, ProductParams& p, 
   const dim3 grid((unsigned)((total + 7) / 8 * 8), (unsigned)plan.splits);
   hipError_t e;
   if (aligned) {
-    e = plan.tile == 0 ? launch_stream<T, KIND, 0>(p, grid, stream) : plan.tile == 1 ? launch_stream<T, KIND, 1>(p, grid, stream)
-      : plan.tile == 2 ? launch_stream<T, KIND, 2>(p, grid, stream) : launch_stream<T, KIND, 3>(p, grid, stream);
+    if constexpr (sizeof(T) == 2)
+      e = plan.tile == 0 ? launch_stream<T, KIND, 0>(p, grid, stream) : plan.tile == 1 ? launch_stream<T, KIND, 1>(p, grid, stream) : launch_stream<T, KIND, 2>(p, grid, stream);
+    else
+      e = launch_stream<T, KIND, kSmallTile>(p, grid, stream);
   } else {
-    const int bytes = 2 * (bm + bn) * kDepthBytes;
-    if (plan.tile == 0) product_kernel<T, KIND, 2, 2><<<grid, dim3(256), bytes, stream>>>(p);
-    else product_kernel<T, KIND, 1, 2><<<grid, dim3(256), bytes, stream>>>(p);
+    constexpr TileShape s = kTiles[kSmallTile];
+    product_kernel<T, KIND, s.fm, s.fn><<<grid, dim3(256), 2 * (bm + bn) * kDepthBytes, stream>>>(p);
     e = hipGetLastError();
   }
   if (e != hipSuccess || plan.splits == 1) return e;
@@ -755,10 +771,11 @@ hipError_t launch_type(ProductKind kind, const ProductPlan& plan, bool aligned, 
 
 }  // namespace
 
-// The tile and the slices of the reduction with the smallest estimated time, in us.  A K tile takes a workgroup its matrix instructions (of all
-// workgroups on its CU; at three quarters of the peak rate) or the way of its operands through the ring, whichever is longer.
+// The tile and the slices of the reduction with the smallest estimated time: the workgroups of the CU that has most of them one after the other,
+// or in pairs where two fit.
 ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, bool aligned) {
   ProductPlan plan;
+  plan.tile = kSmallTile;
   // few rows (of a group, on average): W is read once, whatever is computed with it.  4096 x 4096 bf16: 1 row 8.4 us, 16 10.5, 32 13.8 where 128 x 128
   // tiles take 42; 64 groups of 2048 x 1024: 16 rows 14.2 against 25.1, 256 53 against 59, 512 67 against 60.
   if (kind == kForward && (rows <= 32 || (groups && rows <= 4 * (int64_t)groups))) plan.few = rows <= 16 || groups ? 1 : 2;
@@ -766,29 +783,30 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
   if (plan.few || !rows) return plan;
   const int64_t m = kind == kWeightGrad ? out : rows, n = kind == kForward ? out : in, k = kind == kForward ? in : kind == kInputGrad ? out : rows;
   const int64_t images = kind == kWeightGrad ? std::max(1, groups) : 1, depth = dtype == STRIPE_F32 ? 32 : 64;
-  const double latency = aligned ? 0.62 : 1.2, rate = dtype == STRIPE_F32 ? 0.55 : 7.0;      // us of a fetch; Mflop per us of a CU
+  const double depth_of = kind == kWeightGrad && groups ? (double)k / groups : (double)k;
+  const int64_t k_tiles = std::max<int64_t>(1, (int64_t)std::ceil(depth_of / (double)depth));
   double best = __builtin_huge_val();
   const int forced_tile = tune_int("product_tile", -1), forced_splits = tune_int("product_splits", 0);
   for (int tile = 0; tile < kTileCount; ++tile) {
+    if (tile != kSmallTile && (!aligned || dtype == STRIPE_F32 || (forced_tile >= 0 && tile != forced_tile))) continue;
+    if (tile == kSmallTile && best < __builtin_huge_val() && forced_tile >= 0 && forced_tile != kSmallTile) continue;
     const TileShape s = kTiles[tile];
-    if (!aligned && (tile == 1 || tile == 2)) continue;
-    if (forced_tile >= 0 && tile != forced_tile && (aligned || forced_tile == 0 || forced_tile == 3)) continue;
+    const TileTime t = tile_time(tile, dtype, aligned, kind == kWeightGrad);
     const int64_t bm = 64 * s.fm, bn = 64 * s.fn;
     const double row_tiles = kind == kWeightGrad ? (double)((m + bm - 1) / bm * images)
-                             : groups            ? (double)m / bm + 0.5 * std::min<double>(groups, (double)m)
+                             : groups            ? (double)m / (double)bm + 0.5 * std::min<double>(groups, (double)m)
                                                  : (double)((m + bm - 1) / bm);
-    const double tiles = row_tiles * (double)((n + bn - 1) / bn), depth_of = kind == kWeightGrad && groups ? (double)k / groups : (double)k;
-    const int64_t k_tiles = std::max<int64_t>(1, (int64_t)((depth_of + depth - 1) / depth));
+    const double tiles = row_tiles * (double)((n + bn - 1) / bn);
     for (int splits = 1; splits <= 16; ++splits) {
       if (splits > 1 && (k_tiles < 2 * splits || (forced_splits && splits != forced_splits))) continue;
       const int64_t bytes = splits > 1 ? splits * images * m * n * 4 : 0;
       if (bytes > (64 << 20)) continue;
-      const double workgroups = std::max(1.0, tiles * splits), resident = s.resident;
-      const double rounds = std::ceil(workgroups / (256 * resident)), together = std::min(resident, std::ceil(workgroups / 256));
-      const double flop = 2e-6 * bm * bn * depth / rate;
-      const double each = std::max(latency / (s.stages - 1), together * flop), store = 1.0 + together * bm * bn / 20000.0;
-      double us = 3.0 + rounds * (std::ceil((double)k_tiles / splits) * each + store);
-      if (splits > 1) us += 2.5 + (double)bytes * 2 / 4e6;
+      const double workgroups = std::max(1.0, tiles * splits), most = std::ceil(workgroups / 256), full = std::min(1.0, workgroups / 256);
+      const double kt = std::ceil((double)k_tiles / splits);
+      double us = 4;
+      if (s.resident == 1) us += most * (kt * (t.k_few + (t.k_full - t.k_few) * full) + t.store_few + (t.store_full - t.store_few) * full);
+      else us += std::floor(most / 2) * (kt * t.k_full + t.store_full) + std::fmod(most, 2) * (kt * t.k_few + t.store_few);
+      if (splits > 1) us += 2.0 + (double)bytes * 2.5 / 4e6;
       if (us < best) {
         best = us;
         plan.tile = tile;
