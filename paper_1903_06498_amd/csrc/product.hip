@@ -612,8 +612,9 @@ __global__ __launch_bounds__(256) void product_join_kernel(const ProductParams p
 }
 
 // ---- dz = dy act'(z), and the bias gradient -------------------------------------
-// A workgroup takes up to 64 rows of one group (a "slot") by 64 pieces of 16 bytes, a row per wavefront at a time.
-constexpr int kSlot = 64;
+// A workgroup takes up to 32 rows of one group (a "slot") by 64 pieces of 16 bytes, a row per wavefront at a time.  (64 rows: too few
+// workgroups for 4096 x 2048 in 16 groups; 16: twice the partial sums.)
+constexpr int kSlot = 32;
 
 template <typename T>
 __global__ __launch_bounds__(256) void dz_kernel(const DzParams p, int strips) {
@@ -623,8 +624,8 @@ __global__ __launch_bounds__(256) void dz_kernel(const DzParams p, int strips) {
   const int slot = (int)(blockIdx.x / (unsigned)strips), strip = (int)(blockIdx.x % (unsigned)strips);
   RowTile r = {0, slot * kSlot, 0};
   if (p.groups) {
-    if (slot >= count_row_tiles(p.offsets, p.groups, p.rows, kSlot)) return;
     r = find_row_tile(p.offsets, p.groups, p.rows, kSlot, slot);
+    if (r.rows <= 0) return;      // behind the last one
   } else {
     const int left = p.rows - r.row0;
     r.rows = left < kSlot ? left : kSlot;
@@ -634,7 +635,7 @@ __global__ __launch_bounds__(256) void dz_kernel(const DzParams p, int strips) {
 #pragma unroll
   for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
   if (n > 0) {
-#pragma unroll 4
+#pragma unroll 8
     for (int q = wave; q < r.rows; q += 4) {
       const int64_t row = (int64_t)r.row0 + q;
       float d[VEC];
@@ -642,8 +643,7 @@ __global__ __launch_bounds__(256) void dz_kernel(const DzParams p, int strips) {
       if (p.z) {
         float z[VEC];
         unpack<T>(load_piece<T>((const T*)p.z + row * p.y_row + c, n), z);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) d[i] *= slope<T>(z[i], p.act);
+        times_slope<T>(d, z, p.act);
         if (p.dz) store_piece<T>((T*)p.dz + row * p.dz_row + c, pack<T>(d), n);
       }
 #pragma unroll
