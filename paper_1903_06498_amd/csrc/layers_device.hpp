@@ -64,6 +64,23 @@ __device__ __forceinline__ u32x4 pack(const float (&f)[kVec<T>]) {
   return v;
 }
 
+// ---- sums over a wavefront -------------------------------------------------------
+// In the same order in every call; every lane gets the total.  Six additions whose second operand comes through the lanes' crossbar (a shuffle
+// through LDS hardware takes ten times as long).
+__device__ __forceinline__ float wave_sum(float v) {
+  auto from = [](float x, auto ctrl, auto rows) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, decltype(rows)::value, 0xf, true));
+  };
+  using std::integral_constant;
+  v += from(v, integral_constant<int, 0xb1>{}, integral_constant<int, 0xf>{});       // lane ^ 1
+  v += from(v, integral_constant<int, 0x4e>{}, integral_constant<int, 0xf>{});       // lane ^ 2
+  v += from(v, integral_constant<int, 0x141>{}, integral_constant<int, 0xf>{});      // mirrored within 8
+  v += from(v, integral_constant<int, 0x140>{}, integral_constant<int, 0xf>{});      // mirrored within 16
+  v += from(v, integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});      // rows 0 and 2 of 16 lanes into rows 1 and 3
+  v += from(v, integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});      // the lower half into the upper
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+
 // ---- activations ---------------------------------------------------------------
 // In a bf16 pipeline the hardware's exponential and reciprocal (2 ulp of fp32) are far inside the result's rounding.
 template <typename T>
@@ -190,6 +207,18 @@ __device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_am
 struct RowTile {
   int group, row0, rows;   // first row, rows of the tile (at most height)
 };
+// Of a chunk of groups from number `base` on, the tile number t if it is among them.
+__device__ __forceinline__ bool tile_in_chunk(const GroupChunk& c, int base, int height, int t, RowTile* r) {
+  const uint64_t past = __ballot(c.through > t);
+  if (!past) return false;
+  const int at = __builtin_ctzll(past);
+  const int first = t - (lane_value(c.through, at) - lane_value(c.tiles, at));
+  r->group = base + at;
+  r->row0 = lane_value(c.start, at) + first * height;
+  const int left = lane_value(c.end, at) - r->row0;
+  r->rows = left < height ? left : height;
+  return true;
+}
 // All groups' tiles of `height` rows.
 __device__ __forceinline__ int count_row_tiles(const int32_t* offsets, int groups, int rows, int height) {
   int end = limited(offsets[0], rows), tiles = 0;
@@ -206,16 +235,7 @@ __device__ __forceinline__ RowTile find_row_tile(const int32_t* offsets, int gro
   RowTile r = {0, 0, 0};
   for (int base = 0; base < groups; base += 64) {
     const GroupChunk c = group_chunk(offsets, groups, rows, base, end, tiles, height);
-    const uint64_t past = __ballot(c.through > t);
-    if (past) {
-      const int at = __builtin_ctzll(past);
-      const int first = t - (lane_value(c.through, at) - lane_value(c.tiles, at));
-      r.group = base + at;
-      r.row0 = lane_value(c.start, at) + first * height;
-      const int left = lane_value(c.end, at) - r.row0;
-      r.rows = left < height ? left : height;
-      return r;
-    }
+    if (tile_in_chunk(c, base, height, t, &r)) return r;
     end = lane_value(c.end, 63);
     tiles = lane_value(c.through, 63);
   }

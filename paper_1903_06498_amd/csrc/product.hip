@@ -194,7 +194,15 @@ template <int KIND, int BM, int BN>
 __device__ __forceinline__ bool place(const ProductParams& p, Tile* t) {
   constexpr unsigned PATCH = BM >= 256 ? 4 : 8;
   unsigned row_tiles = (unsigned)p.tiles_m, total, l;
-  if (KIND != kWeightGrad && p.groups) row_tiles = (unsigned)count_row_tiles(p.offsets, p.groups, p.rows, BM);
+  GroupChunk chunk;      // of up to 64 groups: all of them
+  if (KIND != kWeightGrad && p.groups) {
+    if (p.groups <= 64) {
+      chunk = group_chunk(p.offsets, p.groups, p.rows, 0, limited(p.offsets[0], p.rows), 0, BM);
+      row_tiles = (unsigned)lane_value(chunk.through, 63);
+    } else {
+      row_tiles = (unsigned)count_row_tiles(p.offsets, p.groups, p.rows, BM);
+    }
+  }
   total = row_tiles * (unsigned)p.tiles_n;
   if (KIND == kWeightGrad && p.groups) total *= (unsigned)p.groups;
   if (!logical_number(blockIdx.x, total, &l)) return false;
@@ -211,7 +219,9 @@ __device__ __forceinline__ bool place(const ProductParams& p, Tile* t) {
   t->k0 = 0;
   t->k = p.K;
   if (KIND != kWeightGrad && p.groups) {
-    const RowTile r = find_row_tile(p.offsets, p.groups, p.rows, BM, tm);
+    RowTile r = {0, 0, 0};
+    if (p.groups <= 64) tile_in_chunk(chunk, 0, BM, tm, &r);
+    else r = find_row_tile(p.offsets, p.groups, p.rows, BM, tm);
     t->group = r.group;
     t->m0 = r.row0;
     t->m = r.rows;
