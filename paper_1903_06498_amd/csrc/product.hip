@@ -111,6 +111,7 @@ struct Fetch : Operand<T, WIDTH, STRIDED> {
   const T* src[LOADS];
   int k[LOADS], left[LOADS];      // its first k; elements of it inside the rows' range (strided) -- else a constant
   int64_t step;                   // elements from one K tile to the next
+  bool wide;                      // all columns of the tile exist (strided)
 
   // base: element (row0, k = 0); rows: valid rows from row0 on; ld: row stride
   __device__ __forceinline__ void init(const T* base, int rows, int64_t ld) {
@@ -129,6 +130,7 @@ struct Fetch : Operand<T, WIDTH, STRIDED> {
       }
     }
     step = STRIDED ? DEPTH * ld : DEPTH;
+    wide = !STRIDED || rows >= WIDTH;
   }
   // elements of piece u of K tile kt that exist
   __device__ __forceinline__ int valid(int u, int kt, int K) const {
@@ -137,8 +139,20 @@ struct Fetch : Operand<T, WIDTH, STRIDED> {
     else return n > 0 ? left[u] : 0;
   }
   __device__ __forceinline__ void fetch(u32x4 (&to)[LOADS], int kt, int K) const {
+    if (wide && (kt + 1) * DEPTH <= K) {      // uniform: everything exists
 #pragma unroll
-    for (int u = 0; u < LOADS; ++u) to[u] = load_piece<T>(src[u] + (int64_t)kt * step, valid(u, kt, K));
+      for (int u = 0; u < LOADS; ++u) __builtin_memcpy(&to[u], src[u] + (int64_t)kt * step, 16);
+      return;
+    }
+    // whole pieces first, all on their way before the rims' elements, one by one, are waited for
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u) to[u] = (u32x4){0, 0, 0, 0};
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u)
+      if (valid(u, kt, K) >= VEC) __builtin_memcpy(&to[u], src[u] + (int64_t)kt * step, 16);
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u)
+      if (const int n = valid(u, kt, K); n > 0 && n < VEC) to[u] = load_piece<T>(src[u] + (int64_t)kt * step, n);
   }
   static __device__ __forceinline__ void put(unsigned char* stage, const u32x4 (&from)[LOADS]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
