@@ -60,6 +60,7 @@ struct ProductParams {
 struct ProductPlan {
   int tile = 0;             // index into the tile table
   int splits = 1;
+  bool parts = false;       // fp32 in three bf16 parts
   int few = 0;              // kForward: the kernel for few rows, 16 times as many at a time (product_rows.hip)
   int64_t ws_bytes = 0;     // partial images
 };

@@ -100,7 +100,9 @@ struct Operand {
   }
 };
 
-// Where the pieces of an operand come from, element by element at its rims: any alignment.
+// Where the pieces of an operand come from: any alignment.  Every piece of a K tile that exists as a whole is one 16-byte load without a condition -- a
+// load beside a branch would make the compiler wait for all loads at each use, prefetched tiles included.  A strided operand's piece that hangs over the
+// last row lies back as far as it hangs over and is shifted when it is used.
 template <typename T, int WIDTH, bool STRIDED>
 struct Fetch : Operand<T, WIDTH, STRIDED> {
   using Operand<T, WIDTH, STRIDED>::VEC;
@@ -109,55 +111,120 @@ struct Fetch : Operand<T, WIDTH, STRIDED> {
   using Operand<T, WIDTH, STRIDED>::LOADS;
   using Operand<T, WIDTH, STRIDED>::key;
   const T* src[LOADS];
-  int k[LOADS], left[LOADS];      // its first k; elements of it inside the rows' range (strided) -- else a constant
+  int k[LOADS];                   // its first k
+  int back[LOADS];                // elements that the piece lies back (strided)
   int64_t step;                   // elements from one K tile to the next
-  bool wide;                      // all columns of the tile exist (strided)
+  int few;                        // strided, fewer rows in all than a piece has elements: their number, else 0
+  bool hangs;                     // some piece lies back
 
-  // base: element (row0, k = 0); rows: valid rows from row0 on; ld: row stride
-  __device__ __forceinline__ void init(const T* base, int rows, int64_t ld) {
+  // base: element (row0, k = 0); rows: valid rows from row0 on, behind `before` others; ld: row stride
+  __device__ __forceinline__ void init(const T* base, int rows, int before, int64_t ld) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    few = STRIDED && rows + before < VEC ? rows : 0;      // (then row0 = 0)
+    hangs = STRIDED && rows < WIDTH && !few;
 #pragma unroll
     for (int u = 0; u < LOADS; ++u) {
       const int at = (u * 4 + wave) * 1024 + lane * 16, r = at / ROW, piece = (at % ROW / 16) ^ key(r);
+      back[u] = 0;
       if constexpr (!STRIDED) {
         k[u] = piece * VEC;
-        left[u] = 0;
         src[u] = base + (int64_t)(r < rows ? r : rows - 1) * ld + k[u];
       } else {
         k[u] = r;
-        left[u] = rows - piece * VEC;
-        src[u] = base + (int64_t)r * ld + piece * VEC;
+        const int over = (piece + 1) * VEC - rows;
+        if (hangs && over > 0) back[u] = over;
+        src[u] = base + (int64_t)r * ld + piece * VEC - back[u];
       }
     }
     step = STRIDED ? DEPTH * ld : DEPTH;
-    wide = !STRIDED || rows >= WIDTH;
   }
-  // elements of piece u of K tile kt that exist
-  __device__ __forceinline__ int valid(int u, int kt, int K) const {
-    const int n = K - (k[u] + kt * DEPTH);
-    if constexpr (!STRIDED) return n;
-    else return n > 0 ? left[u] : 0;
-  }
+  // whether K tile kt consists of whole pieces
+  __device__ __forceinline__ bool whole(int kt, int K) const { return !few && (kt + 1) * DEPTH <= K; }
+  template <bool WHOLE>
   __device__ __forceinline__ void fetch(u32x4 (&to)[LOADS], int kt, int K) const {
-    if (wide && (kt + 1) * DEPTH <= K) {      // uniform: everything exists
+    if constexpr (WHOLE) {
 #pragma unroll
       for (int u = 0; u < LOADS; ++u) __builtin_memcpy(&to[u], src[u] + (int64_t)kt * step, 16);
-      return;
+    } else {
+#pragma unroll
+      for (int u = 0; u < LOADS; ++u) {
+        const int n = K - (k[u] + kt * DEPTH), left = few - (int)(threadIdx.x % (ROW / 16) ^ key(k[u])) * VEC;
+        to[u] = (u32x4){0, 0, 0, 0};
+        if (!STRIDED || few) to[u] = load_piece<T>(src[u] + (int64_t)kt * step, !STRIDED ? n : n > 0 ? left : 0);
+        else if (n > 0) __builtin_memcpy(&to[u], src[u] + (int64_t)kt * step, 16);
+      }
     }
-    // whole pieces first, all on their way before the rims' elements, one by one, are waited for
+  }
+  __device__ __forceinline__ void shift(u32x4 (&v)[LOADS]) const {
+    if (!STRIDED || !hangs) return;
 #pragma unroll
-    for (int u = 0; u < LOADS; ++u) to[u] = (u32x4){0, 0, 0, 0};
-#pragma unroll
-    for (int u = 0; u < LOADS; ++u)
-      if (valid(u, kt, K) >= VEC) __builtin_memcpy(&to[u], src[u] + (int64_t)kt * step, 16);
-#pragma unroll
-    for (int u = 0; u < LOADS; ++u)
-      if (const int n = valid(u, kt, K); n > 0 && n < VEC) to[u] = load_piece<T>(src[u] + (int64_t)kt * step, n);
+    for (int u = 0; u < LOADS; ++u) {
+      u32x4 x = v[u];
+      if constexpr (sizeof(T) == 2) {
+        const u32x4 half = {x[0] >> 16 | x[1] << 16, x[1] >> 16 | x[2] << 16, x[2] >> 16 | x[3] << 16, x[3] >> 16};
+        x = back[u] & 1 ? half : x;
+      }
+      const int words = back[u] * (int)sizeof(T) / 4;
+      const u32x4 one = {x[1], x[2], x[3], 0};
+      x = words & 1 ? one : x;
+      const u32x4 two = {x[2], x[3], 0, 0};
+      v[u] = words & 2 ? two : x;
+    }
   }
   static __device__ __forceinline__ void put(unsigned char* stage, const u32x4 (&from)[LOADS]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int u = 0; u < LOADS; ++u) *(u32x4*)(stage + (u * 4 + wave) * 1024 + lane * 16) = from[u];
+  }
+};
+
+// fp32 on the bf16 matrix instructions: v = hi + mid + lo, three bf16 values that hold all 24 bits (each is the rounding of what the ones before it left,
+// and the remainders are exact), and a b = lo hi + mid mid + hi lo + mid hi + hi mid + hi hi up to 2^-25 of it.  Six instructions of 16 cycles take the
+// place of eight of 32, the fp32 rate's.  LDS holds a plane of each part, a K tile of 32:
+//   [row][k]: 64 bytes per row, 16-byte piece c of row r in slot c ^ ((r >> 2) & 3);
+//   [k][row]: as a bf16 operand's.
+template <int WIDTH, bool STRIDED>
+struct Split : Operand<__bf16, WIDTH, STRIDED> {
+  using Half = Operand<__bf16, WIDTH, STRIDED>;
+  using From = Fetch<float, WIDTH, STRIDED>;
+  static constexpr int PLANE = WIDTH * 64, STAGE = 3 * PLANE;
+  static __device__ __forceinline__ void split(const u32x4 (&from)[From::LOADS], u32x2 (&part)[From::LOADS][3]) {
+#pragma unroll
+    for (int u = 0; u < From::LOADS; ++u) {
+      f32x4 v = __builtin_bit_cast(f32x4, from[u]);
+#pragma unroll
+      for (int p = 0; p < 3; ++p) {
+        part[u][p] = __builtin_bit_cast(u32x2, __builtin_convertvector(v, bf16x4));
+        if (p < 2) {
+          const uint32_t x = part[u][p].x, y = part[u][p].y;
+          v -= __builtin_bit_cast(f32x4, (u32x4){x << 16, x & 0xffff0000u, y << 16, y & 0xffff0000u});
+        }
+      }
+    }
+  }
+  static __device__ __forceinline__ void put(unsigned char* stage, const u32x2 (&part)[From::LOADS][3]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int u = 0; u < From::LOADS; ++u) {
+      const int at = (u * 4 + wave) * 1024 + lane * 16, r = at / From::ROW, piece = (at % From::ROW / 16) ^ From::key(r);      // as fetched
+      unsigned to;
+      if constexpr (!STRIDED) to = r * 64 + (((piece >> 1) ^ ((r >> 2) & 3)) << 4) + (piece & 1) * 8;
+      else to = r * Half::ROW + (((piece >> 1) ^ Half::key(r)) << 4) + (piece & 1) * 8;
+#pragma unroll
+      for (int p = 0; p < 3; ++p) *(u32x2*)(stage + p * PLANE + to) = part[u][p];
+    }
+  }
+  static __device__ __forceinline__ unsigned first(int row0) {
+    if constexpr (STRIDED) {
+      return Half::first(row0);
+    } else {
+      const int lane = threadIdx.x & 63, fr = lane & 15;
+      return (row0 + fr) * 64 + (((lane >> 4) ^ ((fr >> 2) & 3)) << 4);
+    }
+  }
+  static __device__ __forceinline__ u32x4 fragment(const unsigned char* plane, unsigned first, int i) {
+    if constexpr (STRIDED) return Half::fragment(plane, first, i, 0);
+    else return *(const u32x4*)(plane + first + i * 16 * 64);
   }
 };
 
@@ -173,7 +240,7 @@ struct Stream : Operand<T, WIDTH, STRIDED, WAVES> {
   uint64_t base, step;            // of the next K tile, bytes to the one after it
   uint32_t from[LOADS];
 
-  __device__ __forceinline__ void init(const T* at0, int rows, int64_t ld) {
+  __device__ __forceinline__ void init(const T* at0, int rows, int, int64_t ld) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int u = 0; u < LOADS; ++u) {
@@ -394,12 +461,12 @@ __device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t
 template <typename T, int KIND, typename A, typename B>
 __device__ __forceinline__ void init_operands(const ProductParams& p, const Tile& t, A& a, B& b) {
   if constexpr (KIND == kWeightGrad) {
-    a.init((const T*)p.a + (int64_t)t.k0 * p.a_ld + t.m0, t.m, p.a_ld);
-    b.init((const T*)p.b + (int64_t)t.k0 * p.b_ld + t.n0, p.N - t.n0, p.b_ld);
+    a.init((const T*)p.a + (int64_t)t.k0 * p.a_ld + t.m0, p.M - t.m0, t.m0, p.a_ld);
+    b.init((const T*)p.b + (int64_t)t.k0 * p.b_ld + t.n0, p.N - t.n0, t.n0, p.b_ld);
   } else {
     const T* w = (const T*)p.b + (int64_t)t.group * p.b_group;
-    a.init((const T*)p.a + (int64_t)t.m0 * p.a_ld, t.m, p.a_ld);
-    b.init(KIND == kForward ? w + (int64_t)t.n0 * p.b_ld : w + t.n0, p.N - t.n0, p.b_ld);
+    a.init((const T*)p.a + (int64_t)t.m0 * p.a_ld, t.m, 0, p.a_ld);
+    b.init(KIND == kForward ? w + (int64_t)t.n0 * p.b_ld : w + t.n0, p.N - t.n0, t.n0, p.b_ld);
   }
 }
 // This workgroup's K tiles of `all`.
@@ -413,9 +480,11 @@ __device__ __forceinline__ void own_k_tiles(const ProductParams& p, int all, int
   }
 }
 
-// Operands at any alignment: through registers, two stages of the ring, one K tile ahead.
+// Operands at any alignment, and fp32: through registers, two stages, two K tiles ahead.
+// fp32 sums that end as NaN -- an operand was infinite, NaN or within half a bf16 step of overflow, which leave no finite remainder, or the sum itself
+// met opposite infinities -- are not what fp32 arithmetic gives; their workgroup computes its tile again with fp32 instructions.
 template <typename T, int KIND, int FM, int FN>
-__global__ __launch_bounds__(256) void product_kernel(const ProductParams p) {
+__global__ __launch_bounds__(256, 2) void product_kernel(const ProductParams p) {
   constexpr int BM = 64 * FM, BN = 64 * FN, R = 2 * FM, C = 2 * FN;      // fragments of a wavefront
   using A = Fetch<T, BM, KIND == kWeightGrad>;
   using B = Fetch<T, BN, KIND != kForward>;
@@ -437,17 +506,104 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductParams p) {
 #pragma unroll
     for (int j = 0; j < C; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
 
+  u32x4 ra[2][A::LOADS], rb[2][B::LOADS];      // of tiles kt0, kt0 + 2 ..., and of the others
+  bool native = true;
+  if constexpr (sizeof(T) == 4) {
+    using SA = Split<BM, KIND == kWeightGrad>;
+    using SB = Split<BN, KIND != kForward>;
+    unsigned char *const split_a = lds, *const split_b = lds + 2 * SA::STAGE;
+    const unsigned first_a = SA::first(wm * R * 16), first_b = SB::first(wn * C * 16);
+    // tile kt from stage `at`, while tile kt + 1 (in na, nb) is split and goes to the other stage, and tile kt + 3 is asked for
+    auto tile = [&](auto all, int kt, u32x4 (&na)[A::LOADS], u32x4 (&nb)[B::LOADS], int at) {
+      constexpr bool WHOLE = decltype(all)::value;
+      const unsigned char *const stage_a = split_a + at * SA::STAGE, *const stage_b = split_b + at * SB::STAGE;
+      __syncthreads();          // the tile is complete, and the other stage was read
+      u32x4 fa[3][R], fb[3][C];
+#pragma unroll
+      for (int part = 0; part < 3; ++part) {
+#pragma unroll
+        for (int j = 0; j < C; ++j) fb[part][j] = SB::fragment(stage_b + part * SB::PLANE, first_b, j);
+#pragma unroll
+        for (int i = 0; i < R; ++i) fa[part][i] = SA::fragment(stage_a + part * SA::PLANE, first_a, i);
+      }
+      u32x2 pa[A::LOADS][3], pb[B::LOADS][3];
+      a.shift(na);
+      b.shift(nb);
+      SA::split(na, pa);
+      SB::split(nb, pb);
+      constexpr int ORDER[6][2] = {{0, 0}, {0, 1}, {1, 0}, {1, 1}, {0, 2}, {2, 0}};      // as the parts arrive
+#pragma unroll
+      for (int o = 0; o < 6; ++o)
+#pragma unroll
+        for (int i = 0; i < R; ++i) mma_row<__bf16, C>(fa[ORDER[o][0]][i], fb[ORDER[o][1]], acc[i]);
+      SA::put(split_a + (at ^ 1) * SA::STAGE, pa);
+      SB::put(split_b + (at ^ 1) * SB::STAGE, pb);
+      // the splitting runs beside the matrix instructions
+#pragma unroll
+      for (int i = 0; i < 6 * R * C; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
+      }
+      a.template fetch<WHOLE>(na, kt + 3, t.k);
+      b.template fetch<WHOLE>(nb, kt + 3, t.k);
+    };
+    {
+      u32x2 pa[A::LOADS][3], pb[B::LOADS][3];
+      if (a.whole(kt0 + 1, t.k) && b.whole(kt0 + 1, t.k)) {
+        a.template fetch<true>(ra[0], kt0, t.k);
+        b.template fetch<true>(rb[0], kt0, t.k);
+        a.template fetch<true>(ra[1], kt0 + 1, t.k);
+        b.template fetch<true>(rb[1], kt0 + 1, t.k);
+      } else {
+        a.template fetch<false>(ra[0], kt0, t.k);
+        b.template fetch<false>(rb[0], kt0, t.k);
+        a.template fetch<false>(ra[1], kt0 + 1, t.k);
+        b.template fetch<false>(rb[1], kt0 + 1, t.k);
+      }
+      a.shift(ra[0]);
+      b.shift(rb[0]);
+      SA::split(ra[0], pa);
+      SB::split(rb[0], pb);
+      SA::put(split_a, pa);
+      SB::put(split_b, pb);
+      a.template fetch<false>(ra[0], kt0 + 2, t.k);
+      b.template fetch<false>(rb[0], kt0 + 2, t.k);
+    }
+    int kt = kt0;
+    for (; kt + 1 < kt1 && a.whole(kt + 4, t.k) && b.whole(kt + 4, t.k); kt += 2) {
+      tile(std::true_type{}, kt, ra[1], rb[1], 0);
+      tile(std::true_type{}, kt + 1, ra[0], rb[0], 1);
+    }
+    for (; kt < kt1; kt += 2) {
+      tile(std::false_type{}, kt, ra[1], rb[1], 0);
+      if (kt + 1 < kt1) tile(std::false_type{}, kt + 1, ra[0], rb[0], 1);
+    }
+    native = false;
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int j = 0; j < C; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) native = native || acc[i][j][v] != acc[i][j][v];
+    native = __syncthreads_or(native);
+    if (native) {
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int j = 0; j < C; ++j) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+  }
+  if (native) {
   const unsigned first_a = A::first(wm * R * 16), first_b = B::first(wn * C * 16);
-  u32x4 ra[A::LOADS], rb[B::LOADS];
-  a.fetch(ra, kt0, t.k);
-  b.fetch(rb, kt0, t.k);
-  for (int kt = kt0; kt < kt1; ++kt) {
-    const int stage = kt & 1;
-    A::put(lds_a + stage * A::STAGE, ra);
-    B::put(lds_b + stage * B::STAGE, rb);
-    __syncthreads();          // (the stage that the next turn writes was read before this barrier's turn)
-    a.fetch(ra, kt + 1, t.k);
-    b.fetch(rb, kt + 1, t.k);
+  auto tile = [&](auto all, int kt, u32x4 (&na)[A::LOADS], u32x4 (&nb)[B::LOADS], int stage) {
+    constexpr bool WHOLE = decltype(all)::value;
+    a.shift(na);
+    b.shift(nb);
+    A::put(lds_a + stage * A::STAGE, na);
+    B::put(lds_b + stage * B::STAGE, nb);
+    __syncthreads();
+    a.template fetch<WHOLE>(na, kt + 2, t.k);
+    b.template fetch<WHOLE>(nb, kt + 2, t.k);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       u32x4 fa[R], fb[C];
@@ -458,8 +614,22 @@ __global__ __launch_bounds__(256) void product_kernel(const ProductParams p) {
 #pragma unroll
       for (int i = 0; i < R; ++i) mma_row<T, C>(fa[i], fb, acc[i]);
     }
+  };
+  if (sizeof(T) == 4) __syncthreads();      // the parts' stages were read
+  a.template fetch<false>(ra[0], kt0, t.k);
+  b.template fetch<false>(rb[0], kt0, t.k);
+  a.template fetch<false>(ra[1], kt0 + 1, t.k);
+  b.template fetch<false>(rb[1], kt0 + 1, t.k);
+  int kt = kt0;
+  for (; kt + 1 < kt1 && a.whole(kt + 3, t.k) && b.whole(kt + 3, t.k); kt += 2) {
+    tile(std::true_type{}, kt, ra[0], rb[0], 0);
+    tile(std::true_type{}, kt + 1, ra[1], rb[1], 1);
   }
-
+  for (; kt < kt1; kt += 2) {
+    tile(std::false_type{}, kt, ra[0], rb[0], 0);
+    if (kt + 1 < kt1) tile(std::false_type{}, kt + 1, ra[1], rb[1], 1);
+  }
+  }
   store_tile<T, KIND, FM, C, 4>(p, t, lds, acc);
 }
 
@@ -721,8 +891,10 @@ constexpr int kTileCount = 3, kSmallTile = 2;
 struct TileTime {
   double k_few, k_full, store_few, store_full;
 };
-TileTime tile_time(int tile, int dtype, bool aligned, bool strided) {
-  if (dtype == STRIPE_F32) return aligned ? TileTime{1.0, 1.95, 3, 5} : strided ? TileTime{2.4, 3.2, 3, 5} : TileTime{1.4, 2.4, 3, 5};
+// parts: fp32 split into three bf16 parts, which is faster where the matrix instructions are what a CU waits for (2048^3: 124 us with fp32
+// instructions, 106), and slower where it is the way through the registers (512^3: 12.4 and 14.2).
+TileTime tile_time(int tile, int dtype, bool aligned, bool parts) {
+  if (dtype == STRIPE_F32) return parts ? TileTime{0.95, 1.55, 5, 7} : TileTime{1.0, 1.95, 3, 5};
   if (!aligned) return {0.75, 1.1, 3, 5};
   constexpr TileTime t[] = {{1.1, 1.45, 6, 9}, {0.56, 0.76, 4, 5}, {0.28, 0.5, 3, 5}};
   return t[tile];
@@ -766,15 +938,20 @@ hipError_t launch_kind(const ProductPlan& plan, bool aligned, ProductParams& p, 
     else total = ((int64_t)p.M / bm + std::min<int64_t>(p.groups, p.M)) * p.tiles_n;
   }
   const dim3 grid((unsigned)((total + 7) / 8 * 8), (unsigned)plan.splits);
-  hipError_t e;
-  if (aligned) {
-    if constexpr (sizeof(T) == 2)
-      e = plan.tile == 0 ? launch_stream<T, KIND, 0>(p, grid, stream) : plan.tile == 1 ? launch_stream<T, KIND, 1>(p, grid, stream) : launch_stream<T, KIND, 2>(p, grid, stream);
-    else
+  hipError_t e = hipSuccess;
+  if (aligned && !plan.parts) {
+    if constexpr (sizeof(T) == 4)
       e = launch_stream<T, KIND, kSmallTile>(p, grid, stream);
+    else
+      e = plan.tile == 0 ? launch_stream<T, KIND, 0>(p, grid, stream) : plan.tile == 1 ? launch_stream<T, KIND, 1>(p, grid, stream) : launch_stream<T, KIND, 2>(p, grid, stream);
   } else {
     constexpr TileShape s = kTiles[kSmallTile];
-    product_kernel<T, KIND, s.fm, s.fn><<<grid, dim3(256), 2 * (bm + bn) * kDepthBytes, stream>>>(p);
+    constexpr int bytes = 2 * 64 * (s.fm + s.fn) * (sizeof(T) == 4 ? 3 * 64 : kDepthBytes);
+    if constexpr (bytes > 65536) {
+      static std::atomic<uint64_t> done{0};
+      if (e = allow_lds(product_kernel<T, KIND, s.fm, s.fn>, bytes, done); e != hipSuccess) return e;
+    }
+    product_kernel<T, KIND, s.fm, s.fn><<<grid, dim3(256), bytes, stream>>>(p);
     e = hipGetLastError();
   }
   if (e != hipSuccess || plan.splits == 1) return e;
@@ -811,11 +988,15 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
   const int64_t k_tiles = std::max<int64_t>(1, (int64_t)std::ceil(depth_of / (double)depth));
   double best = __builtin_huge_val();
   const int forced_tile = tune_int("product_tile", -1), forced_splits = tune_int("product_splits", 0);
-  for (int tile = 0; tile < kTileCount; ++tile) {
-    if (tile != kSmallTile && (!aligned || dtype == STRIPE_F32 || (forced_tile >= 0 && tile != forced_tile))) continue;
-    if (tile == kSmallTile && best < __builtin_huge_val() && forced_tile >= 0 && forced_tile != kSmallTile) continue;
+  // fp32: the small tile, with fp32 instructions (whole pieces only) or in parts
+  const bool f32 = dtype == STRIPE_F32;
+  for (int variant = 0; variant < kTileCount; ++variant) {
+    const bool parts = f32 && variant == 1;
+    const int tile = f32 ? kSmallTile : variant;
+    if (f32 ? variant == 2 || (!aligned && !parts) || (aligned && forced_tile >= 0 && forced_tile != variant)
+            : (!aligned && tile != kSmallTile) || (aligned && forced_tile >= 0 && tile != forced_tile)) continue;
     const TileShape s = kTiles[tile];
-    const TileTime t = tile_time(tile, dtype, aligned, kind == kWeightGrad);
+    const TileTime t = tile_time(tile, dtype, aligned, parts);
     const int64_t bm = 64 * s.fm, bn = 64 * s.fn;
     const double row_tiles = kind == kWeightGrad ? (double)((m + bm - 1) / bm * images)
                              : groups            ? (double)m / (double)bm + 0.5 * std::min<double>(groups, (double)m)
@@ -834,6 +1015,7 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
       if (us < best) {
         best = us;
         plan.tile = tile;
+        plan.parts = parts;
         plan.splits = splits;
         plan.ws_bytes = bytes;
       }
@@ -845,8 +1027,8 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
 std::string product_name(ProductKind kind, int dtype, const ProductPlan& plan, bool aligned) {
   if (plan.few) return std::string("product_rows_") + (dtype == STRIPE_F32 ? "f32_" : "bf16_") + std::to_string(16 * plan.few) + "x16";
   const TileShape s = kTiles[plan.tile];
-  return std::string(aligned ? "product_stream_" : "product_") + (kind == kForward ? "nt_" : kind == kInputGrad ? "nn_" : "tn_") + (dtype == STRIPE_F32 ? "f32_" : "bf16_") +
-         std::to_string(64 * s.fm) + "x" + std::to_string(64 * s.fn) + (aligned ? "_s" + std::to_string(s.stages) : "") +
+  return std::string(aligned && !plan.parts ? "product_stream_" : "product_") + (kind == kForward ? "nt_" : kind == kInputGrad ? "nn_" : "tn_") + (dtype == STRIPE_F32 ? "f32_" : "bf16_") +
+         std::to_string(64 * s.fm) + "x" + std::to_string(64 * s.fn) + (plan.parts ? "_parts" : aligned ? "_s" + std::to_string(s.stages) : "") +
          (plan.splits > 1 ? "_k" + std::to_string(plan.splits) : "");
 }
 
