@@ -828,21 +828,36 @@ __global__ __launch_bounds__(256) void dz_kernel(const DzParams p, int strips) {
   float sum[VEC];
 #pragma unroll
   for (int i = 0; i < VEC; ++i) sum[i] = 0.f;
-  if (n > 0) {
-#pragma unroll 8
-    for (int q = wave; q < r.rows; q += 4) {
-      const int64_t row = (int64_t)r.row0 + q;
-      float d[VEC];
-      unpack<T>(load_piece<T>((const T*)p.dy + row * p.y_row + c, n), d);
-      if (p.z) {
-        float z[VEC];
-        unpack<T>(load_piece<T>((const T*)p.z + row * p.y_row + c, n), z);
-        times_slope<T>(d, z, p.act);
-        if (p.dz) store_piece<T>((T*)p.dz + row * p.dz_row + c, pack<T>(d), n);
-      }
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) sum[i] += d[i];
+  const T *dy = (const T*)p.dy + (int64_t)r.row0 * p.y_row + c, *z = (const T*)p.z + (int64_t)r.row0 * p.y_row + c;
+  T* dz = (T*)p.dz + (int64_t)r.row0 * p.dz_row + c;
+  auto use = [&](int64_t row, u32x4 dv, u32x4 zv, int n) {
+    float d[VEC];
+    unpack<T>(dv, d);
+    if (p.z) {
+      float zf[VEC];
+      unpack<T>(zv, zf);
+      times_slope<T>(d, zf, p.act);
+      if (p.dz) store_piece<T>(dz + row * p.dz_row, pack<T>(d), n);
     }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) sum[i] += d[i];
+  };
+  if (n >= VEC && r.rows > 0) {      // (a layer without rows has a last row no more than a first)
+    // all of a wavefront's rows are on their way before the first is used (8192 x 8192 bf16, 403 MB: 112 -> 97 us); rows behind the last repeat it
+    constexpr int EACH = kSlot / 4;
+    u32x4 dv[EACH], zv[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int q = 4 * i + wave;
+      const int64_t row = q < r.rows ? q : r.rows - 1;
+      __builtin_memcpy(&dv[i], dy + row * p.y_row, 16);
+      if (p.z) __builtin_memcpy(&zv[i], z + row * p.y_row, 16);
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+      if (4 * i + wave < r.rows) use(4 * i + wave, dv[i], zv[i], VEC);
+  } else if (n > 0) {
+    for (int64_t q = wave; q < r.rows; q += 4) use(q, load_piece<T>(dy + q * p.y_row, n), p.z ? load_piece<T>(z + q * p.y_row, n) : (u32x4){0, 0, 0, 0}, n);
   }
   if (!p.db) return;
 #pragma unroll
