@@ -79,8 +79,9 @@ bool misaligned(const void* p, int64_t to) { return (uintptr_t)p % (uintptr_t)to
 
 struct stripe_linear {
   stripe_linear_desc_t d;
-  bool wide = false;                    // strides and feature counts are whole 16-byte pieces
-  ProductPlan plan[2][3];               // [operands fetched in 16-byte pieces][ProductKind]
+  Access best = kAny;                   // with 16-byte aligned buffers
+  Access otherwise = kAny;
+  ProductPlan plan[3][3];               // [Access][ProductKind]
   int64_t dz_bytes = 0, sums_bytes = 0, partial_bytes = 0;
   Workspace ws;
   int64_t ws_bytes() const { return dz_bytes + sums_bytes + partial_bytes; }
@@ -120,13 +121,16 @@ stripe_status_t linear_create(const stripe_linear_desc_t* desc, stripe_linear_t*
   auto lin = std::make_unique<stripe_linear>();
   lin->d = d;
   const int64_t v = 16 / elem_size(d.dtype);
-  // (and a tile's rows, at most 256, span less than 2^31 bytes: the kernels that load them have 32-bit offsets)
+  // the kernels that load into LDS have 32-bit offsets: a tile's rows, at most 256, span less than 2^31 bytes
   const int64_t most = (int64_t)1 << 20;
-  lin->wide = d.x_row <= most && d.w_row <= most && d.y_row <= most && d.in_features % v == 0 && d.out_features % v == 0 && d.x_row % v == 0 && d.w_row % v == 0 && d.y_row % v == 0 && (!d.groups || d.w_group % v == 0);
-  for (int aligned = 0; aligned < 2; ++aligned)
+  const bool near = d.x_row <= most && d.w_row <= most && d.y_row <= most;
+  lin->otherwise = near && d.dtype == STRIPE_F32 ? kWords : kAny;
+  lin->best = near && d.in_features % v == 0 && d.out_features % v == 0 && d.x_row % v == 0 && d.w_row % v == 0 && d.y_row % v == 0 &&
+                      (!d.groups || d.w_group % v == 0) ? kPieces : lin->otherwise;
+  for (const Access access : {lin->best, lin->otherwise})
     for (int k = 0; k < 3; ++k) {
-      lin->plan[aligned][k] = plan_product((ProductKind)k, d.dtype, d.rows, d.in_features, d.out_features, d.groups, aligned != 0);
-      lin->partial_bytes = std::max(lin->partial_bytes, round_up_256(lin->plan[aligned][k].ws_bytes));
+      lin->plan[access][k] = plan_product((ProductKind)k, d.dtype, d.rows, d.in_features, d.out_features, d.groups, access);
+      lin->partial_bytes = std::max(lin->partial_bytes, round_up_256(lin->plan[access][k].ws_bytes));
     }
   if (d.activation != STRIPE_ACT_NONE) {
     const int64_t row = (d.out_features + v - 1) / v * v;    // dz's rows start at 16-byte boundaries
@@ -155,8 +159,8 @@ stripe_status_t linear_run(stripe_linear_t* lin, const void* x, const void* w, c
   if (misaligned(x, e) || misaligned(w, e) || misaligned(residual, e) || misaligned(y, e) || misaligned(pre, e) || misaligned(bias, 4))
     return api_fail(STRIPE_ERR_MISALIGNED, "a buffer is not aligned to its element type");
   if (!d.rows) return STRIPE_OK;
-  const bool aligned = lin->wide && !misaligned(x, 16) && !misaligned(w, 16);
-  const ProductPlan& plan = lin->plan[aligned][kForward];
+  const Access access = misaligned(x, 16) || misaligned(w, 16) ? lin->otherwise : lin->best;
+  const ProductPlan& plan = lin->plan[access][kForward];
   unsigned char* ws = nullptr;
   if (plan.ws_bytes)
     if (const stripe_status_t st = lin->ws.get(lin->ws_bytes(), (hipStream_t)hip_stream, &ws); st != STRIPE_OK) return st;
@@ -167,7 +171,7 @@ stripe_status_t linear_run(stripe_linear_t* lin, const void* x, const void* w, c
   p.rows = p.M = (int32_t)d.rows; p.N = (int32_t)d.out_features; p.K = (int32_t)d.in_features;
   p.groups = d.groups; p.act = d.activation;
   p.vec = d.y_row % v == 0 && !misaligned(y, 16) && !misaligned(residual, 16) && !misaligned(pre, 16);
-  return launched(launch_product(kForward, d.dtype, plan, aligned, p, (hipStream_t)hip_stream));
+  return launched(launch_product(kForward, d.dtype, plan, access, p, (hipStream_t)hip_stream));
 }
 
 stripe_status_t linear_backward(stripe_linear_t* lin, const void* dy, const void* x, const void* w, const void* pre, const int32_t* offsets, void* dx, void* dw,
@@ -182,8 +186,9 @@ stripe_status_t linear_backward(stripe_linear_t* lin, const void* dy, const void
   const int64_t e = elem_size(d.dtype), v = 16 / e;
   if (misaligned(dy, e) || misaligned(x, e) || misaligned(w, e) || misaligned(pre, e) || misaligned(dx, e) || misaligned(dw, e) || misaligned(dbias, 4))
     return api_fail(STRIPE_ERR_MISALIGNED, "a buffer is not aligned to its element type");
-  const bool aligned_x = lin->wide && !misaligned(x, 16) && (act || !misaligned(dy, 16)), aligned_w = lin->wide && !misaligned(w, 16) && (act || !misaligned(dy, 16));
-  const ProductPlan &in_plan = lin->plan[aligned_w][kInputGrad], &w_plan = lin->plan[aligned_x][kWeightGrad];
+  const bool dy_off = !act && misaligned(dy, 16);
+  const Access w_access = dy_off || misaligned(w, 16) ? lin->otherwise : lin->best, x_access = dy_off || misaligned(x, 16) ? lin->otherwise : lin->best;
+  const ProductPlan &in_plan = lin->plan[w_access][kInputGrad], &w_plan = lin->plan[x_access][kWeightGrad];
   const int64_t slots = dz_slots(d.rows, d.groups);
   const bool need_dz = act && (dx || dw);
   unsigned char* ws = nullptr;
@@ -209,14 +214,14 @@ stripe_status_t linear_backward(stripe_linear_t* lin, const void* dy, const void
     p.c = dx; p.c_ld = d.x_row;
     p.M = (int32_t)d.rows; p.N = (int32_t)d.in_features; p.K = (int32_t)d.out_features;
     p.vec = d.x_row % v == 0 && !misaligned(dx, 16);
-    if (const stripe_status_t st = launched(launch_product(kInputGrad, d.dtype, in_plan, aligned_w, p, stream)); st != STRIPE_OK) return st;
+    if (const stripe_status_t st = launched(launch_product(kInputGrad, d.dtype, in_plan, w_access, p, stream)); st != STRIPE_OK) return st;
   }
   if (dw) {
     p.b = x; p.b_ld = d.x_row; p.b_group = 0;
     p.c = dw; p.c_ld = d.w_row; p.c_group = d.w_group;
     p.M = (int32_t)d.out_features; p.N = (int32_t)d.in_features; p.K = (int32_t)d.rows;
     p.vec = d.w_row % v == 0 && (!d.groups || d.w_group % v == 0) && !misaligned(dw, 16);
-    if (const stripe_status_t st = launched(launch_product(kWeightGrad, d.dtype, w_plan, aligned_x, p, stream)); st != STRIPE_OK) return st;
+    if (const stripe_status_t st = launched(launch_product(kWeightGrad, d.dtype, w_plan, x_access, p, stream)); st != STRIPE_OK) return st;
   }
   return STRIPE_OK;
 }
@@ -316,7 +321,7 @@ stripe_status_t stripe_linear_query(const stripe_linear_t* lin, stripe_linear_in
     std::memset(info, 0, sizeof *info);
     char* names[3] = {info->forward, info->input_grad, info->weight_grad};
     for (int k = 0; k < 3; ++k)
-      std::snprintf(names[k], sizeof info->forward, "%s", product_name((ProductKind)k, lin->d.dtype, lin->plan[lin->wide][k], lin->wide).c_str());
+      std::snprintf(names[k], sizeof info->forward, "%s", product_name((ProductKind)k, lin->d.dtype, lin->plan[lin->best][k], lin->best).c_str());
     info->workspace_bytes = lin->ws_bytes();
     return STRIPE_OK;
   });

@@ -64,10 +64,12 @@ struct ProductPlan {
   int few = 0;              // kForward: the kernel for few rows, 16 times as many at a time (product_rows.hip)
   int64_t ws_bytes = 0;     // partial images
 };
-ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, bool aligned);
-std::string product_name(ProductKind kind, int dtype, const ProductPlan& plan, bool aligned);
-// aligned: operands and strides allow 16-byte fetches, the contiguous extents are whole 16-byte pieces
-hipError_t launch_product(ProductKind kind, int dtype, const ProductPlan& plan, bool aligned, ProductParams p, hipStream_t stream);
+// How a product's operands can be fetched: element by element at their rims; in whole 16-byte pieces (addresses, strides and contiguous extents are
+// multiples of them); in 4-byte words (fp32).  The latter two also want a tile's rows to span less than 2^31 bytes.
+enum Access { kAny = 0, kPieces = 1, kWords = 2 };
+ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, Access access);
+std::string product_name(ProductKind kind, int dtype, const ProductPlan& plan, Access access);
+hipError_t launch_product(ProductKind kind, int dtype, const ProductPlan& plan, Access access, ProductParams p, hipStream_t stream);
 
 hipError_t launch_product_rows(int dtype, int fm, ProductParams p, hipStream_t stream);
 

@@ -1,8 +1,8 @@
 // Products of the linear layer on the gfx950 matrix cores, dense or with rows sorted by group (see ProductKind for the three
 // layouts).
 //
-// A workgroup of four wavefronts (2 x 2) computes a tile of BM x BN outputs, in 16 x 16 fragments (32 x 32 ones do as many operations per cycle, but
-// draw more power for each: the chip's clock gives way, 4096^3 bf16 on N(0,1) 113 us where 16 x 16 take 9x).  K tiles are 128 bytes deep (64 bf16
+// A workgroup of four or eight wavefronts (2 x 2, 2 x 4) computes a tile of BM x BN outputs, in 16 x 16 fragments (32 x 32 ones do as many operations
+// per cycle, but draw more power for each: the chip's clock gives way, 4096^3 bf16 on N(0,1) 113 us where 16 x 16 take 99).  K tiles are 128 bytes deep (64 bf16
 // or 32 fp32: whole cache lines of a row, where halves of them cost the L2 as much) and lie in a ring of LDS stages:
 //   an operand whose reduction index is contiguous in memory ([row][k]): 128 bytes per row, 16-byte piece c of row r in slot
 //   c ^ ((r >> 1) & 7); a fragment is one 16-byte read;
@@ -40,12 +40,17 @@ __device__ __forceinline__ void mma_row(u32x4 a, const u32x4 (&b)[C], f32x4 (&c)
   }
 }
 
-// A wavefront's LDS-direct load: lane i's 16 bytes from offset `from` of the buffer land at lds_off + 16 i; beyond the buffer: zeros.  Written as
-// assembly because the compiler, which cannot tell a load into one ring stage from fragment reads of another, would wait for all of them
+// A wavefront's LDS-direct load: lane i's PIECE bytes from offset `from` of the buffer land at lds_off + PIECE i; beyond the buffer: zeros.  Written
+// as assembly because the compiler, which cannot tell a load into one ring stage from fragment reads of another, would wait for all of them
 // before every LDS read; the kernels wait by count.  M0 is written here and nowhere else (no register array is indexed dynamically,
 // nothing else reads M0).
+template <int PIECE>
 __device__ __forceinline__ void load_to_lds(u32x4 buffer, unsigned from, unsigned lds_off) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(from), "s"(buffer), "s"(lds_off) : "memory", "m0");
+  static_assert(PIECE == 16 || PIECE == 4, "what a lane can load into LDS");
+  if constexpr (PIECE == 16)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(from), "s"(buffer), "s"(lds_off) : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" : : "v"(from), "s"(buffer), "s"(lds_off) : "memory", "m0");
 }
 template <int N>
 __device__ __forceinline__ void wait_loads() {      // until at most N of the wavefront's loads are outstanding
@@ -228,25 +233,31 @@ struct Split : Operand<__bf16, WIDTH, STRIDED> {
   }
 };
 
-// The same in whole 16-byte pieces, as LDS-direct loads of consecutive K tiles.  The buffer's base moves from K tile to K tile (scalar additions); a
+// The same as LDS-direct loads of consecutive K tiles, PIECE bytes per lane: 16, which wants operands in whole pieces, or 4 -- four times as many loads, which
+// fp32's long matrix instructions hide -- for fp32 at any address.  The buffer's base moves from K tile to K tile (scalar additions); a
 // lane's offsets within it stay, 32 bits each (the host has checked that a tile's rows span less than 2^31 bytes).
-template <typename T, int WIDTH, bool STRIDED, int WAVES>
+template <typename T, int WIDTH, bool STRIDED, int WAVES, int PIECE>
 struct Stream : Operand<T, WIDTH, STRIDED, WAVES> {
   using Operand<T, WIDTH, STRIDED, WAVES>::VEC;
   using Operand<T, WIDTH, STRIDED, WAVES>::DEPTH;
   using Operand<T, WIDTH, STRIDED, WAVES>::ROW;
-  using Operand<T, WIDTH, STRIDED, WAVES>::LOADS;
   using Operand<T, WIDTH, STRIDED, WAVES>::key;
+  static constexpr int LOADS = Operand<T, WIDTH, STRIDED, WAVES>::LOADS * 16 / PIECE, BLOCK = 64 * PIECE;      // bytes of a wavefront's load
   uint64_t base, step;            // of the next K tile, bytes to the one after it
   uint32_t from[LOADS];
 
+  // row of the LDS image that load u of this lane goes to, and its first element there
+  static __device__ __forceinline__ void place(int u, int* r, int* e) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = (u * WAVES + wave) * BLOCK + lane * PIECE;
+    *r = at / ROW;
+    *e = ((at % ROW / 16) ^ key(*r)) * VEC + at % 16 / (int)sizeof(T);
+  }
   __device__ __forceinline__ void init(const T* at0, int rows, int, int64_t ld) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int u = 0; u < LOADS; ++u) {
-      const int at = (u * WAVES + wave) * 1024 + lane * 16, r = at / ROW, piece = (at % ROW / 16) ^ key(r);
-      const bool in = STRIDED ? piece * VEC < rows : r < rows;
-      from[u] = in ? (uint32_t)(r * (uint32_t)ld + piece * VEC) * (uint32_t)sizeof(T) : kOutside;
+      int r, e;
+      place(u, &r, &e);
+      from[u] = (STRIDED ? e : r) < rows ? (uint32_t)(r * (uint32_t)ld + e) * (uint32_t)sizeof(T) : kOutside;
     }
     const uint64_t b = (uint64_t)(uintptr_t)at0;
     base = (uint64_t)__builtin_amdgcn_readfirstlane((int)(b >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)b);
@@ -254,13 +265,13 @@ struct Stream : Operand<T, WIDTH, STRIDED, WAVES> {
   }
   // From here on only `left` (< DEPTH) of a K tile's depth exist: the reduction's last tile, or none of those behind it.
   __device__ __forceinline__ void cut(int u, int left) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int at = (u * WAVES + wave) * 1024 + lane * 16, r = at / ROW, piece = (at % ROW / 16) ^ key(r);
-    if ((STRIDED ? r : piece * VEC) >= left) from[u] = kOutside;
+    int r, e;
+    place(u, &r, &e);
+    if ((STRIDED ? r : e) >= left) from[u] = kOutside;
   }
   __device__ __forceinline__ void load(int u, unsigned stage) const {
     const u32x4 buffer = {(uint32_t)base, (uint32_t)(base >> 32), kRecords, 0x00020000u};
-    load_to_lds(buffer, from[u], stage + u * (1024 * WAVES));
+    load_to_lds<PIECE>(buffer, from[u], stage + u * (BLOCK * WAVES));
   }
 };
 
@@ -385,22 +396,25 @@ __device__ __forceinline__ void finish(const ProductParams& p, int64_t at, int n
 }
 
 // B's fragments are the matrix instruction's first operand, so that a lane holds four neighbouring columns of a row: 4 (l >> 4) .. + 3 of row l & 15.
-// A wavefront lays 64 of its columns at a time into a part of the idle ring, 256 bytes per row, 16-byte pieces swizzled by the row, and
-// takes them out again eight neighbouring columns per lane, eight rows at a time: 128 contiguous bytes of a bf16 row.  A loop and not
-// 256 copies of the epilogue: the residual's loads of four turns are on their way together, two sets of them.
+// A wavefront lays 64 (or its 32) columns at a time into a part of the idle ring, 16-byte pieces swizzled by the row, and takes them out again
+// eight neighbouring columns per lane, eight (16) rows at a time: 128 contiguous bytes of a bf16 row.  A loop and not 256 copies of the
+// epilogue: the residual's loads of four turns are on their way together, two sets of them.
 template <typename T, int KIND, int FM, int C, int WAVES>
 __device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t, unsigned char* lds, const f32x4 (&acc)[2 * FM][C]) {
-  constexpr int PARTS = WAVES / 4, ROWS = FM * 32 / PARTS;      // a wavefront's rows at a time
-  static_assert(C % 4 == 0 && ROWS % 32 == 0, "64 columns, four turns of eight rows");
+  constexpr int PARTS = WAVES / 4, ROWS = FM * 32 / PARTS;                     // a wavefront's rows at a time
+  constexpr int COLS = C >= 4 ? 64 : 32, LANES = COLS / 8, HIGH = 64 / LANES;  // lanes to a row, rows of a turn
+  constexpr int TURNS = ROWS / HIGH, SET = TURNS < 4 ? TURNS : 4;
+  static_assert(C * 16 % COLS == 0 && TURNS % SET == 0, "whole turns");
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / (WAVES / 2), wn = wave % (WAVES / 2);
-  unsigned char* buf = lds + wave * (ROWS * 256);
-  const int fr = lane & 15, fq = lane >> 4, sp = lane >> 3, sc = lane & 7;
+  unsigned char* buf = lds + wave * (ROWS * COLS * 4);
+  const int fr = lane & 15, fq = lane >> 4, sp = lane / LANES, sc = lane % LANES;
   const int64_t image = KIND == kWeightGrad ? (int64_t)t.group * p.M : 0;
   const int64_t images = KIND == kWeightGrad && p.groups ? (int64_t)p.groups * p.M : p.M;
   const int64_t base = (KIND == kWeightGrad ? t.group * p.c_group : 0) + (int64_t)t.m0 * p.c_ld;
+  auto key = [](int row) { return COLS == 64 ? row & 15 : (row >> 1) & 7; };
 #pragma unroll
-  for (int jp = 0; jp < C / 4; ++jp) {
-    const int col = t.n0 + (wn * C + 4 * jp) * 16 + 8 * sc, n = p.N - col;
+  for (int jp = 0; jp < C * 16 / COLS; ++jp) {
+    const int col = t.n0 + wn * C * 16 + jp * COLS + 8 * sc, n = p.N - col;
     float bias[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) bias[e] = 0.f;
@@ -411,14 +425,14 @@ __device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t
         for (int e = 0; e < 8; ++e)
           if (e < n) bias[e] = p.bias[(int64_t)t.group * p.N + col + e];
       }
-    auto load = [&](Eight<T> (&r)[4], int first) {      // the residual of four turns of eight rows, from the wavefront's row `first` on
+    auto load = [&](Eight<T> (&r)[SET], int first) {      // the residual of a set of turns, from the wavefront's row `first` on
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int row = wm * FM * 32 + first + q * 8 + sp;
+      for (int q = 0; q < SET; ++q) {
+        const int row = wm * FM * 32 + first + q * HIGH + sp;
         if (residual && row < t.m && n > 0) r[q].load((const T*)p.residual + base + (int64_t)row * p.c_ld + col, n, p.vec && n >= 8);
       }
     };
-    Eight<T> now[4], ahead[4];
+    Eight<T> now[SET], ahead[SET];
     load(now, 0);
     if (jp == 0) __syncthreads();      // every wavefront is done with the ring
 #pragma unroll
@@ -426,19 +440,20 @@ __device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t
 #pragma unroll
       for (int i = 0; i < ROWS / 16; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) *(f32x4*)(buf + (16 * i + fr) * 256 + (((4 * j + fq) ^ fr) << 4)) = acc[part * (ROWS / 16) + i][4 * jp + j];
+        for (int j = 0; j < COLS / 16; ++j)
+          *(f32x4*)(buf + (16 * i + fr) * (COLS * 4) + (((4 * j + fq) ^ key(fr)) << 4)) = acc[part * (ROWS / 16) + i][jp * (COLS / 16) + j];
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-      for (int turn = 0; turn < ROWS / 8; turn += 4) {
-        const int first = part * ROWS + turn * 8;
-        if (first + 32 < FM * 32) load(ahead, first + 32);
+      for (int turn = 0; turn < TURNS; turn += SET) {
+        const int first = part * ROWS + turn * HIGH;
+        if (first + SET * HIGH < FM * 32) load(ahead, first + SET * HIGH);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int local = (turn + q) * 8 + sp, row = wm * FM * 32 + part * ROWS + local;
+        for (int q = 0; q < SET; ++q) {
+          const int local = (turn + q) * HIGH + sp, row = wm * FM * 32 + part * ROWS + local;
           float v[8];
-          *(f32x4*)v = *(const f32x4*)(buf + local * 256 + (((2 * sc) ^ (local & 15)) << 4));
-          *(f32x4*)(v + 4) = *(const f32x4*)(buf + local * 256 + (((2 * sc + 1) ^ (local & 15)) << 4));
+          *(f32x4*)v = *(const f32x4*)(buf + local * (COLS * 4) + (((2 * sc) ^ key(local)) << 4));
+          *(f32x4*)(v + 4) = *(const f32x4*)(buf + local * (COLS * 4) + (((2 * sc + 1) ^ key(local)) << 4));
           if (row < t.m && n > 0) {
             if (p.splits > 1) {
               Eight<float> out;
@@ -450,7 +465,7 @@ __device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t
           }
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) now[q] = ahead[q];
+        for (int q = 0; q < SET; ++q) now[q] = ahead[q];
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
@@ -643,11 +658,11 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductParams p) 
 // Behind the last tile the loop loads zeros and reads fragments that nobody uses: the counts then never change.
 #define PRODUCT_FENCE() __builtin_amdgcn_sched_barrier(0)
 
-template <typename T, int KIND, int FM, int FN, int S, int WAVES>
+template <typename T, int KIND, int FM, int FN, int S, int WAVES, int PIECE>
 __global__ __launch_bounds__(64 * WAVES, S * 64 * (FM + FN) * kDepthBytes > 80 * 1024 ? 1 : 2) void product_stream_kernel(const ProductParams p) {
   constexpr int BM = 64 * FM, BN = 64 * FN, R = 2 * FM, C = 8 * FN / WAVES;      // fragments of a wavefront
-  using A = Stream<T, BM, KIND == kWeightGrad, WAVES>;
-  using B = Stream<T, BN, KIND != kForward, WAVES>;
+  using A = Stream<T, BM, KIND == kWeightGrad, WAVES, PIECE>;
+  using B = Stream<T, BN, KIND != kForward, WAVES, PIECE>;
   constexpr int LOADS = A::LOADS + B::LOADS, HALF = R / 2;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   unsigned char *const lds_a = lds, *const lds_b = lds + S * A::STAGE;
@@ -670,7 +685,7 @@ __global__ __launch_bounds__(64 * WAVES, S * 64 * (FM + FN) * kDepthBytes > 80 *
     int left = (kt1 * A::DEPTH < t.k ? kt1 * A::DEPTH : t.k) - kt0 * A::DEPTH;      // of this workgroup's part of the reduction, from the next tile on
     a.base += (uint64_t)kt0 * a.step;
     b.base += (uint64_t)kt0 * b.step;
-    const unsigned own = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) * 1024;
+    const unsigned own = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) * A::BLOCK;
     auto load = [&](int first, int last, int stage) {
 #pragma unroll
       for (int u = 0; u < LOADS; ++u)
@@ -895,11 +910,13 @@ __global__ __launch_bounds__(256) void db_kernel(const DzParams p, int strips) {
 struct TileShape {
   int fm, fn, stages, resident, waves;      // resident: workgroups that fit a CU
 };
-// What each is for, bf16: 0 many outputs (4096^3: 100 us, 112 and 150 on the others); 1 half as many, or groups of a few hundred rows (8192 rows of 32
-// groups, 2048 -> 4096: 216, 199, 274; 2048 x 4096 x 4096: 83, 57, 76); 2 few of them, and fp32, whose matrix instructions take so long that nothing
-// else matters.  Operands that are no whole 16-byte pieces run on product_kernel in tile 2's shape.
-constexpr TileShape kTiles[] = {{4, 4, 2, 1, 8}, {2, 4, 3, 1, 8}, {1, 2, 3, 2, 4}};
-constexpr int kTileCount = 3, kSmallTile = 2;
+// What each is for, bf16: 0 many outputs (4096^3: 100 us, 112 and 150 on the next two); 1 half as many, or groups of a few hundred rows (8192 rows of
+// 32 groups, 2048 -> 4096: 216, 199, 274; 2048 x 4096 x 4096: 83, 57, 76); 2 few of them, and fp32, whose matrix instructions take so long that
+// nothing else matters; 3 so few that tile 2's would leave CUs idle (1024^3: 8.5 us on tile 2, 6.9; fp32 1000^3: 27.3 and 21.5; 777 rows of 5
+// groups, 200 -> 328, fp32: 12.0 and 8.2).  Operands that are no whole 16-byte pieces: fp32 loads words into LDS instead (1000 x 777 x 1283: 31 us
+// and 32 through the registers; 333 x 555 x 777: 12.7 and 15.0), bf16 runs on product_kernel in tile 2's shape.
+constexpr TileShape kTiles[] = {{4, 4, 2, 1, 8}, {2, 4, 3, 1, 8}, {1, 2, 3, 2, 4}, {1, 1, 4, 2, 4}};
+constexpr int kTileCount = 4, kSmallTile = 2, kLeastTile = 3;
 
 // Estimated times, in us: of a K tile where workgroups are alone on their CU and few on the chip; where they fill it; the same of what else
 // a workgroup does.
@@ -908,10 +925,10 @@ struct TileTime {
 };
 // parts: fp32 split into three bf16 parts, which is faster where the matrix instructions are what a CU waits for (2048^3: 124 us with fp32
 // instructions, 106), and slower where it is the way through the registers (512^3: 12.4 and 14.2).
-TileTime tile_time(int tile, int dtype, bool aligned, bool parts) {
-  if (dtype == STRIPE_F32) return parts ? TileTime{0.95, 1.55, 5, 7} : TileTime{1.0, 1.95, 3, 5};
-  if (!aligned) return {0.75, 1.1, 3, 5};
-  constexpr TileTime t[] = {{1.1, 1.45, 6, 9}, {0.56, 0.76, 4, 5}, {0.28, 0.5, 3, 5}};
+TileTime tile_time(int tile, int dtype, Access access, bool parts) {
+  if (dtype == STRIPE_F32) return parts ? TileTime{0.95, 1.55, 5, 7} : tile == kLeastTile ? TileTime{0.55, 1.0, 2, 4} : TileTime{1.0, 1.95, 3, 5};
+  if (access != kPieces) return {0.75, 1.1, 3, 5};
+  constexpr TileTime t[] = {{1.1, 1.45, 6, 9}, {0.56, 0.76, 4, 5}, {0.28, 0.5, 3, 5}, {0.22, 0.35, 2, 4}};
   return t[tile];
 }
 
@@ -927,20 +944,20 @@ hipError_t allow_lds(K kernel, int bytes, std::atomic<uint64_t>& done) {
   return e;
 }
 
-template <typename T, int KIND, int TILE>
+template <typename T, int KIND, int TILE, int PIECE = 16>
 hipError_t launch_stream(const ProductParams& p, dim3 grid, hipStream_t stream) {
   constexpr TileShape s = kTiles[TILE];
   constexpr int bytes = s.stages * 64 * (s.fm + s.fn) * kDepthBytes;
   if constexpr (bytes > 65536) {
     static std::atomic<uint64_t> done{0};
-    if (const hipError_t e = allow_lds(product_stream_kernel<T, KIND, s.fm, s.fn, s.stages, s.waves>, bytes, done); e != hipSuccess) return e;
+    if (const hipError_t e = allow_lds(product_stream_kernel<T, KIND, s.fm, s.fn, s.stages, s.waves, PIECE>, bytes, done); e != hipSuccess) return e;
   }
-  product_stream_kernel<T, KIND, s.fm, s.fn, s.stages, s.waves><<<grid, dim3(64 * s.waves), bytes, stream>>>(p);
+  product_stream_kernel<T, KIND, s.fm, s.fn, s.stages, s.waves, PIECE><<<grid, dim3(64 * s.waves), bytes, stream>>>(p);
   return hipGetLastError();
 }
 
 template <typename T, int KIND>
-hipError_t launch_kind(const ProductPlan& plan, bool aligned, ProductParams& p, hipStream_t stream) {
+hipError_t launch_kind(const ProductPlan& plan, Access access, ProductParams& p, hipStream_t stream) {
   const TileShape s = kTiles[plan.tile];
   const int bm = 64 * s.fm, bn = 64 * s.fn;
   p.tiles_n = (p.N + bn - 1) / bn;
@@ -954,11 +971,12 @@ hipError_t launch_kind(const ProductPlan& plan, bool aligned, ProductParams& p, 
   }
   const dim3 grid((unsigned)((total + 7) / 8 * 8), (unsigned)plan.splits);
   hipError_t e = hipSuccess;
-  if (aligned && !plan.parts) {
-    if constexpr (sizeof(T) == 4)
-      e = launch_stream<T, KIND, kSmallTile>(p, grid, stream);
-    else
-      e = plan.tile == 0 ? launch_stream<T, KIND, 0>(p, grid, stream) : plan.tile == 1 ? launch_stream<T, KIND, 1>(p, grid, stream) : launch_stream<T, KIND, 2>(p, grid, stream);
+  if (access == kWords && !plan.parts) {
+    if constexpr (sizeof(T) == 4) e = plan.tile == kLeastTile ? launch_stream<T, KIND, kLeastTile, 4>(p, grid, stream) : launch_stream<T, KIND, kSmallTile, 4>(p, grid, stream);
+  } else if (access == kPieces && !plan.parts) {
+    if (plan.tile == kLeastTile) e = launch_stream<T, KIND, kLeastTile>(p, grid, stream);
+    else if (sizeof(T) == 4 || plan.tile == kSmallTile) e = launch_stream<T, KIND, kSmallTile>(p, grid, stream);
+    else if constexpr (sizeof(T) == 2) e = plan.tile == 0 ? launch_stream<T, KIND, 0>(p, grid, stream) : launch_stream<T, KIND, 1>(p, grid, stream);
   } else {
     constexpr TileShape s = kTiles[kSmallTile];
     constexpr int bytes = 2 * 64 * (s.fm + s.fn) * (sizeof(T) == 4 ? 3 * 64 : kDepthBytes);
@@ -977,11 +995,11 @@ hipError_t launch_kind(const ProductPlan& plan, bool aligned, ProductParams& p, 
 }
 
 template <typename T>
-hipError_t launch_type(ProductKind kind, const ProductPlan& plan, bool aligned, ProductParams& p, hipStream_t stream) {
+hipError_t launch_type(ProductKind kind, const ProductPlan& plan, Access access, ProductParams& p, hipStream_t stream) {
   switch (kind) {
-    case kForward: return launch_kind<T, kForward>(plan, aligned, p, stream);
-    case kInputGrad: return launch_kind<T, kInputGrad>(plan, aligned, p, stream);
-    default: return launch_kind<T, kWeightGrad>(plan, aligned, p, stream);
+    case kForward: return launch_kind<T, kForward>(plan, access, p, stream);
+    case kInputGrad: return launch_kind<T, kInputGrad>(plan, access, p, stream);
+    default: return launch_kind<T, kWeightGrad>(plan, access, p, stream);
   }
 }
 
@@ -989,7 +1007,7 @@ hipError_t launch_type(ProductKind kind, const ProductPlan& plan, bool aligned, 
 
 // The tile and the slices of the reduction with the smallest estimated time: the workgroups of the CU that has most of them one after the other,
 // or in pairs where two fit.
-ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, bool aligned) {
+ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, Access access) {
   ProductPlan plan;
   plan.tile = kSmallTile;
   // few rows (of a group, on average): W is read once, whatever is computed with it.  4096 x 4096 bf16: 1 row 8.4 us, 16 10.5, 32 13.8 where 128 x 128
@@ -1003,15 +1021,14 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
   const int64_t k_tiles = std::max<int64_t>(1, (int64_t)std::ceil(depth_of / (double)depth));
   double best = __builtin_huge_val();
   const int forced_tile = tune_int("product_tile", -1), forced_splits = tune_int("product_splits", 0);
-  // fp32: the small tile, with fp32 instructions (whole pieces only) or in parts
   const bool f32 = dtype == STRIPE_F32;
   for (int variant = 0; variant < kTileCount; ++variant) {
+    // loads into LDS: bf16 any tile, fp32 the small ones; the kernel for any alignment has the small one's shape, for fp32 in parts (variant 1)
     const bool parts = f32 && variant == 1;
-    const int tile = f32 ? kSmallTile : variant;
-    if (f32 ? variant == 2 || (!aligned && !parts) || (aligned && forced_tile >= 0 && forced_tile != variant)
-            : (!aligned && tile != kSmallTile) || (aligned && forced_tile >= 0 && tile != forced_tile)) continue;
+    const int tile = parts ? kSmallTile : variant;
+    if (access == kAny ? (f32 ? !parts : tile != kSmallTile) : (f32 && variant == 0) || (forced_tile >= 0 && forced_tile != variant)) continue;
     const TileShape s = kTiles[tile];
-    const TileTime t = tile_time(tile, dtype, aligned, parts);
+    const TileTime t = tile_time(tile, dtype, access, parts);
     const int64_t bm = 64 * s.fm, bn = 64 * s.fn;
     const double row_tiles = kind == kWeightGrad ? (double)((m + bm - 1) / bm * images)
                              : groups            ? (double)m / (double)bm + 0.5 * std::min<double>(groups, (double)m)
@@ -1026,7 +1043,8 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
       double us = 4;
       if (s.resident == 1) us += most * (kt * (t.k_few + (t.k_full - t.k_few) * full) + t.store_few + (t.store_full - t.store_few) * full);
       else us += std::floor(most / 2) * (kt * t.k_full + t.store_full) + std::fmod(most, 2) * (kt * t.k_few + t.store_few);
-      if (splits > 1) us += 2.0 + (double)bytes * 2.5 / 4e6;
+      // the join: a launch, and its bytes written and read (300^3 fp32: 8.9 us in one piece, 9.6 in the five that would win without the launch)
+      if (splits > 1) us += 3.5 + (double)bytes * 2.5 / 4e6;
       if (us < best) {
         best = us;
         plan.tile = tile;
@@ -1039,17 +1057,17 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
   return plan;
 }
 
-std::string product_name(ProductKind kind, int dtype, const ProductPlan& plan, bool aligned) {
+std::string product_name(ProductKind kind, int dtype, const ProductPlan& plan, Access access) {
   if (plan.few) return std::string("product_rows_") + (dtype == STRIPE_F32 ? "f32_" : "bf16_") + std::to_string(16 * plan.few) + "x16";
   const TileShape s = kTiles[plan.tile];
-  return std::string(aligned && !plan.parts ? "product_stream_" : "product_") + (kind == kForward ? "nt_" : kind == kInputGrad ? "nn_" : "tn_") + (dtype == STRIPE_F32 ? "f32_" : "bf16_") +
-         std::to_string(64 * s.fm) + "x" + std::to_string(64 * s.fn) + (plan.parts ? "_parts" : aligned ? "_s" + std::to_string(s.stages) : "") +
+  return std::string(access != kAny && !plan.parts ? "product_stream_" : "product_") + (kind == kForward ? "nt_" : kind == kInputGrad ? "nn_" : "tn_") + (dtype == STRIPE_F32 ? "f32_" : "bf16_") +
+         std::to_string(64 * s.fm) + "x" + std::to_string(64 * s.fn) + (plan.parts ? "_parts" : access != kAny ? "_s" + std::to_string(s.stages) : "") + (access == kWords && !plan.parts ? "_words" : "") +
          (plan.splits > 1 ? "_k" + std::to_string(plan.splits) : "");
 }
 
-hipError_t launch_product(ProductKind kind, int dtype, const ProductPlan& plan, bool aligned, ProductParams p, hipStream_t stream) {
+hipError_t launch_product(ProductKind kind, int dtype, const ProductPlan& plan, Access access, ProductParams p, hipStream_t stream) {
   if (plan.few) return launch_product_rows(dtype, plan.few, p, stream);
-  return dtype == STRIPE_F32 ? launch_type<float>(kind, plan, aligned, p, stream) : launch_type<__bf16>(kind, plan, aligned, p, stream);
+  return dtype == STRIPE_F32 ? launch_type<float>(kind, plan, access, p, stream) : launch_type<__bf16>(kind, plan, access, p, stream);
 }
 
 // (one more with groups: a single empty group's zeros come from db_kernel)
