@@ -495,9 +495,11 @@ __device__ __forceinline__ void own_k_tiles(const ProductParams& p, int all, int
   }
 }
 
-// Operands at any alignment, and fp32: through registers, two stages, two K tiles ahead.
-// fp32 sums that end as NaN -- an operand was infinite, NaN or within half a bf16 step of overflow, which leave no finite remainder, or the sum itself
-// met opposite infinities -- are not what fp32 arithmetic gives; their workgroup computes its tile again with fp32 instructions.
+// Operands at any alignment, and fp32 in parts: through registers, two stages, two K tiles ahead.  (Parts from an LDS ring of fp32 tiles, split by every
+// wavefront that reads them, are twice the splitting: 4096^3 850 us, 800 here.)
+// fp32 sums that do not end finite -- an operand was infinite, NaN or within half a bf16 step of overflow, which leave no finite remainder, or a sum came so
+// near to overflow that hi hi went beyond it -- are not what fp32 arithmetic gives; their workgroup computes its tile again with fp32
+// instructions.
 template <typename T, int KIND, int FM, int FN>
 __global__ __launch_bounds__(256, 2) void product_kernel(const ProductParams p) {
   constexpr int BM = 64 * FM, BN = 64 * FN, R = 2 * FM, C = 2 * FN;      // fragments of a wavefront
@@ -599,7 +601,7 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductParams p) 
 #pragma unroll
       for (int j = 0; j < C; ++j)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) native = native || acc[i][j][v] != acc[i][j][v];
+        for (int v = 0; v < 4; ++v) native = native || !(__builtin_fabsf(acc[i][j][v]) < __builtin_inff());
     native = __syncthreads_or(native);
     if (native) {
 #pragma unroll
@@ -609,41 +611,41 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductParams p) 
     }
   }
   if (native) {
-  const unsigned first_a = A::first(wm * R * 16), first_b = B::first(wn * C * 16);
-  auto tile = [&](auto all, int kt, u32x4 (&na)[A::LOADS], u32x4 (&nb)[B::LOADS], int stage) {
-    constexpr bool WHOLE = decltype(all)::value;
-    a.shift(na);
-    b.shift(nb);
-    A::put(lds_a + stage * A::STAGE, na);
-    B::put(lds_b + stage * B::STAGE, nb);
-    __syncthreads();
-    a.template fetch<WHOLE>(na, kt + 2, t.k);
-    b.template fetch<WHOLE>(nb, kt + 2, t.k);
+    const unsigned first_a = A::first(wm * R * 16), first_b = B::first(wn * C * 16);
+    auto tile = [&](auto all, int kt, u32x4 (&na)[A::LOADS], u32x4 (&nb)[B::LOADS], int stage) {
+      constexpr bool WHOLE = decltype(all)::value;
+      a.shift(na);
+      b.shift(nb);
+      A::put(lds_a + stage * A::STAGE, na);
+      B::put(lds_b + stage * B::STAGE, nb);
+      __syncthreads();
+      a.template fetch<WHOLE>(na, kt + 2, t.k);
+      b.template fetch<WHOLE>(nb, kt + 2, t.k);
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      u32x4 fa[R], fb[C];
+      for (int s = 0; s < 2; ++s) {
+        u32x4 fa[R], fb[C];
 #pragma unroll
-      for (int i = 0; i < R; ++i) fa[i] = A::fragment(lds_a + stage * A::STAGE, first_a, i, s);
+        for (int i = 0; i < R; ++i) fa[i] = A::fragment(lds_a + stage * A::STAGE, first_a, i, s);
 #pragma unroll
-      for (int j = 0; j < C; ++j) fb[j] = B::fragment(lds_b + stage * B::STAGE, first_b, j, s);
+        for (int j = 0; j < C; ++j) fb[j] = B::fragment(lds_b + stage * B::STAGE, first_b, j, s);
 #pragma unroll
-      for (int i = 0; i < R; ++i) mma_row<T, C>(fa[i], fb, acc[i]);
+        for (int i = 0; i < R; ++i) mma_row<T, C>(fa[i], fb, acc[i]);
+      }
+    };
+    if (sizeof(T) == 4) __syncthreads();      // the parts' stages were read
+    a.template fetch<false>(ra[0], kt0, t.k);
+    b.template fetch<false>(rb[0], kt0, t.k);
+    a.template fetch<false>(ra[1], kt0 + 1, t.k);
+    b.template fetch<false>(rb[1], kt0 + 1, t.k);
+    int kt = kt0;
+    for (; kt + 1 < kt1 && a.whole(kt + 3, t.k) && b.whole(kt + 3, t.k); kt += 2) {
+      tile(std::true_type{}, kt, ra[0], rb[0], 0);
+      tile(std::true_type{}, kt + 1, ra[1], rb[1], 1);
     }
-  };
-  if (sizeof(T) == 4) __syncthreads();      // the parts' stages were read
-  a.template fetch<false>(ra[0], kt0, t.k);
-  b.template fetch<false>(rb[0], kt0, t.k);
-  a.template fetch<false>(ra[1], kt0 + 1, t.k);
-  b.template fetch<false>(rb[1], kt0 + 1, t.k);
-  int kt = kt0;
-  for (; kt + 1 < kt1 && a.whole(kt + 3, t.k) && b.whole(kt + 3, t.k); kt += 2) {
-    tile(std::true_type{}, kt, ra[0], rb[0], 0);
-    tile(std::true_type{}, kt + 1, ra[1], rb[1], 1);
-  }
-  for (; kt < kt1; kt += 2) {
-    tile(std::false_type{}, kt, ra[0], rb[0], 0);
-    if (kt + 1 < kt1) tile(std::false_type{}, kt + 1, ra[1], rb[1], 1);
-  }
+    for (; kt < kt1; kt += 2) {
+      tile(std::false_type{}, kt, ra[0], rb[0], 0);
+      if (kt + 1 < kt1) tile(std::false_type{}, kt + 1, ra[1], rb[1], 1);
+    }
   }
   store_tile<T, KIND, FM, C, 4>(p, t, lds, acc);
 }

@@ -372,6 +372,140 @@ def test_runs_on_the_current_stream_and_on_a_given_one():
     c.check(["y", "pre"])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_far_apart(dtype):
+    """Row strides beyond the 32-bit offsets of a tile's loads."""
+    c = Linear(40, 72, 136, dtype, act="gelu", pad=(1 << 20) + 8, seed=2)
+    c.forward()
+    c.backward()
+    c.check(["y", "pre", "dx", "dw", "dbias"])
+
+
+def test_f32_in_parts_with_infinities_nan_and_the_largest_values():
+    """What three bf16 parts cannot hold is computed again in fp32: every value and every neighbour as the formula has them."""
+    c = Linear(40, 72, 136, "f32", act="none", bias=False, residual=False, pad=(1 << 20) + 8, seed=4)
+    assert "parts" in c.op.info["forward"]
+    big = torch.finfo(torch.float32).max
+    c.x[3, 5], c.x[7, 0], c.x[11, 2], c.x[12, 3], c.x[13, 4] = float("inf"), NAN, big, -big, big
+    c.x[13, 6], c.x[14] = float("-inf"), 0.0
+    c.w[20, 2] = 1.0                                   # big times one is still finite
+    c.dy[9, 8], c.dy[10, 8] = big, float("-inf")
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    x, w, dy = c.x.double(), c.w.double(), c.dy.double()
+
+    def same(got, a, b):
+        v, terms = a @ b, a.abs() @ b.abs()
+        tol = (a.shape[1] + 2) * U * terms
+        tol = tol + U * (v.abs() + tol) + 1e-37
+        # Where the finite terms' sizes add up to the largest fp32 value (big times 1.5, say), fp32 sums of them overflow in some or every order and meet
+        # what infinities there are: 64 bits say nothing about such a result.
+        beyond = a.nan_to_num(0, 0, 0).abs() @ b.nan_to_num(0, 0, 0).abs() * (1 + (a.shape[1] + 2) * U) >= big
+        finite, special = torch.isfinite(v) & ~beyond, ~torch.isfinite(v) & ~beyond
+        assert (((got.double() - v).abs() <= tol) | ~finite).all()
+        assert torch.equal(torch.isnan(got)[special], torch.isnan(v)[special])
+        known = special & ~torch.isnan(v)
+        assert (got[known].double() == v[known]).all()
+        assert (finite | special).double().mean() > 0.9
+
+    same(c.outs["y"][1], x, w.t())
+    same(c.outs["dx"][1], dy, w)
+    same(c.outs["dw"][1], dy.t(), x)
+
+
+def test_many_groups_of_many_tiles():
+    sizes = [(37 * i) % 211 for i in range(75)]
+    offsets = np.concatenate([[3], 3 + np.cumsum(sizes)]).tolist()
+    for dtype in ("bf16", "f32"):
+        c = Linear(offsets[-1] + 20, 72, 200, dtype, act="silu", offsets=offsets, seed=6)
+        c.forward()
+        c.backward()
+        c.check(["y", "pre", "dx", "dw", "dbias"])
+
+
+def test_more_than_two_billion_elements():
+    """y, dz and dx beyond 2^31 elements: the last rows and columns."""
+    rows, cin, cout = 66000, 64, 32776
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x, w = (torch.randn(n, cin, generator=g, device="cuda").to(torch.bfloat16) for n in (rows, cout))
+    y, dy = (torch.empty(rows, cout, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    dy.normal_(generator=g)
+    pre, dx, dw = dy, torch.empty_like(x), torch.empty_like(w)
+    op = B.StripeLinear(rows, cin, cout, "bf16", activation="relu")
+    op.run(x, w, y)
+    op.backward(dy, x, w, pre=pre, dx=dx, dw=dw)
+    torch.cuda.synchronize()
+    for part in (slice(0, 70), slice(rows - 70, rows)):
+        z, terms = x[part].double() @ w.double().t(), x[part].double().abs() @ w.double().abs().t()
+        tol = (cin + 2) * U * terms
+        assert ((y[part].double() - z.clamp(min=0)).abs() <= tol + 2.0 ** -8 * (z.abs() + tol)).all()
+        dz = dy[part].double().clamp(min=0)
+        tol = (cout + 2) * U * (dz @ w.double().abs())
+        assert ((dx[part].double() - dz @ w.double()).abs() <= tol + 2.0 ** -8 * ((dz @ w.double()).abs() + tol)).all()
+    dz = dy[:, -9:].double().clamp(min=0)
+    v, tol = dz.t() @ x.double(), (rows + 2) * U * (dz.t() @ x.double().abs())
+    assert ((dw[-9:].double() - v).abs() <= tol + 2.0 ** -8 * (v.abs() + tol)).all()
+
+
+@pytest.mark.parametrize("rows", [3, 64])
+def test_weights_of_more_than_two_billion_elements(rows):
+    cin, cout = 65544, 32776
+    g = torch.Generator(device="cuda").manual_seed(0)
+    w = torch.empty(cout, cin, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    x, dy = (torch.randn(rows, n, generator=g, device="cuda").to(torch.bfloat16) for n in (cin, cout))
+    y, dx = torch.empty_like(dy), torch.empty_like(x)
+    op = B.StripeLinear(rows, cin, cout, "bf16")
+    op.run(x, w, y)
+    op.backward(dy, x, w, dx=dx)
+    torch.cuda.synchronize()
+    for got, a, b in ((y[:, -40:], x, w[-40:].double().t()), (dx[:, -40:], dy, w[:, -40:].double())):
+        v, tol = a.double() @ b, (a.shape[1] + 2) * U * (a.double().abs() @ b.abs())
+        assert ((got.double() - v).abs() <= tol + 2.0 ** -8 * (v.abs() + tol)).all()
+
+
+def test_two_layers_on_two_streams():
+    a, b = Linear(700, 264, 520, "bf16", act="silu", seed=1), Linear(700, 264, 520, "bf16", act="silu", seed=2)
+    a.backward()                                       # each has its own workspace from here on
+    b.backward()
+    torch.cuda.synchronize()
+    s, t = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        a.forward(stream=s.cuda_stream)
+        b.forward(stream=t.cuda_stream)
+        a.backward(stream=s.cuda_stream)
+        b.backward(stream=t.cuda_stream)
+    for c in (a, b):
+        c.check(["y", "pre", "dx", "dw", "dbias"])
+
+
+def test_two_graphs_with_workspaces_of_their_own():
+    cs = [Linear(300, 128, 136, "f32", act="gelu", seed=i) for i in range(2)]
+    graphs = []
+    for c in cs:
+        c.op.set_workspace(torch.empty(c.op.workspace_bytes, dtype=torch.uint8, device="cuda"))
+        c.backward()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+            c.forward()
+            c.backward()
+        graphs.append(graph)
+    s, t = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        for c in cs:
+            c.x.mul_(0.5)
+            for _, o in c.outs.values():
+                o.fill_(-7.0)
+        torch.cuda.synchronize()
+        for graph, stream in zip(graphs, (s, t)):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for c in cs:
+            c.check(["y", "pre", "dx", "dw", "dbias"])
+
+
 def test_wrapper_refuses_host_tensors():
     c = Linear(16, 32, 48, "bf16")
     with pytest.raises(ValueError, match="x: expected"):
@@ -565,3 +699,29 @@ def test_feed_forward_block(dtype):
     for name, (got, v) in ours.items():
         rel = (got.double() - v).norm() / v.norm()
         assert rel <= tol, f"{name}: {rel:.2e}"
+
+
+def test_norm_of_more_than_two_billion_elements():
+    rows, features = (1 << 18) + 5, 8200
+    x = torch.empty(rows, features, dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(0))
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd, dbeta = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty(features, device="cuda")
+    op = B.StripeNorm(rows, features, "bf16")
+    op.run(x, y, mean=mean, rstd=rstd)
+    op.backward(y, x, mean, rstd, dx=dx, dgamma=torch.empty(features, device="cuda"), dbeta=dbeta)
+    torch.cuda.synchronize()
+    n = 32 + 6 + 16 + 8 + 2
+    for part in (slice(0, 50), slice(rows - 50, rows)):
+        xd = x[part].double()
+        d = xd - xd.mean(1, keepdim=True)
+        s = ((d * d).mean(1, keepdim=True) + 1e-5) ** -0.5
+        # (n + 8) u relative to |d| + mean|x| bounds the statistics' share; one rounding
+        tol = (n + 8) * U * s * (d.abs() + xd.abs().mean(1, keepdim=True)) * 2
+        assert ((y[part].double() - d * s).abs() <= tol + 2.0 ** -8 * ((d * s).abs() + tol)).all()
+        # dx of dy = y = h (rounded): s (y - mean y - h mean(y h))
+        yd, h = y[part].double(), (xd - mean[part].double()[:, None]) * rstd[part].double()[:, None]
+        want = rstd[part].double()[:, None] * (yd - yd.mean(1, keepdim=True) - h * (yd * h).mean(1, keepdim=True))
+        tol = rstd[part].double()[:, None] * (n + 14) * U * (yd.abs() + yd.abs().mean(1, keepdim=True) + h.abs() * (2 + (yd * h).abs().mean(1, keepdim=True)))
+        assert ((dx[part].double() - want).abs() <= tol + 2.0 ** -8 * (want.abs() + tol)).all()
+    v = y[:, -9:].double()
+    assert ((dbeta[-9:].double() - v.sum(0)).abs() <= (rows + 2) * U * v.abs().sum(0)).all()
