@@ -300,6 +300,8 @@ stripe_status_t stripe_device_mfma(const void* operands, void* out, int iters, i
  *    strides and feature counts run faster kernels, nothing else depends on them;
  *  - sums, statistics and totals are fp32 (or wider); a bf16 result is rounded to
  *    nearest even once, on store; zeros, infinities and NaN go the way the formula sends them;
+ *  - a linear layer's fp32 products may be computed as three bf16 parts per value, which hold all
+ *    24 bits down to 2^-110; of smaller values they lose what lies below 2^-133;
  *  - outputs must not overlap inputs or one another, except where stated;
  *  - the same call on the same inputs gives the same bits (no atomics);
  *  - a call that needs a workspace and has none of the caller's allocates it, once per

@@ -110,9 +110,14 @@ stripe_status_t linear_create(const stripe_linear_desc_t* desc, stripe_linear_t*
   if (!d.y_row) d.y_row = d.out_features;
   if (d.x_row < d.in_features || d.x_row > kMaxStride || d.w_row < d.in_features || d.w_row > kMaxStride || d.y_row < d.out_features || d.y_row > kMaxStride)
     return api_fail(STRIPE_ERR_INVALID_DESC, "a row stride is shorter than its row (or beyond 2^40 elements)");
+  // (offsets within a buffer are 64-bit byte counts)
+  auto beyond = [](int64_t n, int64_t stride) { return (__int128)n * stride > (__int128)1 << 56; };
+  if (beyond(d.rows, d.x_row) || beyond(d.rows, d.y_row) || beyond(d.out_features, d.w_row))
+    return api_fail(STRIPE_ERR_INVALID_DESC, "a buffer spans more than 2^56 elements");
   const int64_t matrix = (d.out_features - 1) * d.w_row + d.in_features;
   if (!d.w_group) d.w_group = d.out_features * d.w_row;
-  if (d.groups && (d.w_group < matrix || d.w_group > kMaxStride * 4096)) return api_fail(STRIPE_ERR_INVALID_DESC, "w_group is shorter than a matrix");
+  if (d.groups && d.w_group < matrix) return api_fail(STRIPE_ERR_INVALID_DESC, "w_group is shorter than a matrix");
+  if (beyond(d.groups, d.w_group)) return api_fail(STRIPE_ERR_INVALID_DESC, "a buffer spans more than 2^56 elements");
   // a launch holds fewer than 2^32 lanes: 2^24 workgroups of 256, counted in tiles of 64 x 64 outputs, the smallest
   auto tiles = [](__int128 images, int64_t m, int64_t n) { return (images + m / 64 + 1) * (n / 64 + 1); };
   if (tiles(d.groups, d.rows, d.out_features) >= 1 << 24 || tiles(d.groups, d.rows, d.in_features) >= 1 << 24 ||
@@ -238,6 +243,7 @@ stripe_status_t norm_create(const stripe_norm_desc_t* desc, stripe_norm_t** out)
   if (!d.y_row) d.y_row = d.features;
   if (d.x_row < d.features || d.x_row > kMaxStride || d.y_row < d.features || d.y_row > kMaxStride)
     return api_fail(STRIPE_ERR_INVALID_DESC, "a row stride is shorter than its row (or beyond 2^40 elements)");
+  if ((__int128)d.rows * std::max(d.x_row, d.y_row) > (__int128)1 << 56) return api_fail(STRIPE_ERR_INVALID_DESC, "a buffer spans more than 2^56 elements");
   auto norm = std::make_unique<stripe_norm>();
   norm->d = d;
   norm->blocks = norm_backward_blocks(d.rows, d.features, d.dtype);

@@ -135,7 +135,8 @@ __device__ __forceinline__ float slope(float z, int act) {
     }
     case STRIPE_ACT_GELU_TANH: {
       const float s = inv<T>(1.f + exp_of<T>(-2.f * kGeluA * (z + kGeluB * z * z * z)));
-      return s + z * s * (1.f - s) * 2.f * kGeluA * (1.f + 3.f * kGeluB * z * z);
+      const float c = __builtin_amdgcn_fmed3f(z, -100.f, 100.f);      // beyond, s (1 - s) is 0, and z^2 may overflow
+      return s + c * s * (1.f - s) * 2.f * kGeluA * (1.f + 3.f * kGeluB * c * c);
     }
     case STRIPE_ACT_SILU: {
       const float s = inv<T>(1.f + exp_of<T>(-z));

@@ -265,40 +265,40 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const NormParams p) {
   __shared__ float shared[2][32];
   int turn = 0;
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
-  const T* x = (const T*)p.x + row * p.x_row;
-  T* y = (T*)p.y + row * p.y_row;
-  float sum = 0.f;
-  for (int c = threadIdx.x * VEC; c < p.features; c += 1024 * VEC) {
-    float f[VEC], part = 0.f;
-    unpack<T>(load_piece<T>(x + c, p.features - c), f);
+    const T* x = (const T*)p.x + row * p.x_row;
+    T* y = (T*)p.y + row * p.y_row;
+    float sum = 0.f;
+    for (int c = threadIdx.x * VEC; c < p.features; c += 1024 * VEC) {
+      float f[VEC], part = 0.f;
+      unpack<T>(load_piece<T>(x + c, p.features - c), f);
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) part += f[i];
-    sum += part;
-  }
-  const float mean = row_sum<1024>(sum, shared, turn++) / (float)p.features;
-  float sq = 0.f;
-  for (int c = threadIdx.x * VEC; c < p.features; c += 1024 * VEC) {
-    float f[VEC], part = 0.f;
-    unpack<T>(load_piece<T>(x + c, p.features - c), f);
+      for (int i = 0; i < VEC; ++i) part += f[i];
+      sum += part;
+    }
+    const float mean = row_sum<1024>(sum, shared, turn++) / (float)p.features;
+    float sq = 0.f;
+    for (int c = threadIdx.x * VEC; c < p.features; c += 1024 * VEC) {
+      float f[VEC], part = 0.f;
+      unpack<T>(load_piece<T>(x + c, p.features - c), f);
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) part += c + i < p.features ? (f[i] - mean) * (f[i] - mean) : 0.f;
-    sq += part;
-  }
-  const float rstd = 1.f / sqrtf(row_sum<1024>(sq, shared, turn++) / (float)p.features + p.eps);
-  for (int c = threadIdx.x * VEC; c < p.features; c += 1024 * VEC) {
-    const int n = p.features - c;
-    float f[VEC], g[VEC], b[VEC];
-    unpack<T>(load_piece<T>(x + c, n), f);
-    load_floats<VEC>(p.gamma ? p.gamma + c : nullptr, n, 1.f, g);
-    load_floats<VEC>(p.beta ? p.beta + c : nullptr, n, 0.f, b);
+      for (int i = 0; i < VEC; ++i) part += c + i < p.features ? (f[i] - mean) * (f[i] - mean) : 0.f;
+      sq += part;
+    }
+    const float rstd = 1.f / sqrtf(row_sum<1024>(sq, shared, turn++) / (float)p.features + p.eps);
+    for (int c = threadIdx.x * VEC; c < p.features; c += 1024 * VEC) {
+      const int n = p.features - c;
+      float f[VEC], g[VEC], b[VEC];
+      unpack<T>(load_piece<T>(x + c, n), f);
+      load_floats<VEC>(p.gamma ? p.gamma + c : nullptr, n, 1.f, g);
+      load_floats<VEC>(p.beta ? p.beta + c : nullptr, n, 0.f, b);
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) f[i] = (f[i] - mean) * rstd * g[i] + b[i];
-    store_piece<T>(y + c, pack<T>(f), n);
-  }
-  if (threadIdx.x == 0) {
-    if (p.mean) p.mean[row] = mean;
-    if (p.rstd) p.rstd[row] = rstd;
-  }
+      for (int i = 0; i < VEC; ++i) f[i] = (f[i] - mean) * rstd * g[i] + b[i];
+      store_piece<T>(y + c, pack<T>(f), n);
+    }
+    if (threadIdx.x == 0) {
+      if (p.mean) p.mean[row] = mean;
+      if (p.rstd) p.rstd[row] = rstd;
+    }
   }
 }
 
@@ -308,35 +308,35 @@ __global__ __launch_bounds__(1024) void norm_long_backward_kernel(const NormPara
   __shared__ float shared[2][32];
   int turn = 0;
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
-  const T *x = (const T*)p.x + row * p.x_row, *dy = (const T*)p.dy + row * p.y_row;
-  T* dx = (T*)p.dx + row * p.x_row;
-  const float mean = p.mean_in[row], rstd = p.rstd_in[row];
-  float s1 = 0.f, s2 = 0.f;
-  for (int c = threadIdx.x * VEC; c < p.features; c += 1024 * VEC) {
-    float h[VEC], d[VEC], g[VEC], a = 0.f, b = 0.f;
-    unpack<T>(load_piece<T>(x + c, p.features - c), h);
-    unpack<T>(load_piece<T>(dy + c, p.features - c), d);
-    load_floats<VEC>(p.gamma ? p.gamma + c : nullptr, p.features - c, 1.f, g);
+    const T *x = (const T*)p.x + row * p.x_row, *dy = (const T*)p.dy + row * p.y_row;
+    T* dx = (T*)p.dx + row * p.x_row;
+    const float mean = p.mean_in[row], rstd = p.rstd_in[row];
+    float s1 = 0.f, s2 = 0.f;
+    for (int c = threadIdx.x * VEC; c < p.features; c += 1024 * VEC) {
+      float h[VEC], d[VEC], g[VEC], a = 0.f, b = 0.f;
+      unpack<T>(load_piece<T>(x + c, p.features - c), h);
+      unpack<T>(load_piece<T>(dy + c, p.features - c), d);
+      load_floats<VEC>(p.gamma ? p.gamma + c : nullptr, p.features - c, 1.f, g);
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      a += d[i] * g[i];
-      b += d[i] * g[i] * (h[i] - mean) * rstd;
+      for (int i = 0; i < VEC; ++i) {
+        a += d[i] * g[i];
+        b += d[i] * g[i] * (h[i] - mean) * rstd;
+      }
+      s1 += a;
+      s2 += b;
     }
-    s1 += a;
-    s2 += b;
-  }
-  row_sums<1024>(s1, s2, shared, turn++);
-  s1 /= (float)p.features;
-  s2 /= (float)p.features;
-  for (int c = threadIdx.x * VEC; c < p.features; c += 1024 * VEC) {
-    float h[VEC], d[VEC], g[VEC];
-    unpack<T>(load_piece<T>(x + c, p.features - c), h);
-    unpack<T>(load_piece<T>(dy + c, p.features - c), d);
-    load_floats<VEC>(p.gamma ? p.gamma + c : nullptr, p.features - c, 1.f, g);
+    row_sums<1024>(s1, s2, shared, turn++);
+    s1 /= (float)p.features;
+    s2 /= (float)p.features;
+    for (int c = threadIdx.x * VEC; c < p.features; c += 1024 * VEC) {
+      float h[VEC], d[VEC], g[VEC];
+      unpack<T>(load_piece<T>(x + c, p.features - c), h);
+      unpack<T>(load_piece<T>(dy + c, p.features - c), d);
+      load_floats<VEC>(p.gamma ? p.gamma + c : nullptr, p.features - c, 1.f, g);
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) d[i] = rstd * (d[i] * g[i] - s1 - (h[i] - mean) * rstd * s2);
-    store_piece<T>(dx + c, pack<T>(d), p.features - c);
-  }
+      for (int i = 0; i < VEC; ++i) d[i] = rstd * (d[i] * g[i] - s1 - (h[i] - mean) * rstd * s2);
+      store_piece<T>(dx + c, pack<T>(d), p.features - c);
+    }
   }
 }
 

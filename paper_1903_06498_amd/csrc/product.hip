@@ -928,7 +928,11 @@ struct TileTime {
 // parts: fp32 split into three bf16 parts, which is faster where the matrix instructions are what a CU waits for (2048^3: 124 us with fp32
 // instructions, 106), and slower where it is the way through the registers (512^3: 12.4 and 14.2).
 TileTime tile_time(int tile, int dtype, Access access, bool parts) {
-  if (dtype == STRIPE_F32) return parts ? TileTime{0.95, 1.55, 5, 7} : tile == kLeastTile ? TileTime{0.55, 1.0, 2, 4} : TileTime{1.0, 1.95, 3, 5};
+  if (dtype == STRIPE_F32) {
+    if (parts) return {0.95, 1.55, 5, 7};
+    if (access == kWords) return tile == kLeastTile ? TileTime{0.58, 0.97, 2, 4} : TileTime{1.05, 1.95, 3, 5};
+    return tile == kLeastTile ? TileTime{0.5, 1.0, 2, 4} : TileTime{0.95, 1.95, 3, 5};
+  }
   if (access != kPieces) return {0.75, 1.1, 3, 5};
   constexpr TileTime t[] = {{1.1, 1.45, 6, 9}, {0.56, 0.76, 4, 5}, {0.28, 0.5, 3, 5}, {0.22, 0.35, 2, 4}};
   return t[tile];
@@ -1045,8 +1049,9 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
       double us = 4;
       if (s.resident == 1) us += most * (kt * (t.k_few + (t.k_full - t.k_few) * full) + t.store_few + (t.store_full - t.store_few) * full);
       else us += std::floor(most / 2) * (kt * t.k_full + t.store_full) + std::fmod(most, 2) * (kt * t.k_few + t.store_few);
-      // the join: a launch, and its bytes written and read (300^3 fp32: 8.9 us in one piece, 9.6 in the five that would win without the launch)
-      if (splits > 1) us += 3.5 + (double)bytes * 2.5 / 4e6;
+      // the join: a launch, and its bytes written and read (300^3 fp32: 8.9 us in one piece, 9.6 in the five that would win without the launch;
+      // 1000 x 777 x 1283's dW: 40.9 in one, 34.8 in three)
+      if (splits > 1) us += 3.2 + (double)bytes * 1.5 / 4e6;
       if (us < best) {
         best = us;
         plan.tile = tile;

@@ -506,6 +506,25 @@ def test_two_graphs_with_workspaces_of_their_own():
             c.check(["y", "pre", "dx", "dw", "dbias"])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ACTS)
+def test_activations_of_large_values(act, dtype):
+    """|z| >= 40: act(z) is z or 0 up to |z| e^-40 < 2^-50, act'(z) 1 or 0 up to (1 + |z|^3) e^-40 < 2^-40 or what a square past overflow must not
+    turn into NaN; two roundings of fp32, one of the result's type."""
+    z = torch.tensor([40.0, -40.0, 1e4, -1e4, 1e10, -1e10, 2e19, -2e19, 3e38, -3e38], device="cuda", dtype=TYPES[dtype])
+    n = z.numel()
+    op = B.StripeLinear(1, 1, n, dtype, activation=act)
+    x, y = torch.ones(1, 1, dtype=z.dtype, device="cuda"), torch.zeros(1, n, dtype=z.dtype, device="cuda")
+    dy, db = torch.ones_like(z)[None], torch.zeros(n, device="cuda")
+    op.run(x, z[:, None], y)
+    op.backward(dy, x, z[:, None], pre=z[None], dbias=db)
+    torch.cuda.synchronize()
+    one = torch.ones_like(z) if act == "none" else (z > 0).to(z.dtype)
+    want = (z * one).double()
+    assert ((y[0].double() - want).abs() <= 2.0 ** -50 + (2 * U + HALF[dtype]) * want.abs()).all(), y
+    assert ((db.double() - one.double()).abs() <= 2.0 ** -40 + 2 * U).all(), db
+
+
 def test_wrapper_refuses_host_tensors():
     c = Linear(16, 32, 48, "bf16")
     with pytest.raises(ValueError, match="x: expected"):

@@ -160,3 +160,13 @@ def test_wrapper_checks_tensors():
     assert h._w == ((2, 16, 8), (128, 8, 1)) and h._b == ((2, 16), (16, 1)) and h._o == ((3,), (1,))
     one = B.StripeLinear(1, 8, 16, "bf16", x_row=64)                            # the stride of a single row does not matter
     assert one._ptr("x", torch.empty(1, 8, dtype=torch.bfloat16), torch.bfloat16, *one._x, -1)
+
+
+@pytest.mark.parametrize("change", [dict(rows=1 << 20, x_row=1 << 40), dict(rows=1 << 20, y_row=1 << 40), dict(out_features=1 << 18, w_row=1 << 40),
+                                    dict(groups=4096, w_group=1 << 60), dict(groups=4096, w_row=1 << 40, out_features=1 << 10)])
+def test_buffers_beyond_64_bit_offsets_are_refused(change):
+    args = dict(rows=16, in_features=32, out_features=48, dtype="bf16")
+    args.update(change)
+    assert _status(lambda: B.stripe_linear_create(**args)) == ERR["ERR_INVALID_DESC"]
+    for name in ("x_row", "y_row"):
+        assert _status(lambda: B.stripe_norm_create(1 << 20, 32, "f32", **{name: 1 << 40})) == ERR["ERR_INVALID_DESC"]
