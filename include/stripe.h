@@ -302,7 +302,8 @@ stripe_status_t stripe_device_mfma(const void* operands, void* out, int iters, i
  *    nearest even once, on store; zeros, infinities and NaN go the way the formula sends them;
  *  - a linear layer's fp32 products may be computed as three bf16 parts per value, which hold all
  *    24 bits down to 2^-110; of smaller values they lose what lies below 2^-133;
- *  - outputs must not overlap inputs or one another, except where stated;
+ *  - outputs must not overlap inputs or one another, except where stated (the same
+ *    address is refused with STRIPE_ERR_INVALID_DESC, other overlaps are not looked for);
  *  - the same call on the same inputs gives the same bits (no atomics);
  *  - a call that needs a workspace and has none of the caller's allocates it, once per
  *    device, and keeps it until the handle is destroyed; under graph capture such a first call

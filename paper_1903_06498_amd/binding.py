@@ -488,6 +488,12 @@ class _Layer:
         _check(getattr(lib, f"stripe_{self._name}_set_workspace")(self.handle, ptr, size))
         self._ws = tensor
 
+    def _current(self) -> int:
+        device = self._device()
+        if self._ws is not None and self._ws.get_device() != device:
+            raise ValueError(f"the workspace is on {self._ws.device}, the current device is cuda:{device}")
+        return device
+
     def _ptr(self, what, t, dtype, shape, strides, device):
         """The tensor's address; None (NULL) for None."""
         if t is None:
@@ -535,7 +541,7 @@ class StripeLinear(_Layer):
 
     def run(self, x, w, y, bias=None, residual=None, offsets=None, pre=None, stream: Optional[int] = None) -> None:
         """y = act(x W^T + bias) + residual; pre (optional) receives x W^T + bias for a backward pass."""
-        dev, p, t = self._device(), self._ptr, self._dtype
+        dev, p, t = self._current(), self._ptr, self._dtype
         st = lib.stripe_linear_run(self.handle, p("x", x, t, *self._x, dev), p("w", w, t, *self._w, dev), p("bias", bias, self._f32, *self._b, dev),
                                    p("residual", residual, t, *self._y, dev), p("offsets", offsets, self._i32, *self._o, dev), p("y", y, t, *self._y, dev),
                                    p("pre", pre, t, *self._y, dev), current_stream() if stream is None else stream)
@@ -544,7 +550,7 @@ class StripeLinear(_Layer):
 
     def backward(self, dy, x, w, pre=None, offsets=None, dx=None, dw=None, dbias=None, stream: Optional[int] = None) -> None:
         """The gradients that are given a tensor: dx, dw, dbias (that of the residual is dy itself)."""
-        dev, p, t = self._device(), self._ptr, self._dtype
+        dev, p, t = self._current(), self._ptr, self._dtype
         st = lib.stripe_linear_backward(self.handle, p("dy", dy, t, *self._y, dev), p("x", x, t, *self._x, dev), p("w", w, t, *self._w, dev),
                                         p("pre", pre, t, *self._y, dev), p("offsets", offsets, self._i32, *self._o, dev), p("dx", dx, t, *self._x, dev),
                                         p("dw", dw, t, *self._w, dev), p("dbias", dbias, self._f32, *self._b, dev),
@@ -569,7 +575,7 @@ class StripeNorm(_Layer):
 
     def run(self, x, y, gamma=None, beta=None, mean=None, rstd=None, stream: Optional[int] = None) -> None:
         """y = (x - mean) rstd gamma + beta; mean and rstd (optional) are stored for a backward pass."""
-        dev, p, f = self._device(), self._ptr, self._f32
+        dev, p, f = self._current(), self._ptr, self._f32
         st = lib.stripe_norm_run(self.handle, p("x", x, self._dtype, *self._x, dev), p("gamma", gamma, f, *self._c, dev), p("beta", beta, f, *self._c, dev),
                                  p("y", y, self._dtype, *self._y, dev), p("mean", mean, f, *self._r, dev), p("rstd", rstd, f, *self._r, dev),
                                  current_stream() if stream is None else stream)
@@ -578,7 +584,7 @@ class StripeNorm(_Layer):
 
     def backward(self, dy, x, mean, rstd, gamma=None, dx=None, dgamma=None, dbeta=None, stream: Optional[int] = None) -> None:
         """The gradients that are given a tensor: dx, dgamma, dbeta."""
-        dev, p, f = self._device(), self._ptr, self._f32
+        dev, p, f = self._current(), self._ptr, self._f32
         st = lib.stripe_norm_backward(self.handle, p("dy", dy, self._dtype, *self._y, dev), p("x", x, self._dtype, *self._x, dev),
                                       p("gamma", gamma, f, *self._c, dev), p("mean", mean, f, *self._r, dev), p("rstd", rstd, f, *self._r, dev),
                                       p("dx", dx, self._dtype, *self._x, dev), p("dgamma", dgamma, f, *self._c, dev), p("dbeta", dbeta, f, *self._c, dev),

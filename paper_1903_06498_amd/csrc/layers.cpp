@@ -3,6 +3,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <memory>
 
 #include "layers.hpp"
@@ -74,6 +75,13 @@ stripe_status_t launched(hipError_t e) {
 }
 
 bool misaligned(const void* p, int64_t to) { return (uintptr_t)p % (uintptr_t)to != 0; }
+
+// An output that begins where an input or another output does (overlaps with other beginnings are the caller's word).
+bool shared(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins) {
+  for (const void* const* o = outs.begin(); o != outs.end(); ++o)
+    if (*o && (std::find(ins.begin(), ins.end(), *o) != ins.end() || std::find(o + 1, outs.end(), *o) != outs.end())) return true;
+  return false;
+}
 
 }  // namespace
 
@@ -164,6 +172,7 @@ stripe_status_t linear_run(stripe_linear_t* lin, const void* x, const void* w, c
   if (misaligned(x, e) || misaligned(w, e) || misaligned(residual, e) || misaligned(y, e) || misaligned(pre, e) || misaligned(bias, 4))
     return api_fail(STRIPE_ERR_MISALIGNED, "a buffer is not aligned to its element type");
   if (!d.rows) return STRIPE_OK;
+  if (shared({y, pre}, {x, w, bias, offsets}) || (pre && pre == residual)) return api_fail(STRIPE_ERR_INVALID_DESC, "y or pre is an input, or one another");
   const Access access = misaligned(x, 16) || misaligned(w, 16) ? lin->otherwise : lin->best;
   const ProductPlan& plan = lin->plan[access][kForward];
   unsigned char* ws = nullptr;
@@ -191,6 +200,7 @@ stripe_status_t linear_backward(stripe_linear_t* lin, const void* dy, const void
   const int64_t e = elem_size(d.dtype), v = 16 / e;
   if (misaligned(dy, e) || misaligned(x, e) || misaligned(w, e) || misaligned(pre, e) || misaligned(dx, e) || misaligned(dw, e) || misaligned(dbias, 4))
     return api_fail(STRIPE_ERR_MISALIGNED, "a buffer is not aligned to its element type");
+  if (d.rows && shared({dx, dw, dbias}, {dy, x, w, pre, offsets})) return api_fail(STRIPE_ERR_INVALID_DESC, "a gradient's buffer is an input's or another's");
   const bool dy_off = !act && misaligned(dy, 16);
   const Access w_access = dy_off || misaligned(w, 16) ? lin->otherwise : lin->best, x_access = dy_off || misaligned(x, 16) ? lin->otherwise : lin->best;
   const ProductPlan &in_plan = lin->plan[w_access][kInputGrad], &w_plan = lin->plan[x_access][kWeightGrad];
@@ -268,6 +278,8 @@ stripe_status_t norm_run(stripe_norm_t* norm, const void* x, const float* gamma,
   if (misaligned(x, e) || misaligned(y, e) || misaligned(gamma, 4) || misaligned(beta, 4) || misaligned(mean, 4) || misaligned(rstd, 4))
     return api_fail(STRIPE_ERR_MISALIGNED, "a buffer is not aligned to its element type");
   if (!norm->d.rows) return STRIPE_OK;
+  if (shared({y, mean, rstd}, {gamma, beta}) || x == mean || x == rstd || (x == y && norm->d.rows > 1 && norm->d.x_row != norm->d.y_row))
+    return api_fail(STRIPE_ERR_INVALID_DESC, "an output is an input or another output, or y is x with other row strides");
   NormParams p = norm_params(norm);
   p.x = x; p.gamma = gamma; p.beta = beta; p.y = y; p.mean = mean; p.rstd = rstd;
   return launched(launch_norm(norm->d.dtype, p, (hipStream_t)hip_stream));
@@ -282,6 +294,8 @@ stripe_status_t norm_backward(stripe_norm_t* norm, const void* dy, const void* x
   if (misaligned(x, e) || misaligned(dy, e) || misaligned(dx, e) || misaligned(gamma, 4) || misaligned(mean, 4) || misaligned(rstd, 4) ||
       misaligned(dgamma, 4) || misaligned(dbeta, 4))
     return api_fail(STRIPE_ERR_MISALIGNED, "a buffer is not aligned to its element type");
+  if (norm->d.rows && shared({dx, dgamma, dbeta}, {dy, x, gamma, mean, rstd}))
+    return api_fail(STRIPE_ERR_INVALID_DESC, "a gradient's buffer is an input's or another's");
   unsigned char* ws = nullptr;
   if (norm->ws_bytes && (dgamma || dbeta))
     if (const stripe_status_t st = norm->ws.get(norm->ws_bytes, (hipStream_t)hip_stream, &ws); st != STRIPE_OK) return st;

@@ -170,3 +170,46 @@ def test_buffers_beyond_64_bit_offsets_are_refused(change):
     assert _status(lambda: B.stripe_linear_create(**args)) == ERR["ERR_INVALID_DESC"]
     for name in ("x_row", "y_row"):
         assert _status(lambda: B.stripe_norm_create(1 << 20, 32, "f32", **{name: 1 << 40})) == ERR["ERR_INVALID_DESC"]
+
+
+def test_outputs_that_are_inputs_are_refused():
+    """Every buffer at an address of its own but for one pair."""
+    spread = lambda names: {n: (i + 1) << 20 for i, n in enumerate(names)}      # noqa: E731
+    lin, norm, strided = _linear(activation="silu"), B.stripe_norm_create(16, 32, "bf16"), B.stripe_norm_create(16, 32, "bf16", y_row=40)
+
+    def check(call, handle, names, pairs):
+        for a, b in pairs:
+            args = spread(names)
+            if "offsets" in args:
+                args["offsets"] = None
+            args[a] = args[b]
+            assert call(handle, *args.values(), None) == ERR["ERR_INVALID_DESC"], (a, b)
+
+    check(B.lib.stripe_linear_run, lin, ("x", "w", "bias", "residual", "offsets", "y", "pre"), [("y", "x"), ("y", "w"), ("pre", "x"), ("pre", "y"), ("pre", "residual")])
+    check(B.lib.stripe_linear_backward, lin, ("dy", "x", "w", "pre", "offsets", "dx", "dw", "dbias"),
+          [("dx", "dy"), ("dx", "x"), ("dx", "pre"), ("dw", "w"), ("dw", "dx"), ("dbias", "dw")])
+    check(B.lib.stripe_norm_run, norm, ("x", "gamma", "beta", "y", "mean", "rstd"), [("y", "gamma"), ("mean", "rstd"), ("mean", "x"), ("rstd", "y")])
+    check(B.lib.stripe_norm_run, strided, ("x", "gamma", "beta", "y", "mean", "rstd"), [("y", "x")])
+    check(B.lib.stripe_norm_backward, norm, ("dy", "x", "gamma", "mean", "rstd", "dx", "dgamma", "dbeta"),
+          [("dx", "dy"), ("dx", "x"), ("dgamma", "gamma"), ("dgamma", "dbeta"), ("dbeta", "mean")])
+    B.lib.stripe_linear_destroy(lin)
+    for h in (norm, strided):
+        B.lib.stripe_norm_destroy(h)
+
+
+def test_a_workspace_of_another_device_is_refused():
+    h = B.StripeNorm(512, 256, "bf16")
+
+    class Elsewhere:
+        device = "cuda:1"
+
+        def get_device(self):
+            return 1
+
+    h._device, h._ws = lambda: 0, Elsewhere()
+    with pytest.raises(ValueError, match="workspace is on"):
+        h.run(None, None)
+    with pytest.raises(ValueError, match="workspace is on"):
+        h.backward(None, None, None, None)
+    h._ws = None
+    h.close()
