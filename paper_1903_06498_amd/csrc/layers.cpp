@@ -142,7 +142,7 @@ stripe_status_t linear_create(const stripe_linear_desc_t* desc, stripe_linear_t*
                       (!d.groups || d.w_group % v == 0) ? kPieces : lin->otherwise;
   for (const Access access : {lin->best, lin->otherwise})
     for (int k = 0; k < 3; ++k) {
-      lin->plan[access][k] = plan_product((ProductKind)k, d.dtype, d.rows, d.in_features, d.out_features, d.groups, access);
+      lin->plan[access][k] = plan_product((ProductKind)k, d.dtype, d.rows, d.in_features, d.out_features, d.groups, access, d.w_row * elem_size(d.dtype) % 4 != 0);
       lin->partial_bytes = std::max(lin->partial_bytes, round_up_256(lin->plan[access][k].ws_bytes));
     }
   if (d.activation != STRIPE_ACT_NONE) {

@@ -61,17 +61,17 @@ struct ProductPlan {
   int tile = 0;             // index into the tile table
   int splits = 1;
   bool parts = false;       // fp32 in three bf16 parts
-  int few = 0;              // kForward: the kernel for few rows, 16 times as many at a time (product_rows.hip)
+  bool few = false;         // kForward: the kernel for few rows (product_rows.hip)
   int64_t ws_bytes = 0;     // partial images
 };
 // How a product's operands can be fetched: element by element at their rims; in whole 16-byte pieces (addresses, strides and contiguous extents are
 // multiples of them); in 4-byte words (fp32).  The latter two also want a tile's rows to span less than 2^31 bytes.
 enum Access { kAny = 0, kPieces = 1, kWords = 2 };
-ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, Access access);
+ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, Access access, bool odd_rows);
 std::string product_name(ProductKind kind, int dtype, const ProductPlan& plan, Access access);
 hipError_t launch_product(ProductKind kind, int dtype, const ProductPlan& plan, Access access, ProductParams p, hipStream_t stream);
 
-hipError_t launch_product_rows(int dtype, int fm, ProductParams p, hipStream_t stream);
+hipError_t launch_product_rows(int dtype, ProductParams p, hipStream_t stream);
 
 // dz = dy act'(z) (dz == nullptr: not stored; act none: not needed) and db = sums of dz over each group's rows (db == nullptr: not
 // computed).  partial: fp32, dz_slots(rows, groups) x out, unused if db is nullptr or there is one slot.

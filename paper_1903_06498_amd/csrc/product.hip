@@ -8,8 +8,8 @@
 //   c ^ ((r >> 1) & 7); a fragment is one 16-byte read;
 //   one whose row index is contiguous ([k][row]): as it lies in memory, a row of BM or BN elements per k, pieces swizzled by k; a bf16
 //   fragment is two transposing reads, an fp32 one four 4-byte reads.
-// Everything beyond the reduction's end is zero in both operands; rows and columns beyond the output repeat valid ones, whose sums are
-// never stored.
+// Everything beyond the reduction's end is zero in both operands; rows and columns beyond the output are zeros or repeat valid ones, and their sums
+// are never stored.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -1009,23 +1009,36 @@ hipError_t launch_type(ProductKind kind, const ProductPlan& plan, Access access,
   }
 }
 
+// Few rows, which read W once for every 16 rows of a group, 16 columns a workgroup: a launch, and for each workgroup of a CU its bytes at the rate that one
+// reaches; bf16 rows at odd addresses take three times as long (4095 -> 4095, 16 rows: 26.7 us, 18.4 on tiles).  floor: what the tiles take at least once
+// they are more than one to a CU, W from memory.  The groups that have rows are taken to be as many as if rows were dealt out at random.
+// Measured, this kernel and the tiles, us: 4096 -> 4096 bf16 1 row 8.3 and 10.8, 16 10.5 and 10.6, 32 18.3 and 11.3; 1024 -> 1024 6.3 and 6.5 up to 64 rows;
+// 8192 -> 2048 1 row 12 and 12, 16 16.8 and 11.3; fp32 4096 -> 4096 16 rows 20.5 and 23, 32 36.9 and 23.5; 2048 -> 1024 of 64 groups 16 rows 14.2 and 11.2,
+// 64 35 and 42, 256 53 and 55; of 8 groups 64 rows 9.5 and 12.6; 1024 -> 4096 of 64 groups 64 rows 71 and 62.
+struct RowsTime {
+  double us, floor;
+};
+RowsTime rows_time(int dtype, int64_t rows, int64_t in, int64_t out, int groups, bool odd_rows) {
+  const double all = groups, used = groups ? all * (1 - std::exp(-(double)rows / all)) : 1;
+  const double slots = used * std::ceil((double)rows / (16 * used)), each = 16.0 * (double)in * (dtype == STRIPE_F32 ? 4 : 2);
+  const double rate = odd_rows ? 6e3 : 20e3;      // bytes per us
+  const double workgroups = slots * (double)((out + 15) / 16);
+  return {3.5 + std::max(1.0, workgroups / 256) * (each / rate + 0.15), 4 + used * (double)in * (double)out * (dtype == STRIPE_F32 ? 4 : 2) / 5.2e6};
+}
+
 }  // namespace
 
 // The tile and the slices of the reduction with the smallest estimated time: the workgroups of the CU that has most of them one after the other,
 // or in pairs where two fit.
-ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, Access access) {
+ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, Access access, bool odd_rows) {
   ProductPlan plan;
   plan.tile = kSmallTile;
-  // few rows (of a group, on average): W is read once, whatever is computed with it.  4096 x 4096 bf16: 1 row 8.4 us, 16 10.5, 32 13.8 where 128 x 128
-  // tiles take 42; 64 groups of 2048 x 1024: 16 rows 14.2 against 25.1, 256 53 against 59, 512 67 against 60.
-  if (kind == kForward && (rows <= 32 || (groups && rows <= 4 * (int64_t)groups))) plan.few = rows <= 16 || groups ? 1 : 2;
-  if (const int forced = tune_int("product_few", -1); forced >= 0 && kind == kForward) plan.few = forced;
-  if (plan.few || !rows) return plan;
+  if (!rows) return plan;
   const int64_t m = kind == kWeightGrad ? out : rows, n = kind == kForward ? out : in, k = kind == kForward ? in : kind == kInputGrad ? out : rows;
   const int64_t images = kind == kWeightGrad ? std::max(1, groups) : 1, depth = dtype == STRIPE_F32 ? 32 : 64;
   const double depth_of = kind == kWeightGrad && groups ? (double)k / groups : (double)k;
   const int64_t k_tiles = std::max<int64_t>(1, (int64_t)std::ceil(depth_of / (double)depth));
-  double best = __builtin_huge_val();
+  double best = __builtin_huge_val(), best_workgroups = 0;
   const int forced_tile = tune_int("product_tile", -1), forced_splits = tune_int("product_splits", 0);
   const bool f32 = dtype == STRIPE_F32;
   for (int variant = 0; variant < kTileCount; ++variant) {
@@ -1058,14 +1071,23 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
         plan.parts = parts;
         plan.splits = splits;
         plan.ws_bytes = bytes;
+        best_workgroups = workgroups;
       }
     }
   }
+  if (kind == kForward && rows <= (groups ? 8 * (int64_t)groups : 64)) {
+    const RowsTime few = rows_time(dtype, rows, in, out, groups, odd_rows);
+    if (best_workgroups > 256) best = std::max(best, few.floor);
+    plan.few = few.us <= 1.05 * best;
+  }
+  if (const int forced = tune_int("product_few", -1); forced >= 0 && kind == kForward) plan.few = forced != 0;
+  if ((groups ? rows / 16 + std::min<int64_t>(groups, rows) : (rows + 15) / 16) * ((out + 15) / 16) >= 1 << 23) plan.few = false;      // 2^32 lanes
+  if (plan.few) plan.splits = 1, plan.ws_bytes = 0;
   return plan;
 }
 
 std::string product_name(ProductKind kind, int dtype, const ProductPlan& plan, Access access) {
-  if (plan.few) return std::string("product_rows_") + (dtype == STRIPE_F32 ? "f32_" : "bf16_") + std::to_string(16 * plan.few) + "x16";
+  if (plan.few) return std::string("product_rows_") + (dtype == STRIPE_F32 ? "f32_" : "bf16_") + "16x16";
   const TileShape s = kTiles[plan.tile];
   return std::string(access != kAny && !plan.parts ? "product_stream_" : "product_") + (kind == kForward ? "nt_" : kind == kInputGrad ? "nn_" : "tn_") + (dtype == STRIPE_F32 ? "f32_" : "bf16_") +
          std::to_string(64 * s.fm) + "x" + std::to_string(64 * s.fn) + (plan.parts ? "_parts" : access != kAny ? "_s" + std::to_string(s.stages) : "") + (access == kWords && !plan.parts ? "_words" : "") +
@@ -1073,7 +1095,7 @@ std::string product_name(ProductKind kind, int dtype, const ProductPlan& plan, A
 }
 
 hipError_t launch_product(ProductKind kind, int dtype, const ProductPlan& plan, Access access, ProductParams p, hipStream_t stream) {
-  if (plan.few) return launch_product_rows(dtype, plan.few, p, stream);
+  if (plan.few) return launch_product_rows(dtype, p, stream);
   return dtype == STRIPE_F32 ? launch_type<float>(kind, plan, access, p, stream) : launch_type<__bf16>(kind, plan, access, p, stream);
 }
 

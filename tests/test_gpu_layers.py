@@ -381,10 +381,12 @@ def test_rows_far_apart(dtype):
     c.check(["y", "pre", "dx", "dw", "dbias"])
 
 
-def test_f32_in_parts_with_infinities_nan_and_the_largest_values():
+@pytest.mark.parametrize("few", [0, 1])
+def test_f32_in_parts_with_infinities_nan_and_the_largest_values(few, monkeypatch):
     """What three bf16 parts cannot hold is computed again in fp32: every value and every neighbour as the formula has them."""
+    monkeypatch.setenv("STRIPE_TUNE", f"product_few={few}")
     c = Linear(40, 72, 136, "f32", act="none", bias=False, residual=False, pad=(1 << 20) + 8, seed=4)
-    assert "parts" in c.op.info["forward"]
+    assert ("rows" if few else "parts") in c.op.info["forward"] and "parts" in c.op.info["input_grad"] and "parts" in c.op.info["weight_grad"]
     big = torch.finfo(torch.float32).max
     c.x[3, 5], c.x[7, 0], c.x[11, 2], c.x[12, 3], c.x[13, 4] = float("inf"), NAN, big, -big, big
     c.x[13, 6], c.x[14] = float("-inf"), 0.0

@@ -213,3 +213,11 @@ def test_a_workspace_of_another_device_is_refused():
         h.backward(None, None, None, None)
     h._ws = None
     h.close()
+
+
+def test_few_rows_run_on_their_kernel_where_a_launch_holds_them():
+    forward = lambda *a, **kw: B.StripeLinear(*a, **kw).info["forward"]                            # noqa: E731
+    assert "rows" in forward(1, 1024, 1024, "f32") and "rows" in forward(8, 1024, 1024, "bf16", groups=8)
+    assert "rows" not in forward(65, 1024, 1024, "f32") and "rows" not in forward(1000, 1024, 1024, "bf16", groups=8)
+    # 4096 groups of 16 rows at most, 2^17 / 16 columns: more than 2^32 lanes
+    assert "rows" not in forward(4096, 8, 1 << 17, "bf16", groups=4096)
