@@ -1065,6 +1065,7 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
       // the join: a launch, and its bytes written and read (300^3 fp32: 8.9 us in one piece, 9.6 in the five that would win without the launch;
       // 1000 x 777 x 1283's dW: 40.9 in one, 34.8 in three)
       if (splits > 1) us += 3.2 + (double)bytes * 1.5 / 4e6;
+      if (forced_splits && splits != forced_splits) us += 1e9;      // one piece, only where that many cannot be made
       if (us < best) {
         best = us;
         plan.tile = tile;

@@ -221,3 +221,15 @@ def test_few_rows_run_on_their_kernel_where_a_launch_holds_them():
     assert "rows" not in forward(65, 1024, 1024, "f32") and "rows" not in forward(1000, 1024, 1024, "bf16", groups=8)
     # 4096 groups of 16 rows at most, 2^17 / 16 columns: more than 2^32 lanes
     assert "rows" not in forward(4096, 8, 1 << 17, "bf16", groups=4096)
+
+
+@pytest.mark.parametrize("splits", [1, 2, 3, 4])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tile", [1, 2, 3])
+def test_the_number_of_slices_can_be_chosen(tile, dtype, splits, monkeypatch):
+    """STRIPE_TUNE's product_splits decides, whatever the time model says; one piece where a reduction has too few K tiles for it."""
+    monkeypatch.setenv("STRIPE_TUNE", f"product_few=0,product_tile={tile},product_splits={splits}")
+    name = f"_k{splits}" if splits > 1 else ""
+    for kernel in list(B.StripeLinear(1400, 1352, 1368, dtype, groups=2).info.values())[:3] + list(B.StripeLinear(700, 520, 904, dtype).info.values())[:3]:
+        assert kernel.endswith(name) and ("_k" in kernel) == (splits > 1), kernel
+    assert not any("_k" in k for k in list(B.StripeLinear(60, 56, 48, "bf16").info.values())[:3])
