@@ -7,7 +7,7 @@ taken twice or read from the wrong stage is 64 (32) terms of a sum of up to 1816
 import pytest
 import torch
 
-from tests.test_gpu_layers import HALF, NAN, TYPES, U, Linear, untouched, window
+from tests.test_gpu_layers import NAN, U, Linear, untouched, window
 
 pytestmark = pytest.mark.gpu
 
