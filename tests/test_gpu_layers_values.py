@@ -59,3 +59,74 @@ def test_activations_of_negative_values(act, dtype, rows):
     tol = (rel + 6 * U) * (p + second.abs()) + 2.0 ** -118
     err = (db.double() - slope).abs() / tol
     assert err.max() <= 1, f"act'({z[err.argmax()].item()}): {db[err.argmax()].item()} for {slope[err.argmax()].item()}, {err.max().item():.2f} of the tolerance"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("features", [7, 64, 1000, 3001, 8192, 16384, 16391, 40000])
+def test_norm_of_constant_rows(features, dtype):
+    """h = 0, y = beta and mean = x, whatever x is.
+
+    n fp32 additions after one another leave a first mean m that is off by d, |d| <= n u |x|; the distances from it are exact and all d, their mean is d
+    up to n u |d|: h is off by (n u)^2 |x| / sqrt(eps), and the mean by that and its own rounding."""
+    value = torch.tensor([0.1, 1000.1, -77777.7, 3e-3, 0.0], device="cuda").to(TYPES[dtype])
+    x = value[:, None].expand(-1, features).contiguous()
+    rows, eps, n = len(value), 1e-5, 32 + 6 + 16 + features // 1024 + 4
+    g = torch.Generator(device="cuda").manual_seed(features)
+    gamma, beta = (torch.randn(features, generator=g, device="cuda") for _ in range(2))
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    B.StripeNorm(rows, features, dtype, eps=eps).run(x, y, gamma=gamma, beta=beta, mean=mean, rstd=rstd)
+    torch.cuda.synchronize()
+    v = value.double()
+    left = (n * U) ** 2 * v.abs()
+    assert ((mean.double() - v).abs() <= left + U * (v.abs() + left)).all(), (mean, value)
+    tol = left[:, None] * eps ** -0.5 * gamma.double().abs() + U * beta.double().abs()
+    err = (y.double() - beta.double()).abs()
+    tol = tol + HALF[dtype] * (beta.double().abs() + tol)
+    assert (err <= tol).all(), [(value[r].item(), err[r].max().item(), tol[r].max().item()) for r in range(rows)]
+    # var <= (n u x)^2 changes eps by that much
+    s = eps ** -0.5
+    assert ((rstd.double() - s).abs() <= s * ((n * U * v) ** 2 / eps + 6 * U)).all(), rstd
+
+
+def test_norm_of_rows_whose_mean_is_far_larger_than_their_spread():
+    """x = m (1 + k 2^-20), |k| <= 3: the spread is a few of fp32's steps.  The first mean is off by up to n u |m|, more than the spread; the corrected
+    one by (n u)^2 |m| + n u mean |x - m| and its own rounding."""
+    rows, features, n = 40, 3001, 32 + 6 + 16 + 8
+    g = torch.Generator(device="cuda").manual_seed(7)
+    m = 2.0 ** torch.randint(-3, 12, (rows, 1), generator=g, device="cuda").float()
+    x = m * (1 + torch.randint(-3, 4, (rows, features), generator=g, device="cuda").float() * 2.0 ** -20)
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    eps = 1e-12
+    B.StripeNorm(rows, features, "f32", eps=eps).run(x, y, mean=mean, rstd=rstd)
+    torch.cuda.synchronize()
+    xd = x.double()
+    mu = xd.mean(1, keepdim=True)
+    d = xd - mu
+    var = (d * d).mean(1, keepdim=True) + eps
+    s = var ** -0.5
+    # distances from the first mean are at most |d| + n u |m|, which their squares' sum and the correction's square carry into the variance
+    wide = d.abs() + n * U * xd.abs()
+    em = (n * U) ** 2 * xd.abs().mean(1, keepdim=True) + (n + 2) * U * wide.mean(1, keepdim=True)
+    es = s * ((n + 8) * U * 2 * (wide * wide).mean(1, keepdim=True) / var + em * em / var + 8 * U)
+    ey = (em + U * mu.abs() + 2 * U * wide) * s + d.abs() * es + 3 * U * (d * s).abs()
+    assert ((mean.double()[:, None] - mu).abs() <= em + U * mu.abs()).all()
+    assert ((rstd.double()[:, None] - s).abs() <= es + U * s).all()
+    assert ((y.double() - d * s).abs() <= ey).all(), ((y.double() - d * s).abs() / ey).max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("features", [7, 3001, 16384, 40000])
+def test_norm_of_rows_with_infinities_nan_and_large_values(features, dtype):
+    """An infinity in a row is its mean and leaves no finite distance; equal values whose distances from a rounded mean have no finite square are beta still."""
+    x = torch.randn(6, features, generator=torch.Generator(device="cuda").manual_seed(0), device="cuda").to(TYPES[dtype])
+    x[0, 3], x[1, features - 1], x[2, 1], x[3], x[4] = float("inf"), float("-inf"), float("nan"), 1e30, -1e26
+    beta = torch.randn(features, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    y, mean, rstd = torch.empty_like(x), torch.empty(6, device="cuda"), torch.empty(6, device="cuda")
+    B.StripeNorm(6, features, dtype).run(x, y, beta=beta, mean=mean, rstd=rstd)
+    torch.cuda.synchronize()
+    assert mean[0] == float("inf") and mean[1] == float("-inf") and torch.isnan(mean[2]) and torch.isnan(rstd[:3]).all() and torch.isnan(y[:3]).all()
+    n = 32 + 6 + 16 + features // 1024 + 4
+    assert ((mean[3:5].double() - x[3:5, 0].double()).abs() <= n * U * x[3:5, 0].double().abs()).all()
+    # the mean is exact, or its error's square overflows and s is 0
+    assert torch.equal(y[3:5], beta.to(y.dtype).expand(2, -1))
+    assert torch.isfinite(y[5]).all()
