@@ -8,6 +8,8 @@
 // 6 % longer with it, 32768 x 512 13 %; fp32 up to 2 %): where their spread is small beside their mean, the values are multiples of 2^-9 of the largest, and
 // sums of up to 2^15 of them are exact in fp32.  The backward pass keeps its columns' sums of dy h and dy in registers over all the
 // rows that its workgroup takes, leaves one row of partial sums per workgroup and adds those in a second launch in a fixed order.
+#include <algorithm>
+
 #include "layers_device.hpp"
 
 namespace stripe {
@@ -459,8 +461,15 @@ hipError_t backward_t(const NormParams& p, hipStream_t stream) {
 }  // namespace
 
 // Each workgroup leaves 8 bytes for each feature, to be read again: one for each CU; two where rows are short and there are many (8192 x 8192 bf16: 85 us,
-// 95 with two; 32768 x 512: 31 and 26; 1537 x 1000 fp32: 10.9 and 13.2).
+// 95 with two; 32768 x 512: 31 and 26; 1537 x 1000 fp32: 10.9 and 13.2).  Rows too long for registers are summed in strips of 256 lanes, by as many
+// workgroups to a strip as make about 1024 of all strips: the sums take at most 16 MB, and the two launches
+// 23.5 us at 300 x 20000 bf16 (38 with 256 to a strip; 16.3 with half as many), 222 at 16384 x 20000 (256; 268), 190 at 512 x 2^18 fp32 (405;
+// 215), 235 at 256 x 2^20 bf16 (1735 and 2 GB of sums; 204).
 int norm_backward_blocks(int64_t rows, int64_t features, int dtype) {
+  if (features > kLong) {
+    const int64_t lane = dtype == STRIPE_F32 ? 4 : 8, strips = (features + 256 * lane - 1) / (256 * lane);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(rows, 1024 / strips));
+  }
   const int64_t at_once = lanes_of(features, true) == 64 ? 4 : 1, groups = (rows + at_once - 1) / at_once;
   const int64_t most = features * (dtype == STRIPE_F32 ? 4 : 2) <= 4096 && groups >= 16 * 512 ? 512 : 256;
   return (int)(groups < 1 ? 1 : groups < most ? groups : most);

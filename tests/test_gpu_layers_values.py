@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_1903_06498_amd import binding as B
-from tests.test_gpu_layers import HALF, TYPES, U, act_eval
+from tests.test_gpu_layers import HALF, TYPES, U, Norm, act_eval
 
 pytestmark = pytest.mark.gpu
 
@@ -130,3 +130,14 @@ def test_norm_of_rows_with_infinities_nan_and_large_values(features, dtype):
     # the mean is exact, or its error's square overflows and s is 0
     assert torch.equal(y[3:5], beta.to(y.dtype).expand(2, -1))
     assert torch.isfinite(y[5]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,features", [(300, 20000), (1100, 16392), (77, 131075), (9, (1 << 21) + 1)])
+def test_norm_of_long_rows(rows, features, dtype):
+    """Column sums in one, a few and many workgroups to a strip of columns."""
+    c = Norm(rows, features, dtype)
+    c.forward()
+    c.check_forward()
+    c.backward()
+    c.check_backward()

@@ -233,3 +233,13 @@ def test_the_number_of_slices_can_be_chosen(tile, dtype, splits, monkeypatch):
     for kernel in list(B.StripeLinear(1400, 1352, 1368, dtype, groups=2).info.values())[:3] + list(B.StripeLinear(700, 520, 904, dtype).info.values())[:3]:
         assert kernel.endswith(name) and ("_k" in kernel) == (splits > 1), kernel
     assert not any("_k" in k for k in list(B.StripeLinear(60, 56, 48, "bf16").info.values())[:3])
+
+
+@pytest.mark.parametrize("features", [16384, 16385, 20000, 1 << 17, 1 << 20, (1 << 22) + 3, 1 << 24])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_norms_workspace_stays_small(dtype, features):
+    """The column sums that the backward pass leaves between its launches, whatever the shape: at most 256 rows of 16384 features, or 1024 strips."""
+    for rows in (1, 255, 256, 1 << 20):
+        h = B.StripeNorm(rows, features, dtype)
+        assert h.workspace_bytes <= 256 * 2 * 16384 * 4, (rows, h.workspace_bytes)
+        h.close()
