@@ -141,3 +141,44 @@ def test_norm_of_long_rows(rows, features, dtype):
     c.check_forward()
     c.backward()
     c.check_backward()
+
+
+@pytest.mark.parametrize("other", [2.0 ** 40, 2.0 ** 60])
+@pytest.mark.parametrize("splits", [1, 3])
+def test_f32_in_parts_of_small_values(splits, other, monkeypatch):
+    """Three bf16 parts hold all 24 bits of a value down to 2^-110, and of a smaller one what does not lie below 2^-133.
+
+    One value in each row: the result is a single product, six products of parts added up with a rounding or truncation each, at most 2 u, and the dropped
+    ones below 2^-25 of it: within 14 u.  A part that ends at 2^-133 is off by half of that, times the other factor."""
+    monkeypatch.setenv("STRIPE_TUNE", f"product_few=0,product_tile=1,product_splits={splits}")
+    rows, cin, cout = 200, 421, 389
+    op = B.StripeLinear(rows, cin, cout, "f32")
+    name = "_parts" + (f"_k{splits}" if splits > 1 else "")
+    assert all(op.info[k].endswith(name) for k in ("forward", "input_grad", "weight_grad")), op.info
+    g = torch.Generator(device="cuda").manual_seed(1)
+
+    def single(n, m, exponent):       # a value from 2^exponent to twice that in each row of a matrix, of either sign
+        v = torch.zeros(n, m, dtype=torch.float64, device="cuda")
+        size = (1 + torch.rand(n, generator=g, device="cuda", dtype=torch.float64)) * 2.0 ** exponent
+        v[torch.arange(n, device="cuda"), torch.randint(0, m, (n,), generator=g, device="cuda")] = torch.where(torch.rand(n, generator=g, device="cuda") < 0.5, size, -size)
+        return v.float()
+
+    def dense(n, m):
+        return (1 + torch.rand(n, m, generator=g, device="cuda")) * other
+
+    for exponent in (0, -60, -100, -109, -110, -111, -118, -125, -130, -133, -140):
+        for first in (True, False):       # the small values in the first operand, in the second
+            x, w, dy = (single(rows, cin, exponent), dense(cout, cin), single(rows, cout, exponent)) if first else (
+                dense(rows, cin), single(cout, cin, exponent), dense(rows, cout))
+            wt = w if first else single(cin, cout, exponent).t().contiguous()      # dx: one value in each column of W
+            xs, dys = (single(cin, rows, exponent).t().contiguous(), dense(rows, cout)) if first else (dense(rows, cin), single(cout, rows, exponent).t().contiguous())
+            y, dx, dw = torch.empty(rows, cout, device="cuda"), torch.empty_like(x), torch.empty_like(w)
+            op.run(x, w, y)
+            op.backward(dy, x, wt, dx=dx)
+            op.backward(dys, xs, w, dw=dw)
+            torch.cuda.synchronize()
+            for what, got, a, b in (("y", y, x, w.t()), ("dx", dx, dy, wt), ("dw", dw, dys.t(), xs)):
+                v = a.double() @ b.double()
+                tol = 14 * U * v.abs() + (2.0 ** -134 * 2 * other if exponent < -110 else 0)
+                worst = (got.double() - v).abs() / tol
+                assert (worst <= 1).all(), f"{what}: {worst.max().item():.1f} of the tolerance, values from 2^{exponent}"
