@@ -299,9 +299,13 @@ stripe_status_t stripe_device_mfma(const void* operands, void* out, int iters, i
  *    is not is refused (STRIPE_ERR_MISALIGNED).  16-byte aligned pointers,
  *    strides and feature counts run faster kernels, nothing else depends on them;
  *  - sums, statistics and totals are fp32 (or wider); a bf16 result is rounded to
- *    nearest even once, on store; zeros, infinities and NaN go the way the formula sends them;
- *  - a linear layer's fp32 products may be computed as three bf16 parts per value, which hold all
+ *    nearest even once, on store; zeros, infinities and NaN go the way the formula sends them.  A bf16 linear layer's
+ *    dz is rounded to bf16 before dx and dW are computed from it (db adds it up unrounded);
+ *  - values of an activation that are smaller than 2^-118 may be 0;
+ *  - a linear layer's fp32 products may be computed as three bf16 parts per value (large ones are: the kernels' names
+ *    in stripe_linear_info_t then say "parts"), which hold all
  *    24 bits down to 2^-110; of smaller values they lose what lies below 2^-133;
+ *  - a layer norm's squared distances are fp32: a row where their sum passes fp32's largest value has s = 0;
  *  - outputs must not overlap inputs or one another, except where stated (the same
  *    address is refused with STRIPE_ERR_INVALID_DESC, other overlaps are not looked for);
  *  - the same call on the same inputs gives the same bits (no atomics);

@@ -465,7 +465,7 @@ class _Layer:
     """What the layers' wrappers share: the handle, its workspace, the checks of a call's tensors.
 
     Tensors are checked before anything is launched: element type, shape, strides as the handle was made for, device.  Every tensor
-    has to be on the current device, whose current stream the call runs on unless it is given one.
+    has to be on the current device, whose current stream the call runs on unless it is given one.  The caller keeps them until the call has run.
     """
 
     _name = ""
@@ -481,7 +481,11 @@ class _Layer:
         self._f32, self._i32, self._device = torch.float32, torch.int32, torch.cuda.current_device
 
     def set_workspace(self, tensor) -> None:
-        """Hand the handle a caller-owned device workspace (a contiguous torch CUDA tensor, kept alive here), or None."""
+        """Hand the handle a caller-owned device workspace (a contiguous torch CUDA tensor, kept alive here), or None.
+
+        The workspace (dz, partial sums; workspace_bytes) belongs to the handle, this one or the one it allocates: its calls, and replays of graphs that hold
+        them, may overlap only where they need none or each was recorded with a workspace of its own, which the caller then keeps.
+        """
         if tensor is not None and not (tensor.is_cuda and tensor.is_contiguous()):
             raise ValueError("the workspace is a contiguous CUDA tensor")
         ptr, size = (0, 0) if tensor is None else (tensor.data_ptr(), tensor.numel() * tensor.element_size())
