@@ -7,6 +7,7 @@ taken twice or read from the wrong stage is 64 (32) terms of a sum of up to 1816
 import pytest
 import torch
 
+from paper_1903_06498_amd import binding as B
 from tests.test_gpu_layers import NAN, U, Linear, untouched, window
 
 pytestmark = pytest.mark.gpu
@@ -126,3 +127,20 @@ def test_f32_in_parts_with_some_tiles_that_are_computed_again(splits, monkeypatc
     assert not torch.isfinite(got[[0, 5, 6]]).any() and not torch.isfinite(got[:, [0, 5, 6]]).any()
     for name in ("y", "dx", "dw"):
         assert untouched(*c.outs[name], -7.0)
+
+
+def test_weight_gradient_of_more_than_two_billion_elements():
+    """dW beyond 2^31 elements, on 256 x 256 tiles: its first and last rows."""
+    rows, cin, cout = 200, 65544, 32776
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x, dy = (torch.randn(rows, n, generator=g, device="cuda").to(torch.bfloat16) for n in (cin, cout))
+    dw = torch.full((cout, cin), -7.0, dtype=torch.bfloat16, device="cuda")
+    op = B.StripeLinear(rows, cin, cout, "bf16")
+    assert "256x256" in op.info["weight_grad"]
+    op.backward(dy, x, None, dw=dw)
+    torch.cuda.synchronize()
+    for part in (slice(0, 40), slice(cout - 40, cout)):
+        v, terms = dy[:, part].double().t() @ x.double(), dy[:, part].double().abs().t() @ x.double().abs()
+        tol = (rows + 2) * U * terms
+        assert ((dw[part].double() - v).abs() <= tol + 2.0 ** -8 * (v.abs() + tol)).all()
+    assert not (dw == -7.0).all(1).any()
