@@ -4,9 +4,9 @@
 // Each row is read once into registers: 64, 256 or 512 lanes share a row, at most 32 elements each (longer rows are read again for
 // each sum).  Mean first, then the mean of the squared distances from it -- not E[x^2] - E[x]^2, which loses
 // what the mean's square has more digits than -- together with the mean distance, which is the first mean's rounding error, up to n 2^-24 |x| for its n
-// additions: without it, 3001 equal fp32 values 1000.1 came out as 0.1 gamma + beta.  Rows of bf16 do without it where they stay in registers (16384 x 4096 takes
-// 6 % longer with it, 32768 x 512 13 %; fp32 up to 2 %): where their spread is small beside their mean, the values are multiples of 2^-9 of the largest, and
-// sums of up to 2^15 of them are exact in fp32.  The backward pass keeps its columns' sums of dy h and dy in registers over all the
+// additions: without it, 16384 equal fp32 values 1000.1 came out as 0.1 gamma + beta (1000 of them: 0.04).  Rows of bf16 do without it where they stay in
+// registers (16384 x 4096 takes 6 % longer with it, 32768 x 512 13 %; fp32 up to 2 %): where their spread is small beside their mean, the values are
+// multiples of 2^-9 of the largest, and sums of up to 2^15 of them are exact in fp32.  The backward pass keeps its columns' sums of dy h and dy in registers over all the
 // rows that its workgroup takes, leaves one row of partial sums per workgroup and adds those in a second launch in a fixed order.
 #include <algorithm>
 
