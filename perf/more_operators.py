@@ -1,0 +1,511 @@
+"""The rest of a training step around the feed-forward block as measured cases: the gated unit, the cross entropy of a linear head over a
+vocabulary, and AdamW over many tensors.
+
+`own` false: the plain form, elementary torch operations in 32 bits, rounded once at the end.  `own` true: this package's calls.
+Formulas (x rows of `cin` features):
+
+    gated   [g | u] = x W^T (W [2 cout][cin]: gate rows, then up rows),  y = act(g) u;
+            dg = dy u act'(g),  du = dy act(g),  dz = [dg | du],  dx = dz W,  dW = dz^T x;
+            with groups rows offsets[e] .. offsets[e+1] - 1 meet W[e].  A training pass runs the forward operator and then the backward one, whose
+            g and u are an input of their own, as a schedule that alternates micro-batches has them.
+    loss    z = x W^T (W [classes][cin]),  lse = log sum exp z,  loss = lse - z[target];
+            dz = exp(z - lse) (dloss + dlse) - [class = target] dloss,  dx = dz W,  dW = dz^T x;
+            rows whose target is no class: loss = lse = 0, dx = 0, nothing in dW.
+    adamw   g = factor grad,  m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  p = p (1 - lr wd) - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps).
+            States in 8 bits, blocks of 256 elements of a tensor: m is a / 127^2 times c |c|, a the block's largest |m|, c in -127 .. 127; s = sqrt(v) is
+            a / 255^2 times c^2, c in 0 .. 255, a its largest s.  c is rounded at random to one of its two neighbours so that the value's mean is kept: to the
+            upper one where the value's place between them is beyond b / 2^16, b the lower (m) or upper (s) 16 bits of a hash of the element's number and
+            the tensor's, and of the call's seed.  An s that is not 0 has a c of 1 at least; a block whose a is at most 1e-30 is 0.
+"""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+SIZE = {"bf16": 2, "f32": 4}
+ACTIVATIONS = ("none", "relu", "gelu", "gelu_tanh", "silu")
+BLOCK = 256
+BETAS, EPS, LR, STEP = (0.9, 0.999), 1e-8, 1e-3, 100
+LARGEST = 6 * 8192 * 2048 * 65536       # operations of the largest listed product
+MOST_ELEMENTS = 160 << 20               # of the largest optimizer step
+
+
+def _gated(rows, cin, cout, dtype, act, train, groups=0):
+    return dict(op="gated", rows=rows, cin=cin, cout=cout, groups=groups, dtype=dtype, act=act, train=train)
+
+
+def _loss(rows, cin, classes, dtype, train, ignored=0.0, dlse=False):
+    return dict(op="loss", rows=rows, cin=cin, classes=classes, dtype=dtype, train=train, ignored=ignored, dlse=dlse)
+
+
+def _adamw(tensors, least, most, grads, states, copies):
+    return dict(op="adamw", tensors=tensors, least=least, most=most, grads=grads, states=states, copies=copies)
+
+
+def listed():
+    return [
+        # one token while answering: the latency of a call, and reading the weights
+        dict(_gated(1, 4096, 8192, "bf16", "silu", False), name="gated_token"),
+        # a prompt
+        dict(_gated(4096, 4096, 8192, "bf16", "silu", False), name="gated_prompt"),
+        # a training step's tokens
+        dict(_gated(8192, 2048, 4096, "bf16", "gelu_tanh", True), name="gated_train"),
+        # a training step of a layer of experts, rows sorted by expert
+        dict(_gated(8192, 1024, 2048, "bf16", "silu", True, 16), name="gated_experts_train"),
+        # a small layer in full precision with sizes that fit no tile and no vector
+        dict(_gated(777, 500, 1283, "f32", "silu", True), name="gated_train_odd_f32"),
+        # a few answers' tokens scored under a vocabulary
+        dict(_loss(16, 4096, 32768, "bf16", False), name="loss_score"),
+        # a training step: a tenth of the rows is padding or prompt, and lse has a gradient too, as a penalty on its size gives it
+        dict(_loss(8192, 2048, 65536, "bf16", True, 0.1, True), name="loss_train"),
+        # a step of tuning on few tokens, most of them prompt, with a vocabulary of no round size
+        dict(_loss(512, 4096, 50001, "bf16", True, 0.6), name="loss_tune"),
+        # a small model in full precision
+        dict(_loss(1000, 333, 10007, "f32", True, 0.1), name="loss_train_odd_f32"),
+        # the gains and biases of a small model: latency
+        dict(_adamw(24, 1, 8192, "f32", "f32", False), name="adamw_small"),
+        # a few layers' matrices, gradients and copies in bf16
+        dict(_adamw(16, 1 << 20, 16 << 20, "bf16", "f32", True), name="adamw_layers"),
+        # the same with states in 8 bits, read back as for a checkpoint
+        dict(_adamw(16, 1 << 20, 16 << 20, "bf16", "8bit", True), name="adamw_layers_8bit"),
+    ]
+
+
+def _log(rng, low, high):
+    return int(round(math.exp(rng.uniform(math.log(low), math.log(high)))))
+
+
+def _width(rng, low, high):
+    """A feature count: mostly whole vectors, as models have them, sometimes any number."""
+    n = _log(rng, low, high)
+    return n if rng.random() < 0.25 else max(8, n // 8 * 8)
+
+
+def draw(rng):
+    dtype = "bf16" if rng.random() < 0.7 else "f32"
+    train = rng.random() < 0.6
+    op = rng.choice(["gated", "gated", "loss", "loss", "adamw"])
+    # full precision costs the plain form as much, and gradients are two more products
+    most = (LARGEST if dtype == "bf16" else LARGEST // 8) // (6 if train else 2)
+    if op == "gated":
+        groups = rng.choice([0, 0, rng.randint(2, 64)])
+        while True:
+            rows, cin, cout = _log(rng, 1, 16384), _width(rng, 32, 8192), _width(rng, 32, 8192)
+            if 2 * rows * cin * cout <= most // 8 and max(1, groups) * 2 * cin * cout <= 128 << 20:
+                return _gated(rows, cin, cout, dtype, rng.choice(ACTIVATIONS), train, groups)
+    if op == "loss":
+        while True:
+            rows, cin, classes = _log(rng, 1, 16384), _width(rng, 32, 8192), _width(rng, 100, 131072)
+            if rows * cin * classes <= most and rows * classes <= 8192 * 65536 and cin * classes <= 256 << 20:
+                return _loss(rows, cin, classes, dtype, train, rng.choice([0.0, 0.1, 0.5]), train and rng.random() < 0.3)
+    while True:
+        tensors, least = _log(rng, 1, 100), _log(rng, 1, 4 << 20)
+        mean = least * math.exp(rng.uniform(0, 4))
+        if tensors * mean <= MOST_ELEMENTS / 4:
+            return _adamw(tensors, least, int(2 * mean), dtype, rng.choice(["f32", "8bit"]), rng.random() < 0.5)
+
+
+def _sizes(case):
+    """Elements of each tensor: spread over the logarithm of the range, odd ones among them, the same for every seed."""
+    r = np.random.RandomState(case["tensors"] * 7919 + case["least"])
+    n = np.exp(r.uniform(math.log(case["least"]), math.log(case["most"]), case["tensors"])).astype(np.int64)
+    n[0], n[-1] = case["least"], case["most"]
+    whole = r.rand(case["tensors"]) < 0.75
+    return [int(v // BLOCK * BLOCK) if w and v >= BLOCK else max(1, int(v)) for v, w in zip(n, whole)]
+
+
+# ---- inputs ------------------------------------------------------------------
+def prepare(case, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return {"gated": _prepare_gated, "loss": _prepare_loss, "adamw": _prepare_adamw}[case["op"]](case, seed, g)
+
+
+def _normal(g, *shape, scale=1.0, dtype=torch.float32):
+    return (torch.randn(*shape, generator=g, device="cuda") * scale).to(dtype)
+
+
+def _empty(*shape, dtype=torch.float32):
+    return torch.empty(*shape, device="cuda", dtype=dtype)
+
+
+def _with_workspace(op):
+    if op.workspace_bytes:
+        op.set_workspace(torch.empty(op.workspace_bytes, dtype=torch.uint8, device="cuda"))
+    return op
+
+
+def _prepare_gated(case, seed, g):
+    rows, k, n, e, dt = case["rows"], case["cin"], case["cout"], case["groups"], TYPES[case["dtype"]]
+    lead = (e,) if e else ()
+    s = dict(case=case, x=_normal(g, rows, k, dtype=dt), w=_normal(g, *lead, 2 * n, k, scale=k ** -0.5, dtype=dt), offsets=None, pre=None)
+    if e:
+        # an uneven share for each expert, and none for some
+        r = np.random.RandomState(seed % (1 << 32))
+        share = r.gamma(2.0, size=e) * (r.rand(e) > 0.1) + 1e-9
+        s["counts"] = r.multinomial(rows, share / share.sum())
+        s["offsets"] = torch.from_numpy(np.concatenate([[0], np.cumsum(s["counts"])]).astype(np.int32)).cuda()
+    s["y"] = _empty(rows, n, dtype=dt)
+    if case["train"]:
+        s["pre"], s["dy"], s["z"] = _empty(rows, 2 * n, dtype=dt), _normal(g, rows, n, dtype=dt), _normal(g, rows, 2 * n, dtype=dt)
+        s["dx"], s["dw"] = _empty(rows, k, dtype=dt), _empty(*lead, 2 * n, k, dtype=dt)
+    if own:
+        from paper_1903_06498_amd.binding import StripeGated
+        s["op"] = _with_workspace(StripeGated(rows, k, n, case["dtype"], activation=case["act"], groups=e))
+    return s
+
+
+def _prepare_loss(case, seed, g):
+    rows, k, n, dt = case["rows"], case["cin"], case["classes"], TYPES[case["dtype"]]
+    s = dict(case=case, w=_normal(g, n, k, scale=k ** -0.5, dtype=dt))
+    target = torch.randint(0, n, (rows,), generator=g, device="cuda")
+    # what the last norm gives, turned towards the target's row: some targets are sure, some are not
+    sure = torch.rand(rows, 1, generator=g, device="cuda") * 12
+    s["x"] = (_normal(g, rows, k) + sure * s["w"][target].float()).to(dt)
+    ignored = torch.rand(rows, generator=g, device="cuda") < case["ignored"]
+    s["targets"] = torch.where(ignored, torch.full_like(target, -100), target).to(torch.int32)
+    s["loss"], s["lse"] = _empty(rows), _empty(rows)
+    if case["train"]:
+        s["dloss"] = (0.5 + torch.rand(rows, generator=g, device="cuda")) / rows
+        s["dlse"] = torch.rand(rows, generator=g, device="cuda") * 1e-2 / rows if case["dlse"] else None
+        s["dx"], s["dw"] = _empty(rows, k, dtype=dt), _empty(n, k, dtype=dt)
+    if own:
+        from paper_1903_06498_amd.binding import StripeXent
+        s["op"] = _with_workspace(StripeXent(rows, k, n, case["dtype"]))
+    return s
+
+
+def _prepare_adamw(case, seed, g):
+    """Tensors are parts of flat buffers, each from a multiple of BLOCK elements on."""
+    sizes = _sizes(case)
+    blocks = [-(-n // BLOCK) for n in sizes]
+    total, all_blocks, eight = sum(blocks) * BLOCK, sum(blocks), case["states"] == "8bit"
+    tensor = torch.repeat_interleave(torch.arange(len(sizes)), torch.tensor(blocks)).cuda()
+    first = torch.tensor(np.concatenate([[0], np.cumsum(blocks)[:-1]]), device="cuda")
+    number = torch.arange(all_blocks, device="cuda") - first[tensor]            # of a block within its tensor
+    left = torch.tensor(sizes, device="cuda")[tensor] - number * BLOCK
+    real = (torch.arange(BLOCK, device="cuda") < left[:, None]).view(-1)
+    decay = [0.1 if n > BLOCK else 0.0 for n in sizes]
+    # tensors learn at very different rates, and one block in ten has had no gradient
+    size = torch.exp(_normal(g, len(sizes)) * 2 - 6)[tensor] * (torch.rand(all_blocks, generator=g, device="cuda") > 0.1)
+    size = size.repeat_interleave(BLOCK) * real
+    s = dict(case=case, tensor=tensor, number=number, seed=int(seed) * 2654435761 % (1 << 32), decay=torch.tensor(decay, device="cuda")[tensor])
+    s["p"] = _normal(g, total, scale=0.05) * real
+    s["grad"] = (_normal(g, total) * size).to(TYPES[case["grads"]])
+    s["copy"] = torch.zeros(total, device="cuda", dtype=torch.bfloat16) if case["copies"] else None
+    if eight:
+        s["m"] = torch.randint(-127, 128, (total,), generator=g, device="cuda", dtype=torch.int16).mul_(real).to(torch.int8)
+        s["v"] = torch.randint(1, 256, (total,), generator=g, device="cuda", dtype=torch.int16).mul_(real).to(torch.uint8)
+        s["m_scale"], s["v_scale"] = 0.3 * size[::BLOCK] / 16129, 1.5 * size[::BLOCK] / 65025
+        s["m_out"], s["v_out"] = _empty(total), _empty(total)
+    else:
+        s["m"] = _normal(g, total, scale=0.2) * size
+        s["v"] = torch.square(size) * (0.2 + torch.rand(total, generator=g, device="cuda"))
+        s["m_scale"] = s["v_scale"] = None
+    if own:
+        from paper_1903_06498_amd.binding import StripeAdamW
+        starts = [int(b) * BLOCK for b in first]
+
+        def parts(flat):
+            return None if flat is None else [flat[a:a + n] for a, n in zip(starts, sizes)]
+
+        def scales(flat):
+            return None if flat is None else [flat[a // BLOCK:a // BLOCK + b] for a, b in zip(starts, blocks)]
+
+        s["op"] = StripeAdamW(sizes, grads=case["grads"], states=case["states"], betas=BETAS, eps=EPS, weight_decay=decay)
+        s["op"].bind(parts(s["p"]), parts(s["grad"]), parts(s["m"]), parts(s["v"]), m_scales=scales(s["m_scale"]), v_scales=scales(s["v_scale"]),
+                     copies=parts(s["copy"]))
+        s["outs"] = (parts(s["m_out"]), parts(s["v_out"])) if eight else None
+    return s
+
+
+# ---- the package's calls ---------------------------------------------------
+def _run_own(s):
+    case, op = s["case"], s["op"]
+    if case["op"] == "gated":
+        op.run(s["x"], s["w"], s["y"], offsets=s["offsets"], pre=s["pre"])
+        out = {"y": s["y"]}
+        if case["train"]:
+            op.backward(s["dy"], s["x"], s["w"], s["z"], offsets=s["offsets"], dx=s["dx"], dw=s["dw"])
+            out.update(pre=s["pre"], dx=s["dx"], dw=s["dw"])
+        return out
+    if case["op"] == "loss":
+        op.run(s["x"], s["w"], s["targets"], s["loss"], s["lse"])
+        out = {"loss": s["loss"], "lse": s["lse"]}
+        if case["train"]:
+            op.backward(s["x"], s["w"], s["targets"], s["lse"], dloss=s["dloss"], dlse=s["dlse"], dx=s["dx"], dw=s["dw"])
+            out.update(dx=s["dx"], dw=s["dw"])
+        return out
+    op.run(LR, STEP, seed=s["seed"])
+    if s["outs"]:
+        op.read(*s["outs"])
+    return _adamw_outputs(s)
+
+
+def _adamw_outputs(s):
+    eight = s["case"]["states"] == "8bit"
+    out = {"p": s["p"], "m": s["m_out"] if eight else s["m"], "v": s["v_out"] if eight else s["v"]}
+    if s["copy"] is not None:
+        out["copy"] = s["copy"]
+    return out
+
+
+# ---- the plain form --------------------------------------------------------
+def _act(z, name):
+    if name == "relu":
+        return torch.where(z > 0, z, torch.zeros_like(z))
+    if name == "gelu":
+        return 0.5 * z * (1 + torch.erf(z * math.sqrt(0.5)))
+    if name == "gelu_tanh":
+        return 0.5 * z * (1 + torch.tanh(math.sqrt(2 / math.pi) * (z + 0.044715 * z * z * z)))
+    if name == "silu":
+        return z / (1 + torch.exp(-z))
+    return z
+
+
+def _slope(z, name):
+    if name == "relu":
+        return (z > 0).to(z.dtype)
+    if name == "gelu":
+        return 0.5 * (1 + torch.erf(z * math.sqrt(0.5))) + z * torch.exp(-0.5 * z * z) * (1 / math.sqrt(2 * math.pi))
+    if name == "gelu_tanh":
+        a = math.sqrt(2 / math.pi)
+        t = torch.tanh(a * (z + 0.044715 * z * z * z))
+        return 0.5 * (1 + t) + 0.5 * z * (1 - t * t) * a * (1 + 3 * 0.044715 * z * z)
+    if name == "silu":
+        p = 1 / (1 + torch.exp(-z))
+        return p * (1 + z * (1 - p))
+    return torch.ones_like(z)
+
+
+def _padded(rows, at, groups, longest):
+    out = torch.zeros(groups * longest, rows.shape[1], device="cuda")
+    out[at] = rows
+    return out.view(groups, longest, rows.shape[1])
+
+
+def _plain_gated(s):
+    case = s["case"]
+    dt, e, n, act = TYPES[case["dtype"]], case["groups"], case["cout"], case["act"]
+    x, w = s["x"].float(), s["w"].float()
+    if e:
+        # each row's place in a padded [groups][longest group] layout
+        group = torch.searchsorted(s["offsets"][1:], torch.arange(case["rows"], device="cuda", dtype=torch.int32), right=True)
+        longest = int(s["counts"].max())
+        at = group * longest + torch.arange(case["rows"], device="cuda") - s["offsets"][group]
+        xp = _padded(x, at, e, longest)
+        z = torch.bmm(xp, w.transpose(1, 2).contiguous()).view(e * longest, -1)[at]
+    else:
+        z = x @ w.t()
+    out = {"y": (_act(z[:, :n], act) * z[:, n:]).to(dt)}
+    if case["train"]:
+        out["pre"] = z.to(dt)
+        dy, gate, up = s["dy"].float(), s["z"][:, :n].float(), s["z"][:, n:].float()
+        dz = torch.cat([dy * up * _slope(gate, act), dy * _act(gate, act)], 1)
+        if e:
+            dp = _padded(dz, at, e, longest)
+            dx, dw = torch.bmm(dp, w).view(e * longest, -1)[at], torch.bmm(dp.transpose(1, 2).contiguous(), xp)
+        else:
+            dx, dw = dz @ w, dz.t() @ x
+        out.update(dx=dx.to(dt), dw=dw.to(dt))
+    return out
+
+
+def _plain_loss(s):
+    case = s["case"]
+    dt, n = TYPES[case["dtype"]], case["classes"]
+    x, w, target = s["x"].float(), s["w"].float(), s["targets"].long()
+    counts = (target >= 0) & (target < n)
+    z = x @ w.t()
+    top = z.max(1, keepdim=True).values
+    lse = top + torch.log(torch.exp(z - top).sum(1, keepdim=True))
+    at = torch.where(counts, target, torch.zeros_like(target))[:, None]
+    zero = torch.zeros_like(lse[:, 0])
+    out = {"loss": torch.where(counts, lse[:, 0] - z.gather(1, at)[:, 0], zero), "lse": torch.where(counts, lse[:, 0], zero)}
+    if case["train"]:
+        dloss = torch.where(counts, s["dloss"], zero)
+        both = dloss if s["dlse"] is None else torch.where(counts, s["dloss"] + s["dlse"], zero)
+        dz = torch.exp(z - lse) * both[:, None]
+        dz.scatter_(1, at, dz.gather(1, at) - dloss[:, None])
+        out.update(dx=(dz @ w).to(dt), dw=(dz.t() @ x).to(dt))
+    return out
+
+
+def _hash(x):
+    """MurmurHash3's finalizer on 32-bit values held in 64 bits."""
+    low = 0xffffffff
+    x = x ^ (x >> 16)
+    x = (x * 0x85ebca6b) & low
+    x = x ^ (x >> 13)
+    x = (x * 0xc2b2ae35) & low
+    return x ^ (x >> 16)
+
+
+def _coded(value, most, bits, least):
+    """Codes of a block's values (a row each; not negative), and the factor of their squares."""
+    top = value.max(1, keepdim=True).values
+    fine = top > 1e-30
+    scale = torch.where(fine, top * (1 / most ** 2), torch.zeros_like(top))
+    t = value * torch.where(fine, torch.reciprocal(top) * most ** 2, torch.zeros_like(top))
+    low = torch.floor(torch.sqrt(t))
+    up = (t - low * low) > (bits.float() * 2.0 ** -16) * (2 * low + 1)
+    return torch.maximum(torch.clamp(low + up, max=most), least * (t > 0)), scale
+
+
+def _plain_adamw(s):
+    case = s["case"]
+    (b1, b2), eight = BETAS, case["states"] == "8bit"
+    g = s["grad"].float().view(-1, BLOCK)
+    if eight:
+        c = s["m"].float().view(-1, BLOCK)
+        m = c * torch.abs(c) * s["m_scale"][:, None]
+        c = s["v"].float().view(-1, BLOCK)
+        r = c * c * s["v_scale"][:, None]
+        v = r * r
+    else:
+        m, v = s["m"].view(-1, BLOCK), s["v"].view(-1, BLOCK)
+    m = m * b1 + g * (1 - b1)
+    v = v * b2 + (g * g) * (1 - b2)
+    r = torch.sqrt(v)
+    p = s["p"].view(-1, BLOCK)
+    step = (m * (LR / (1 - b1 ** STEP))) / (r * (1 / math.sqrt(1 - b2 ** STEP)) + EPS)
+    s["p"].copy_((p * (1 - LR * s["decay"])[:, None] - step).view(-1))
+    if s["copy"] is not None:
+        s["copy"].copy_(s["p"])
+    if eight:
+        key = _hash((s["seed"] + s["tensor"]) & 0xffffffff)
+        bits = _hash((key[:, None] + s["number"][:, None] * BLOCK + torch.arange(BLOCK, device="cuda")) & 0xffffffff)
+        c, scale = _coded(torch.abs(m), 127, bits & 0xffff, 0)
+        c = torch.where(m < 0, -c, c)
+        s["m"].copy_(c.view(-1))
+        s["m_scale"].copy_(scale[:, 0])
+        s["m_out"].copy_((c * torch.abs(c) * scale).view(-1))
+        c, scale = _coded(r, 255, bits >> 16, 1)
+        s["v"].copy_(c.view(-1))
+        s["v_scale"].copy_(scale[:, 0])
+        r = c * c * scale
+        s["v_out"].copy_((r * r).view(-1))
+    else:
+        s["m"].copy_(m.view(-1))
+        s["v"].copy_(v.view(-1))
+    return _adamw_outputs(s)
+
+
+def run(state):
+    if own:
+        return _run_own(state)
+    return {"gated": _plain_gated, "loss": _plain_loss, "adamw": _plain_adamw}[state["case"]["op"]](state)
+
+
+def work(case):
+    if case["op"] == "adamw":
+        n = sum(_sizes(case))
+        size = 8 + SIZE[case["grads"]] + (2 if case["copies"] else 0) + (16 if case["states"] == "f32" else 4)
+        if case["states"] == "8bit":        # and read back
+            size += 2 + 8
+        return {"bytes": n * size, "flops": 20 * n}
+    size, m, k = SIZE[case["dtype"]], case["rows"], case["cin"]
+    if case["op"] == "gated":
+        n, e = case["cout"], case["groups"]
+        used = min(max(1, e), m)      # weight matrices that some row meets, at most
+        moved, flops = size * (m * k + used * 2 * n * k + m * n), 4 * m * n * k
+        if case["train"]:             # g and u are stored; dy, others' g and u, x and W are read, dx and dW written
+            moved += size * (2 * m * n + 3 * m * n + 2 * m * k + (used + max(1, e)) * 2 * n * k)
+            flops *= 3
+        return {"bytes": moved, "flops": flops}
+    n = case["classes"]
+    m = max(1, round(m * (1 - case["ignored"])))      # rows that count
+    moved, flops = size * (m * k + n * k) + 12 * case["rows"], 2 * m * n * k
+    if case["train"]:
+        moved, flops = moved + size * (2 * m * k + 2 * n * k) + 12 * case["rows"], 3 * flops
+    return {"bytes": moved, "flops": flops}
+
+
+# ---- the definition in 64 bits ---------------------------------------------
+def _exact_act(z, name):
+    """Value and derivative."""
+    if name == "relu":
+        return z.clamp(min=0), torch.heaviside(z, torch.zeros_like(z))
+    if name == "gelu":
+        cdf = torch.special.ndtr(z)
+        return z * cdf, cdf + z * torch.exp(-z.square() / 2) / math.sqrt(2 * math.pi)
+    if name == "gelu_tanh":      # 1/2 (1 + tanh(u)) = sigmoid(2u)
+        u2 = 2 * math.sqrt(2 / math.pi) * (z + 0.044715 * z.pow(3))
+        p = torch.sigmoid(u2)
+        return z * p, p + z * p * (1 - p) * 2 * math.sqrt(2 / math.pi) * (1 + 0.134145 * z.square())
+    if name == "silu":
+        p = torch.sigmoid(z)
+        return z * p, p + z * p * (1 - p)
+    return z, torch.ones_like(z)
+
+
+def _exact_gated(s):
+    case, n = s["case"], s["case"]["cout"]
+    x, w = s["x"].double(), s["w"].double()
+    ends = s["offsets"].tolist() if case["groups"] else [0, case["rows"]]
+    w = w if case["groups"] else w[None]
+    spans = list(enumerate(zip(ends, ends[1:])))
+    z = x.new_zeros(case["rows"], 2 * n)
+    for g, (a, b) in spans:
+        z[a:b] = torch.mm(x[a:b], w[g].t())
+    out = {"y": _exact_act(z[:, :n], case["act"])[0].mul(z[:, n:])}
+    if case["train"]:
+        value, slope = _exact_act(s["z"][:, :n].double(), case["act"])
+        dz = torch.hstack((s["z"][:, n:].double() * slope, value)) * s["dy"].double().repeat(1, 2)
+        dx, dw = torch.zeros_like(x), torch.zeros_like(w)
+        for g, (a, b) in spans:
+            dx[a:b], dw[g] = torch.mm(dz[a:b], w[g]), torch.mm(dz[a:b].t(), x[a:b])
+        out.update(pre=z, dx=dx, dw=dw.view(s["w"].shape))
+    return out
+
+
+def _exact_loss(s):
+    case = s["case"]
+    rows = torch.nonzero((s["targets"] >= 0) & (s["targets"] < case["classes"]))[:, 0]
+    w = s["w"].double()
+    f64 = dict(dtype=torch.float64, device="cuda")
+    out = {"loss": torch.zeros(case["rows"], **f64), "lse": torch.zeros(case["rows"], **f64)}
+    if case["train"]:
+        out["dx"], out["dw"] = torch.zeros(s["x"].shape, **f64), torch.zeros(s["w"].shape, **f64)
+    for some in rows.split(2048):      # some rows at a time: a matrix of all their values in 64 bits is large
+        x, target = s["x"][some].double(), s["targets"][some].long()
+        z = torch.mm(x, w.t())
+        lse = torch.logsumexp(z, 1)
+        own_z = z[torch.arange(len(some), device="cuda"), target]
+        out["loss"][some], out["lse"][some] = lse - own_z, lse
+        if case["train"]:
+            weight = s["dloss"][some].double()
+            total = weight if s["dlse"] is None else weight + s["dlse"][some].double()
+            dz = torch.softmax(z, 1).mul_(total[:, None])
+            dz[torch.arange(len(some), device="cuda"), target] -= weight
+            out["dx"][some] = torch.mm(dz, w)
+            out["dw"].addmm_(dz.t(), x)
+    return out
+
+
+def _exact_adamw(s):
+    """States in 8 bits have no such value after the step: where they are rounded to hangs on their last bit."""
+    case, eight = s["case"], s["case"]["states"] == "8bit"
+    grad = s["grad"].double()
+    if eight:
+        wide = torch.repeat_interleave(torch.stack([s["m_scale"], s["v_scale"]]).double(), BLOCK, dim=1)
+        m, v = s["m"].double() * s["m"].double().abs() * wide[0], (s["v"].double().square() * wide[1]).square()
+    else:
+        m, v = s["m"].double(), s["v"].double()
+    m, v = torch.lerp(grad, m, BETAS[0]), torch.lerp(grad.square(), v, BETAS[1])
+    rate = m.div(1 - BETAS[0] ** STEP) / (v.div(1 - BETAS[1] ** STEP).sqrt() + EPS)
+    p = s["p"].double()
+    p = p - LR * (rate + s["decay"].double().repeat_interleave(BLOCK) * p)
+    out = {"p": p, "m": None if eight else m, "v": None if eight else v}
+    if s["copy"] is not None:
+        out["copy"] = p
+    return out
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return {"gated": _exact_gated, "loss": _exact_loss, "adamw": _exact_adamw}[case["op"]](s)
