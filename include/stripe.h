@@ -289,7 +289,8 @@ stripe_status_t stripe_device_mfma(const void* operands, void* out, int iters, i
  * Layers: the operators of a transformer's feed-forward block that are no
  * single Stripe block -- the linear layer with its epilogue, the same over
  * rows sorted by expert (a data-dependent, hence not affine, index space), the
- * layer norm -- each with its gradients.  Handles work like those of blocks:
+ * layer norm, the gated unit, the cross entropy of a linear head -- each with its
+ * gradients, and the step of the optimizer, AdamW.  Handles work like those of blocks:
  * create() validates and plans on the host, run() / backward() enqueue on
  * `hip_stream` of the current device and return, the workspace is the caller's
  * (set_workspace) or the handle's.
@@ -396,6 +397,125 @@ stripe_status_t stripe_norm_backward(stripe_norm_t* norm, const void* dy, const 
 stripe_status_t stripe_norm_workspace_size(const stripe_norm_t* norm, size_t* bytes);
 stripe_status_t stripe_norm_set_workspace(stripe_norm_t* norm, void* device_ptr, size_t bytes);
 void stripe_norm_destroy(stripe_norm_t* norm);
+
+/*
+ * Gated unit:  [g | u] = x W^T,  y = act(g) u,  and its gradients for a given dy
+ *   dg = dy u act'(g),  du = dy act(g),  dz = [dg | du],  dx = dz W,  dW = dz^T x.
+ * x [rows][in_features], y [rows][out_features]; W [2 out_features][in_features]: the gate's rows, then up's; pre = [g | u], [rows][2 out_features].
+ * groups > 0: rows sorted by expert, W [groups][2 out_features][in_features] and `offsets` as for the linear layer.
+ * y is computed from g and u as they were before pre's rounding; dz is rounded to the operands' type before its products.
+ */
+typedef struct {
+  int64_t rows;                        /* 0 .. 2^28 */
+  int64_t in_features, out_features;   /* 1 .. 2^24, 1 .. 2^23 */
+  int32_t groups;                      /* 0: one matrix for all rows; else 1 .. 4096 matrices */
+  stripe_dtype_t dtype;                /* of x, W, y, pre, dy, dx, dW: STRIPE_BF16 or STRIPE_F32 */
+  stripe_activation_t activation;      /* STRIPE_ACT_NONE: y = g u */
+  /* Strides in elements, 0 = dense.  x_row: rows of x and dx; w_row, w_group: rows and matrices of W and dW; y_row: rows of y and dy;
+   * pre_row: rows of pre. */
+  int64_t x_row, w_row, w_group, y_row, pre_row;
+} stripe_gated_desc_t;
+
+typedef struct stripe_gated stripe_gated_t;
+
+stripe_status_t stripe_gated_create(const stripe_gated_desc_t* desc, stripe_gated_t** out);
+
+/* offsets: NULL without groups.  pre may be NULL (not stored); it receives g and u in `dtype`, for a later backward pass. */
+stripe_status_t stripe_gated_run(stripe_gated_t* gated, const void* x, const void* w, const int32_t* offsets, void* y, void* pre, void* hip_stream);
+
+/* pre: as run() stored it.  dx, dw: either of them may be NULL (not computed), then w or x may be NULL. */
+stripe_status_t stripe_gated_backward(stripe_gated_t* gated, const void* dy, const void* x, const void* w, const void* pre, const int32_t* offsets, void* dx,
+                                      void* dw, void* hip_stream);
+
+stripe_status_t stripe_gated_workspace_size(const stripe_gated_t* gated, size_t* bytes);
+stripe_status_t stripe_gated_set_workspace(stripe_gated_t* gated, void* device_ptr, size_t bytes);
+stripe_status_t stripe_gated_query(const stripe_gated_t* gated, stripe_linear_info_t* info);
+void stripe_gated_destroy(stripe_gated_t* gated);
+
+/*
+ * Softmax cross entropy of a linear head, e.g. over a vocabulary, without keeping its logits:
+ *   z = x W^T,  lse = log(sum of exp(z) over the classes),  loss = lse - z[target];
+ *   dz = exp(z - lse) (dloss + dlse) - [class = target] dloss,  dx = dz W,  dW = dz^T x.
+ * x [rows][in_features], W [classes][in_features]; targets [rows]: int32 on the DEVICE; loss, lse, dloss, dlse [rows]: fp32.
+ * A row whose target is not one of 0 .. classes - 1 does not count: x is not read there (it may hold anything), loss, lse and dx are 0, and dW
+ * has nothing of it.  The backward pass computes z again, a piece of the vocabulary at a time; a piece's dz is in the workspace, rounded
+ * to the operands' type.  dx is added up in fp32 over the pieces.
+ */
+typedef struct {
+  int64_t rows;             /* 0 .. 2^24 */
+  int64_t in_features;      /* 1 .. 2^20 */
+  int64_t classes;          /* 1 .. 2^24 */
+  stripe_dtype_t dtype;     /* of x, W, dx, dW: STRIPE_BF16 or STRIPE_F32 */
+  int64_t x_row, w_row;     /* strides in elements, 0 = dense: rows of x and dx, rows of W and dW */
+} stripe_xent_desc_t;
+
+typedef struct stripe_xent stripe_xent_t;
+
+stripe_status_t stripe_xent_create(const stripe_xent_desc_t* desc, stripe_xent_t** out);
+
+/* loss, lse: either of them may be NULL. */
+stripe_status_t stripe_xent_run(stripe_xent_t* xent, const void* x, const void* w, const int32_t* targets, float* loss, float* lse, void* hip_stream);
+
+/* lse: as run() stored it for the same x, W and targets.  dloss: the gradient of every row's loss, NULL: ones; dlse: that of lse, NULL: zeros.
+ * dx, dw: either of them may be NULL. */
+stripe_status_t stripe_xent_backward(stripe_xent_t* xent, const void* x, const void* w, const int32_t* targets, const float* lse, const float* dloss,
+                                     const float* dlse, void* dx, void* dw, void* hip_stream);
+
+stripe_status_t stripe_xent_workspace_size(const stripe_xent_t* xent, size_t* bytes);
+stripe_status_t stripe_xent_set_workspace(stripe_xent_t* xent, void* device_ptr, size_t bytes);
+void stripe_xent_destroy(stripe_xent_t* xent);
+
+/*
+ * AdamW over many tensors:  with t = step and g = factor grad,
+ *   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  p = p (1 - lr wd) - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps).
+ * p, m, v are updated in place; `copy`, where a tensor has one, receives p in bf16.  All tensors are contiguous.
+ * state_dtype STRIPE_F32: m, v fp32.  STRIPE_I8: blocks of 256 consecutive elements; m is m_scale[block] c |c| with c = m[i] in -127 .. 127 (int8), the square
+ * root of v is v_scale[block] c^2 with c = v[i] in 0 .. 255 (uint8); m_scale, v_scale: fp32, ceil(elements / 256).  All zeros is the state before the first
+ * step.  A value between two codes becomes one of them at random, such that its mean is kept (a square root of v that is not 0 does not become 0); the random
+ * bits are a hash of (seed, the tensor's number, the element's), so that the same call gives the same bits: give every step another seed.  A block whose
+ * largest value is at most 1e-30 becomes 0, one that holds a value that is not finite becomes NaN as a whole.  p's update uses m and v
+ * before they are coded.
+ */
+typedef struct {
+  int32_t tensors;                  /* 0 .. 2^20 */
+  const int64_t* elements;          /* [tensors], 0 .. 2^34 */
+  const double* weight_decay;       /* [tensors] wd, or NULL: 0 */
+  stripe_dtype_t grad_dtype;        /* STRIPE_BF16 or STRIPE_F32 */
+  stripe_dtype_t state_dtype;       /* STRIPE_F32 or STRIPE_I8 */
+  double beta1, beta2;              /* 0 <= b < 1 */
+  double eps;                       /* >= 0 and finite */
+} stripe_adamw_desc_t;
+
+typedef struct {
+  float* p;
+  const void* grad;
+  void *m, *v;
+  float *m_scale, *v_scale;         /* STRIPE_I8 only, else NULL */
+  void* copy;                       /* bf16, or NULL */
+} stripe_adamw_tensor_t;
+
+typedef struct {
+  double lr;
+  int64_t step;                     /* t: 1 .. 2^53 */
+  double factor;                    /* of the gradients, e.g. what limits their norm; 1: none */
+  uint32_t seed;                    /* STRIPE_I8 */
+  /* NULL, or five 4-byte values on the DEVICE that are read when the step runs, in place of the four above (which are then ignored): fp32 lr,
+   * 1 / (1 - b1^t), 1 / sqrt(1 - b2^t), factor; uint32 seed.  For steps that are captured once and replayed. */
+  const void* control;
+} stripe_adamw_step_t;
+
+typedef struct stripe_adamw stripe_adamw_t;
+
+stripe_status_t stripe_adamw_create(const stripe_adamw_desc_t* desc, stripe_adamw_t** out);
+
+/* The tensors that the steps update, desc.tensors of them (the pointers of one without elements are not looked at): kept until the next call of bind(),
+ * which no step may overlap on the host.  No buffer may be bound twice (the same address is refused), but two gradients may be one. */
+stripe_status_t stripe_adamw_bind(stripe_adamw_t* adamw, const stripe_adamw_tensor_t* tensors);
+stripe_status_t stripe_adamw_run(stripe_adamw_t* adamw, const stripe_adamw_step_t* step, void* hip_stream);
+
+/* The values that bound states of STRIPE_I8 stand for: m[i], v[i] receive those of tensor i in fp32 (NULL, or NULL entries: not wanted). */
+stripe_status_t stripe_adamw_read(stripe_adamw_t* adamw, float* const* m, float* const* v, void* hip_stream);
+void stripe_adamw_destroy(stripe_adamw_t* adamw);
 
 /* ------------------------------------------------------------------------
  * Autotiling (paper Section 3.3, Figures 4 and 5): host-only integer code.

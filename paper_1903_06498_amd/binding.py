@@ -35,7 +35,11 @@ EXPORTS = ("stripe_block_create", "stripe_block_create_for_path", "stripe_block_
            "stripe_tile_cost", "stripe_tile_search", "stripe_block_tile", "stripe_desc_free",
            "stripe_linear_create", "stripe_linear_run", "stripe_linear_backward", "stripe_linear_workspace_size", "stripe_linear_set_workspace",
            "stripe_linear_query", "stripe_linear_destroy", "stripe_norm_create", "stripe_norm_run", "stripe_norm_backward",
-           "stripe_norm_workspace_size", "stripe_norm_set_workspace", "stripe_norm_destroy")
+           "stripe_norm_workspace_size", "stripe_norm_set_workspace", "stripe_norm_destroy",
+           "stripe_gated_create", "stripe_gated_run", "stripe_gated_backward", "stripe_gated_workspace_size", "stripe_gated_set_workspace",
+           "stripe_gated_query", "stripe_gated_destroy", "stripe_xent_create", "stripe_xent_run", "stripe_xent_backward",
+           "stripe_xent_workspace_size", "stripe_xent_set_workspace", "stripe_xent_destroy",
+           "stripe_adamw_create", "stripe_adamw_bind", "stripe_adamw_run", "stripe_adamw_read", "stripe_adamw_destroy")
 
 
 class stripe_refinement_t(C.Structure):
@@ -88,6 +92,28 @@ class stripe_linear_info_t(C.Structure):
 
 class stripe_norm_desc_t(C.Structure):
     _fields_ = [("rows", C.c_int64), ("features", C.c_int64), ("dtype", C.c_int), ("eps", C.c_double), ("x_row", C.c_int64), ("y_row", C.c_int64)]
+
+
+class stripe_gated_desc_t(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("in_features", C.c_int64), ("out_features", C.c_int64), ("groups", C.c_int32), ("dtype", C.c_int),
+                ("activation", C.c_int), ("x_row", C.c_int64), ("w_row", C.c_int64), ("w_group", C.c_int64), ("y_row", C.c_int64), ("pre_row", C.c_int64)]
+
+
+class stripe_xent_desc_t(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("in_features", C.c_int64), ("classes", C.c_int64), ("dtype", C.c_int), ("x_row", C.c_int64), ("w_row", C.c_int64)]
+
+
+class stripe_adamw_desc_t(C.Structure):
+    _fields_ = [("tensors", C.c_int32), ("elements", C.POINTER(C.c_int64)), ("weight_decay", C.POINTER(C.c_double)), ("grad_dtype", C.c_int),
+                ("state_dtype", C.c_int), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double)]
+
+
+class stripe_adamw_tensor_t(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in ("p", "grad", "m", "v", "m_scale", "v_scale", "copy")]
+
+
+class stripe_adamw_step_t(C.Structure):
+    _fields_ = [("lr", C.c_double), ("step", C.c_int64), ("factor", C.c_double), ("seed", C.c_uint32), ("control", C.c_void_p)]
 
 
 class StripeError(RuntimeError):
@@ -148,13 +174,19 @@ def _load():
     lib.stripe_desc_free.restype = None
     lib.stripe_desc_free.argtypes = [C.POINTER(stripe_block_desc_t)]
     ptr = C.c_void_p
-    for name, desc, run, backward in (("linear", stripe_linear_desc_t, 8, 9), ("norm", stripe_norm_desc_t, 7, 9)):
+    for name, desc, run, backward in (("linear", stripe_linear_desc_t, 8, 9), ("norm", stripe_norm_desc_t, 7, 9), ("gated", stripe_gated_desc_t, 6, 8),
+                                      ("xent", stripe_xent_desc_t, 6, 9)):
         for call, args in (("create", [C.POINTER(desc), C.POINTER(handle)]), ("run", [handle] + [ptr] * run), ("backward", [handle] + [ptr] * backward),
                            ("workspace_size", [handle, C.POINTER(C.c_size_t)]), ("set_workspace", [handle, ptr, C.c_size_t]), ("destroy", [handle])):
             f = getattr(lib, f"stripe_{name}_{call}")
             f.restype, f.argtypes = None if call == "destroy" else C.c_int, args
-    lib.stripe_linear_query.restype = C.c_int
-    lib.stripe_linear_query.argtypes = [handle, C.POINTER(stripe_linear_info_t)]
+    for name in ("linear", "gated"):
+        f = getattr(lib, f"stripe_{name}_query")
+        f.restype, f.argtypes = C.c_int, [handle, C.POINTER(stripe_linear_info_t)]
+    for call, args in (("create", [C.POINTER(stripe_adamw_desc_t), C.POINTER(handle)]), ("bind", [handle, C.POINTER(stripe_adamw_tensor_t)]),
+                       ("run", [handle, C.POINTER(stripe_adamw_step_t), ptr]), ("read", [handle, C.POINTER(ptr), C.POINTER(ptr), ptr]), ("destroy", [handle])):
+        f = getattr(lib, f"stripe_adamw_{call}")
+        f.restype, f.argtypes = None if call == "destroy" else C.c_int, args
     return lib
 
 
@@ -447,11 +479,50 @@ def stripe_linear_create(rows: int, in_features: int, out_features: int, dtype: 
     return h
 
 
-def stripe_linear_query(handle) -> dict:
+def _layer_info(query, handle) -> dict:
     info = stripe_linear_info_t()
-    _check(lib.stripe_linear_query(handle, C.byref(info)))
+    _check(query(handle, C.byref(info)))
     return {"forward": info.forward.decode(), "input_grad": info.input_grad.decode(), "weight_grad": info.weight_grad.decode(),
             "workspace_bytes": info.workspace_bytes}
+
+
+def stripe_linear_query(handle) -> dict:
+    return _layer_info(lib.stripe_linear_query, handle)
+
+
+def stripe_gated_create(rows: int, in_features: int, out_features: int, dtype: str, activation: str = "silu", groups: int = 0, x_row: int = 0,
+                        w_row: int = 0, w_group: int = 0, y_row: int = 0, pre_row: int = 0) -> C.c_void_p:
+    d = stripe_gated_desc_t(int(rows), int(in_features), int(out_features), int(groups), _DTYPE[dtype], _ACT[activation], int(x_row), int(w_row),
+                            int(w_group), int(y_row), int(pre_row))
+    h = C.c_void_p()
+    _check(lib.stripe_gated_create(C.byref(d), C.byref(h)))
+    return h
+
+
+def stripe_gated_query(handle) -> dict:
+    return _layer_info(lib.stripe_gated_query, handle)
+
+
+def stripe_xent_create(rows: int, in_features: int, classes: int, dtype: str, x_row: int = 0, w_row: int = 0) -> C.c_void_p:
+    d = stripe_xent_desc_t(int(rows), int(in_features), int(classes), _DTYPE[dtype], int(x_row), int(w_row))
+    h = C.c_void_p()
+    _check(lib.stripe_xent_create(C.byref(d), C.byref(h)))
+    return h
+
+
+_STATES = {"f32": "f32", "8bit": "i8"}
+
+
+def stripe_adamw_create(elements: Sequence[int], weight_decay: Sequence[float], grads: str = "f32", states: str = "f32", beta1: float = 0.9,
+                        beta2: float = 0.999, eps: float = 1e-8) -> C.c_void_p:
+    n = len(elements)
+    if len(weight_decay) != n:
+        raise ValueError("weight_decay needs one entry per tensor")
+    d = stripe_adamw_desc_t(n, (C.c_int64 * max(1, n))(*[int(v) for v in elements]), (C.c_double * max(1, n))(*[float(v) for v in weight_decay]),
+                            _DTYPE[grads], _DTYPE[_STATES.get(states, states)], float(beta1), float(beta2), float(eps))
+    h = C.c_void_p()
+    _check(lib.stripe_adamw_create(C.byref(d), C.byref(h)))
+    return h
 
 
 def stripe_norm_create(rows: int, features: int, dtype: str, eps: float = 1e-5, x_row: int = 0, y_row: int = 0) -> C.c_void_p:
@@ -595,3 +666,165 @@ class StripeNorm(_Layer):
                                       current_stream() if stream is None else stream)
         if st != STRIPE_OK:
             raise StripeError(st, stripe_last_error())
+
+
+class StripeGated(_Layer):
+    """Gated unit y = act(g) u, [g | u] = x W^T, and its gradients (see include/stripe.h); owns one handle.
+
+    w [2 out][in]: the gate's rows, then up's; pre [rows][2 out].  groups > 0: rows sorted by expert, w [groups][2 out][in], offsets int32 [groups + 1].
+    Strides (x_row, w_row, w_group, y_row, pre_row; 0 = dense) are in elements: x_row of x and dx, w_row and w_group of w and dw, y_row of y and dy.
+    """
+
+    _name = "gated"
+
+    def __init__(self, rows: int, in_features: int, out_features: int, dtype: str = "bf16", activation: str = "silu", groups: int = 0, x_row: int = 0,
+                 w_row: int = 0, w_group: int = 0, y_row: int = 0, pre_row: int = 0):
+        self.handle = None
+        self._open(stripe_gated_create(rows, in_features, out_features, dtype, activation, groups, x_row, w_row, w_group, y_row, pre_row), dtype)
+        self.info = stripe_gated_query(self.handle)
+        w_row, both = w_row or in_features, 2 * out_features
+        lead, lead_stride = ((groups,), (w_group or both * w_row,)) if groups else ((), ())
+        self._x = ((rows, in_features), (x_row or in_features, 1))
+        self._y = ((rows, out_features), (y_row or out_features, 1))
+        self._p = ((rows, both), (pre_row or both, 1))
+        self._w = (lead + (both, in_features), lead_stride + (w_row, 1))
+        self._o = ((groups + 1,), (1,))
+
+    def run(self, x, w, y, offsets=None, pre=None, stream: Optional[int] = None) -> None:
+        """y = act(g) u; pre (optional) receives g and u for a backward pass."""
+        dev, p, t = self._current(), self._ptr, self._dtype
+        st = lib.stripe_gated_run(self.handle, p("x", x, t, *self._x, dev), p("w", w, t, *self._w, dev), p("offsets", offsets, self._i32, *self._o, dev),
+                                  p("y", y, t, *self._y, dev), p("pre", pre, t, *self._p, dev), current_stream() if stream is None else stream)
+        if st != STRIPE_OK:
+            raise StripeError(st, stripe_last_error())
+
+    def backward(self, dy, x, w, pre, offsets=None, dx=None, dw=None, stream: Optional[int] = None) -> None:
+        """The gradients that are given a tensor: dx, dw."""
+        dev, p, t = self._current(), self._ptr, self._dtype
+        st = lib.stripe_gated_backward(self.handle, p("dy", dy, t, *self._y, dev), p("x", x, t, *self._x, dev), p("w", w, t, *self._w, dev),
+                                       p("pre", pre, t, *self._p, dev), p("offsets", offsets, self._i32, *self._o, dev), p("dx", dx, t, *self._x, dev),
+                                       p("dw", dw, t, *self._w, dev), current_stream() if stream is None else stream)
+        if st != STRIPE_OK:
+            raise StripeError(st, stripe_last_error())
+
+
+class StripeXent(_Layer):
+    """Softmax cross entropy of a linear head, loss = log sum exp(x W^T) - (x W^T)[target], and its gradients, without keeping the logits (see
+    include/stripe.h); owns one handle.
+
+    targets: int32 [rows]; a row whose target is not one of 0 .. classes - 1 does not count.  Strides (0 = dense) are in elements: x_row of x and dx,
+    w_row of w and dw.
+    """
+
+    _name = "xent"
+
+    def __init__(self, rows: int, in_features: int, classes: int, dtype: str = "bf16", x_row: int = 0, w_row: int = 0):
+        self.handle = None
+        self._open(stripe_xent_create(rows, in_features, classes, dtype, x_row, w_row), dtype)
+        self._x, self._w = ((rows, in_features), (x_row or in_features, 1)), ((classes, in_features), (w_row or in_features, 1))
+        self._r = ((rows,), (1,))
+
+    def run(self, x, w, targets, loss=None, lse=None, stream: Optional[int] = None) -> None:
+        """Every row's loss and log sum exp, those that are given a tensor."""
+        dev, p, t, f = self._current(), self._ptr, self._dtype, self._f32
+        st = lib.stripe_xent_run(self.handle, p("x", x, t, *self._x, dev), p("w", w, t, *self._w, dev), p("targets", targets, self._i32, *self._r, dev),
+                                 p("loss", loss, f, *self._r, dev), p("lse", lse, f, *self._r, dev), current_stream() if stream is None else stream)
+        if st != STRIPE_OK:
+            raise StripeError(st, stripe_last_error())
+
+    def backward(self, x, w, targets, lse, dloss=None, dlse=None, dx=None, dw=None, stream: Optional[int] = None) -> None:
+        """The gradients that are given a tensor, dx and dw, of the sum of dloss loss + dlse lse (None: ones, zeros)."""
+        dev, p, t, f = self._current(), self._ptr, self._dtype, self._f32
+        st = lib.stripe_xent_backward(self.handle, p("x", x, t, *self._x, dev), p("w", w, t, *self._w, dev), p("targets", targets, self._i32, *self._r, dev),
+                                      p("lse", lse, f, *self._r, dev), p("dloss", dloss, f, *self._r, dev), p("dlse", dlse, f, *self._r, dev),
+                                      p("dx", dx, t, *self._x, dev), p("dw", dw, t, *self._w, dev), current_stream() if stream is None else stream)
+        if st != STRIPE_OK:
+            raise StripeError(st, stripe_last_error())
+
+
+class StripeAdamW:
+    """AdamW over many tensors (see include/stripe.h); owns one handle.
+
+    sizes: each tensor's elements; grads "bf16" or "f32"; states "f32" or "8bit" (m int8, v uint8, their factors fp32 [ceil(size / 256)]);
+    weight_decay: one number, or one for each tensor.  bind() checks and keeps the tensors, run() is a step on them, on the device they are on, which has
+    to be the current one.
+    """
+
+    def __init__(self, sizes: Sequence[int], grads: str = "f32", states: str = "f32", betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.0):
+        import torch
+        self.handle = None
+        self.sizes = [int(n) for n in sizes]
+        decay = [float(weight_decay)] * len(self.sizes) if isinstance(weight_decay, (int, float)) else list(weight_decay)
+        self.handle = stripe_adamw_create(self.sizes, decay, grads, states, betas[0], betas[1], eps)
+        self._eight, self._betas, self._device, self._kept = states == "8bit", betas, None, None
+        self._grad = {"bf16": torch.bfloat16, "f32": torch.float32}[grads]
+
+    def _list(self, what, tensors, dtype, sizes, device):
+        """Addresses of contiguous tensors of the given sizes; None for None."""
+        if tensors is None:
+            return [None] * len(sizes)
+        if len(tensors) != len(sizes):
+            raise ValueError(f"{what}: expected {len(sizes)} tensors, got {len(tensors)}")
+        for i, (t, n) in enumerate(zip(tensors, sizes)):
+            if t is not None and (t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != device):
+                raise ValueError(f"{what}[{i}]: expected {n} contiguous elements of {dtype} on cuda:{device}, got {t.numel()} of {t.dtype} on {t.device}")
+        return [t if t is None else t.data_ptr() for t in tensors]
+
+    def bind(self, params, grads, m, v, m_scales=None, v_scales=None, copies=None) -> None:
+        """The tensors that run() updates, kept here until the next bind(): params fp32, copies bf16 (or None, or None entries)."""
+        import torch
+        blocks = [-(-n // 256) for n in self.sizes]
+        f32, states = torch.float32, (torch.int8, torch.uint8) if self._eight else (torch.float32, torch.float32)
+        device = torch.cuda.current_device()
+        lists = [self._list("params", params, f32, self.sizes, device), self._list("grads", grads, self._grad, self.sizes, device),
+                 self._list("m", m, states[0], self.sizes, device), self._list("v", v, states[1], self.sizes, device),
+                 self._list("m_scales", m_scales, f32, blocks, device), self._list("v_scales", v_scales, f32, blocks, device),
+                 self._list("copies", copies, torch.bfloat16, self.sizes, device)]
+        _check(lib.stripe_adamw_bind(self.handle, (stripe_adamw_tensor_t * max(1, len(self.sizes)))(*zip(*lists))))
+        self._device = device
+        self._kept = [list(x) for x in (params, grads, m, v, m_scales or (), v_scales or (), copies or ())]
+
+    def _current(self, stream):
+        import torch
+        if self._device is not None and torch.cuda.current_device() != self._device:
+            raise ValueError(f"the tensors are on cuda:{self._device}, the current device is cuda:{torch.cuda.current_device()}")
+        return current_stream() if stream is None else stream
+
+    def run(self, lr: float = 0.0, step: int = 1, factor: float = 1.0, seed: int = 0, control=None, stream: Optional[int] = None) -> None:
+        """One step.  control (see control()): a device tensor that is read when the step runs, in place of lr, step, factor and seed."""
+        address, stream = None, self._current(stream)
+        if control is not None:
+            import torch
+            if control.dtype is not torch.int32 or control.shape != (5,) or not control.is_contiguous() or control.get_device() != torch.cuda.current_device():
+                raise ValueError("control: expected 5 contiguous int32 values on the current device, as control() gives them")
+            address = control.data_ptr()
+        st = lib.stripe_adamw_run(self.handle, C.byref(stripe_adamw_step_t(lr, step, factor, seed & 0xffffffff, address)), stream)
+        if st != STRIPE_OK:
+            raise StripeError(st, stripe_last_error())
+
+    def control(self, lr: float, step: int, factor: float = 1.0, seed: int = 0):
+        """What run() reads from a control tensor for this step: five 32-bit values, on the host."""
+        import torch
+        values = torch.tensor([lr, 1 / (1 - self._betas[0] ** step), (1 - self._betas[1] ** step) ** -0.5, factor], dtype=torch.float32)
+        return torch.cat([values.view(torch.int32), torch.tensor([seed & 0xffffffff]).to(torch.int32)])
+
+    def read(self, m=None, v=None, stream: Optional[int] = None) -> None:
+        """The values that states in 8 bits stand for, into fp32 tensors (lists; None, or None entries: not wanted)."""
+        import torch
+        device, arrays = torch.cuda.current_device(), []
+        for what, tensors in (("m", m), ("v", v)):
+            arrays.append((C.c_void_p * max(1, len(self.sizes)))(*self._list(what, tensors, torch.float32, self.sizes, device)))
+        st = lib.stripe_adamw_read(self.handle, *arrays, self._current(stream))
+        if st != STRIPE_OK:
+            raise StripeError(st, stripe_last_error())
+
+    def close(self) -> None:
+        if self.handle is not None:
+            lib.stripe_adamw_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

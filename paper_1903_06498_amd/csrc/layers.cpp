@@ -3,10 +3,9 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
-#include <initializer_list>
 #include <memory>
 
-#include "layers.hpp"
+#include "layers_host.hpp"
 
 using namespace stripe;
 
@@ -54,34 +53,7 @@ stripe_status_t Workspace::get(int64_t need, hipStream_t stream, unsigned char**
 
 namespace {
 
-constexpr int64_t kMaxLinearRows = (int64_t)1 << 28, kMaxNormRows = (int64_t)1 << 30, kMaxFeatures = (int64_t)1 << 24, kMaxStride = (int64_t)1 << 40;
-constexpr int kMaxGroups = 4096;
-
-int64_t round_up_256(int64_t v) { return (v + 255) / 256 * 256; }
-int64_t elem_size(int dtype) { return dtype == STRIPE_F32 ? 4 : 2; }
-
-// No exception leaves a C entry: what runs out here is host memory (or a mutex).
-template <typename F>
-stripe_status_t guarded(F&& body) {
-  try {
-    return body();
-  } catch (...) {
-    return STRIPE_ERR_NOMEM;
-  }
-}
-
-stripe_status_t launched(hipError_t e) {
-  return e == hipSuccess ? STRIPE_OK : api_fail(STRIPE_ERR_HIP, std::string("kernel launch failed: ") + hipGetErrorString(e));
-}
-
-bool misaligned(const void* p, int64_t to) { return (uintptr_t)p % (uintptr_t)to != 0; }
-
-// An output that begins where an input or another output does (overlaps with other beginnings are the caller's word).
-bool shared(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins) {
-  for (const void* const* o = outs.begin(); o != outs.end(); ++o)
-    if (*o && (std::find(ins.begin(), ins.end(), *o) != ins.end() || std::find(o + 1, outs.end(), *o) != outs.end())) return true;
-  return false;
-}
+constexpr int64_t kMaxLinearRows = (int64_t)1 << 28, kMaxNormRows = (int64_t)1 << 30;
 
 }  // namespace
 
@@ -118,8 +90,6 @@ stripe_status_t linear_create(const stripe_linear_desc_t* desc, stripe_linear_t*
   if (!d.y_row) d.y_row = d.out_features;
   if (d.x_row < d.in_features || d.x_row > kMaxStride || d.w_row < d.in_features || d.w_row > kMaxStride || d.y_row < d.out_features || d.y_row > kMaxStride)
     return api_fail(STRIPE_ERR_INVALID_DESC, "a row stride is shorter than its row (or beyond 2^40 elements)");
-  // (offsets within a buffer are 64-bit byte counts)
-  auto beyond = [](int64_t n, int64_t stride) { return (__int128)n * stride > (__int128)1 << 56; };
   if (beyond(d.rows, d.x_row) || beyond(d.rows, d.y_row) || beyond(d.out_features, d.w_row))
     return api_fail(STRIPE_ERR_INVALID_DESC, "a buffer spans more than 2^56 elements");
   const int64_t matrix = (d.out_features - 1) * d.w_row + d.in_features;

@@ -35,7 +35,14 @@ class Workspace {
 //   kForward      A [m][k] = x,   B [n][k] = W      y  = act(x W^T + b) + r
 //   kInputGrad    A [m][k] = dz,  B [k][n] = W      dx = dz W
 //   kWeightGrad   A [k][m] = dz,  B [k][n] = x      dW = dz^T x
-enum ProductKind { kForward = 0, kInputGrad = 1, kWeightGrad = 2 };
+// and, of the operators around it,
+//   kGated        kForward, W's rows in two halves      y  = act(g) u                    (gated.hip)
+//   kLogSum       kForward                              each tile's part of log sum exp  (xent.hip)
+//   kLossGrad     kForward                              gradient of the logits
+//   kSumGrad      kInputGrad                            added to an fp32 image; the last product's total goes to the rows that `index` names
+enum ProductKind { kForward = 0, kInputGrad = 1, kWeightGrad = 2, kGated = 3, kLogSum = 4, kLossGrad = 5, kSumGrad = 6 };
+// B is [k][n]
+constexpr bool reduces_rows(int kind) { return kind == kInputGrad || kind == kWeightGrad || kind == kSumGrad; }
 
 struct ProductParams {
   const void *a, *b;
@@ -55,6 +62,18 @@ struct ProductParams {
   int32_t splits;
   int32_t act;
   int32_t vec;              // rows of c, residual and pre start at 16-byte boundaries
+  // kGated: N outputs from 2 N rows of W
+  int64_t half, pre_ld;     // elements from a gate row to its up row; row stride of pre, [rows][2 N]
+  int32_t vec_pre;          // as vec, of both halves of pre
+  // kLogSum, kLossGrad
+  int32_t class0, classes;  // kLossGrad: the first class of this piece, and how many it has (N: with the zeros behind them)
+  const int32_t* targets;   // [rows]
+  const float *row_lse, *row_all, *row_loss;   // kLossGrad: lse, dloss + dlse, dloss
+  float *stats, *target_z;  // kLogSum: [tiles_n][M] pairs; [rows]
+  // kSumGrad
+  float* sum;               // [M][N], nullptr: one product is all
+  const int32_t* index;     // [rows]
+  int32_t first, last;
 };
 
 struct ProductPlan {
@@ -67,11 +86,13 @@ struct ProductPlan {
 // How a product's operands can be fetched: element by element at their rims; in whole 16-byte pieces (addresses, strides and contiguous extents are
 // multiples of them); in 4-byte words (fp32).  The latter two also want a tile's rows to span less than 2^31 bytes.
 enum Access { kAny = 0, kPieces = 1, kWords = 2 };
-ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, Access access, bool odd_rows);
+// (in_one: the reduction in one piece, on tiles)
+ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, Access access, bool odd_rows, bool in_one = false);
+int tile_columns(const ProductPlan& plan);
 std::string product_name(ProductKind kind, int dtype, const ProductPlan& plan, Access access);
 hipError_t launch_product(ProductKind kind, int dtype, const ProductPlan& plan, Access access, ProductParams p, hipStream_t stream);
 
-hipError_t launch_product_rows(int dtype, ProductParams p, hipStream_t stream);
+hipError_t launch_product_rows(ProductKind kind, int dtype, ProductParams p, hipStream_t stream);     // kForward, kGated
 
 // dz = dy act'(z) (dz == nullptr: not stored; act none: not needed) and db = sums of dz over each group's rows (db == nullptr: not
 // computed).  partial: fp32, dz_slots(rows, groups) x out, unused if db is nullptr or there is one slot.
@@ -85,6 +106,69 @@ struct DzParams {
 };
 int64_t dz_slots(int64_t rows, int groups);
 hipError_t launch_dz(int dtype, const DzParams& p, hipStream_t stream);
+
+// ---- gated unit (gated.hip) ---------------------------------------------------
+// [dg | du] from dy and [g | u], rows `dz_row` apart, zeros behind column 2 out up to it.
+struct GatedGradParams {
+  const void *dy, *pre;
+  void* dz;
+  int64_t y_row, pre_row, dz_row;
+  int32_t rows, out, act;
+};
+hipError_t launch_gated(int dtype, const ProductPlan& plan, Access access, ProductParams p, hipStream_t stream);
+hipError_t launch_gated_grad(int dtype, const GatedGradParams& p, hipStream_t stream);
+
+// ---- cross entropy of a linear head (xent.hip) ---------------------------------
+// The rows that count, i.e. whose target is a class, are copied to the front, in their order: index[i] is the i-th of them, span = {0, their
+// number}.  Arrays of the others: all [rows].  What the outputs hold for rows that do not count is written here.
+struct XentRowsParams {
+  const void* x;
+  const int32_t* targets;
+  const float *lse_in, *dloss, *dlse;        // nullptr: no gradient; ones; zeros
+  void* rows_x;                              // [rows][x_ld], zeros behind column `features`
+  int32_t *index, *span, *row_target;
+  float *row_lse, *row_all, *row_loss;
+  float *loss, *lse;                         // forward: 0 where a row does not count
+  void* dx;                                  // backward: the same
+  int64_t x_row, x_ld;
+  int32_t rows, features, classes;
+};
+hipError_t launch_xent_rows(int dtype, const XentRowsParams& p, hipStream_t stream);
+// loss and lse from the tiles' parts
+struct XentJoinParams {
+  const float *stats, *target_z;
+  const int32_t *index, *span;
+  float *loss, *lse;
+  int32_t rows, tiles;
+};
+hipError_t launch_xent_join(const XentJoinParams& p, hipStream_t stream);
+hipError_t launch_xent(ProductKind kind, int dtype, const ProductPlan& plan, Access access, ProductParams p, hipStream_t stream);
+
+// ---- AdamW (adamw.hip) ----------------------------------------------------------
+constexpr int kAdamWBlock = 256;             // elements that share a factor (states in 8 bits)
+constexpr int kAdamWTensors = 40;            // of a launch: their records are kernel arguments
+struct AdamWTensor {
+  float* p;
+  const void* grad;
+  void *m, *v;
+  float *m_scale, *v_scale;
+  void* copy;
+  int64_t elements;
+  float keep;                                // 1 - lr wd; with control: wd
+  uint32_t number;
+};
+struct AdamWParams {
+  AdamWTensor tensor[kAdamWTensors];
+  uint32_t through[kAdamWTensors];           // chunks of the tensors up to and with it
+  int32_t count;
+  float b1, c1, b2, c2, eps;
+  float lr, rate, spread, factor;            // lr; lr / (1 - b1^t); 1 / sqrt(1 - b2^t); of the gradients
+  uint32_t seed;
+  const float* control;                      // nullptr: the values above; else {lr, 1 / (1 - b1^t), 1 / sqrt(1 - b2^t), factor, seed's bits}
+};
+uint32_t adamw_chunks(int64_t elements);     // workgroups of a tensor
+hipError_t launch_adamw(int grad_dtype, bool eight, const AdamWParams& p, hipStream_t stream);
+hipError_t launch_adamw_read(const AdamWParams& p, hipStream_t stream);
 
 // ---- layer norm (norm.hip) ----------------------------------------------------
 struct NormParams {
