@@ -63,9 +63,10 @@ __device__ __forceinline__ void store4(T* q, int n, const T (&from)[4]) {
   }
 }
 
-// Codes of a block's values (not negative), and the factor of their squares.
+// Codes of a block's values (not negative), and the factor of their squares.  The root's last bit does not matter: where it decides about a floor, the value
+// is next to a code, which is the one that is chosen from either side.
 template <int MOST, bool KEEPS>
-__device__ __forceinline__ float encode(const float (&value)[4], const uint32_t (&bits)[4], int (&code)[4]) {
+__device__ __forceinline__ float encode(const float (&value)[4], const uint32_t (&bits)[4], float (&code)[4]) {
 #pragma clang fp contract(off)
   uint32_t high = 0;
 #pragma unroll
@@ -76,17 +77,17 @@ __device__ __forceinline__ float encode(const float (&value)[4], const uint32_t 
   const float top = wave_largest(high);
   if (!(top < __builtin_inff())) {      // not finite: the block is NaN from here on
 #pragma unroll
-    for (int i = 0; i < 4; ++i) code[i] = 1;
+    for (int i = 0; i < 4; ++i) code[i] = 1.f;
     return __builtin_nanf("");
   }
   const bool fine = top > 1e-30f;
   const float inverse = fine ? 1.f / top * (float)(MOST * MOST) : 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float t = value[i] * inverse, low = floorf(sqrtf(t)), past = t - low * low, place = (float)bits[i] * 0x1p-16f * (2.f * low + 1.f);
-    int c = (int)low + (past > place ? 1 : 0);
-    c = c > MOST ? MOST : c;
-    if (KEEPS && t > 0.f && c == 0) c = 1;
+    const float t = value[i] * inverse, low = floorf(__builtin_amdgcn_sqrtf(t)), past = t - low * low, place = (float)bits[i] * 0x1p-16f * (2.f * low + 1.f);
+    float c = low + (past > place ? 1.f : 0.f);
+    c = fminf(c, (float)MOST);
+    if (KEEPS) c = t > 0.f ? fmaxf(c, 1.f) : c;
     code[i] = c;
   }
   return fine ? top * (float)(1.0 / (MOST * MOST)) : 0.f;
@@ -158,7 +159,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamWParams p) {
       m[e] = m[e] * p.b1 + g * p.c1;
       v[e] = v[e] * p.b2 + g * g * p.c2;
       r[e] = sqrtf(v[e]);
-      pv[b][e] = pv[b][e] * keep - m[e] * rate / (r[e] * spread + p.eps);
+      pv[b][e] = pv[b][e] * keep - m[e] * rate * __builtin_amdgcn_rcpf(r[e] * spread + p.eps);      // (the reciprocal is off by 1 ulp at most)
     }
     store4<float>(x.p + i, n, pv[b]);
     if (x.copy) {
@@ -171,7 +172,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamWParams p) {
       const int64_t block = (first + b * kAdamWBlock) / kAdamWBlock;
       float size[4];
       uint32_t low[4], high[4];
-      int code[4];
+      float code[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const uint32_t bits = mix(key + (uint32_t)(i + e));
@@ -182,10 +183,10 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamWParams p) {
       }
       const float mscale = encode<127, false>(size, low, code);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) mc[b][e] = (int8_t)(m[e] < 0.f ? -code[e] : code[e]);
+      for (int e = 0; e < 4; ++e) mc[b][e] = (int8_t)(int)(m[e] < 0.f ? -code[e] : code[e]);
       const float vscale = encode<255, true>(r, high, code);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) vc[b][e] = (uint8_t)code[e];
+      for (int e = 0; e < 4; ++e) vc[b][e] = (uint8_t)(int)code[e];
       store4<int8_t>((int8_t*)x.m + i, n, mc[b]);
       store4<uint8_t>((uint8_t*)x.v + i, n, vc[b]);
       if (lane == 0 && block * kAdamWBlock < x.elements) {
@@ -199,32 +200,48 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamWParams p) {
   }
 }
 
-// The values that states in 8 bits stand for: m to `p`, v to `copy`.
+// The values that states in 8 bits stand for: m to `p`, v to `copy`.  A lane's loads are 4 bytes: those of four chunks are on their way together.
+constexpr int kReadChunks = 4;
 __global__ __launch_bounds__(256) void adamw_read_kernel(const AdamWParams p) {
 #pragma clang fp contract(off)
+  constexpr int N = kReadChunks * kEach;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int at = find_tensor(p.through, p.count, blockIdx.x);
-  const AdamWTensor& x = p.tensor[at];
-  const int64_t chunk = (int64_t)(blockIdx.x - (at ? p.through[at - 1] : 0u)), first = chunk * kChunk + wave * (kEach * kAdamWBlock);
+  float *mto[N], *vto[N], mq[N], vq[N];
+  int left[N];
+  int8_t mc[N][4];
+  uint8_t vc[N][4];
 #pragma unroll
-  for (int b = 0; b < kEach; ++b) {
-    const int64_t block = (first + b * kAdamWBlock) / kAdamWBlock, i = block * kAdamWBlock + 4 * lane;
-    const int n = x.elements - i < 4 ? (x.elements > i ? (int)(x.elements - i) : 0) : 4;
-    if (n <= 0) continue;
-    int8_t mc[4];
-    uint8_t vc[4];
-    load4<int8_t>((const int8_t*)x.m + i, n, mc);
-    load4<uint8_t>((const uint8_t*)x.v + i, n, vc);
-    const float mq = x.m_scale[block], vq = x.v_scale[block];
+  for (int c = 0; c < kReadChunks; ++c) {
+    uint32_t number = blockIdx.x * kReadChunks + c;
+    const bool there = number < p.through[p.count - 1];
+    number = there ? number : 0;
+    const int at = find_tensor(p.through, p.count, number);
+    const AdamWTensor& x = p.tensor[at];
+    const int64_t chunk = (int64_t)(number - (at ? p.through[at - 1] : 0u)), first = chunk * kChunk + wave * (kEach * kAdamWBlock);
+#pragma unroll
+    for (int b = 0; b < kEach; ++b) {
+      const int k = c * kEach + b;
+      const int64_t i = first + b * kAdamWBlock + 4 * lane, block = i / kAdamWBlock;
+      left[k] = !there || x.elements <= i ? 0 : x.elements - i < 4 ? (int)(x.elements - i) : 4;
+      load4<int8_t>((const int8_t*)x.m + i, left[k], mc[k]);
+      load4<uint8_t>((const uint8_t*)x.v + i, left[k], vc[k]);
+      mq[k] = left[k] ? x.m_scale[block] : 0.f;
+      vq[k] = left[k] ? x.v_scale[block] : 0.f;
+      mto[k] = x.p ? x.p + i : nullptr;
+      vto[k] = x.copy ? (float*)x.copy + i : nullptr;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
     float m[4], v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float c = (float)mc[e], k = (float)vc[e], s = k * k * vq;
-      m[e] = c * __builtin_fabsf(c) * mq;
+      const float c = (float)mc[k][e], d = (float)vc[k][e], s = d * d * vq[k];
+      m[e] = c * __builtin_fabsf(c) * mq[k];
       v[e] = s * s;
     }
-    if (x.p) store4<float>(x.p + i, n, m);
-    if (x.copy) store4<float>((float*)x.copy + i, n, v);
+    if (mto[k]) store4<float>(mto[k], left[k], m);
+    if (vto[k]) store4<float>(vto[k], left[k], v);
   }
 }
 
@@ -245,7 +262,7 @@ hipError_t launch_adamw(int grad_dtype, bool eight, const AdamWParams& p, hipStr
 }
 
 hipError_t launch_adamw_read(const AdamWParams& p, hipStream_t stream) {
-  adamw_read_kernel<<<dim3(p.through[p.count - 1]), dim3(256), 0, stream>>>(p);
+  adamw_read_kernel<<<dim3((p.through[p.count - 1] + kReadChunks - 1) / kReadChunks), dim3(256), 0, stream>>>(p);
   return hipGetLastError();
 }
 

@@ -40,9 +40,12 @@ class Workspace {
 //   kLogSum       kForward                              each tile's part of log sum exp  (xent.hip)
 //   kLossGrad     kForward                              gradient of the logits
 //   kSumGrad      kInputGrad                            added to an fp32 image; the last product's total goes to the rows that `index` names
-enum ProductKind { kForward = 0, kInputGrad = 1, kWeightGrad = 2, kGated = 3, kLogSum = 4, kLossGrad = 5, kSumGrad = 6 };
+//   kLossWeight   kWeightGrad                           the gradients of kLossGrad come divided by `scale`: the outputs times it (kSumGrad's too)
+enum ProductKind { kForward = 0, kInputGrad = 1, kWeightGrad = 2, kGated = 3, kLogSum = 4, kLossGrad = 5, kSumGrad = 6, kLossWeight = 7 };
+// A is [k][m], the reduction goes over rows
+constexpr bool over_rows(int kind) { return kind == kWeightGrad || kind == kLossWeight; }
 // B is [k][n]
-constexpr bool reduces_rows(int kind) { return kind == kInputGrad || kind == kWeightGrad || kind == kSumGrad; }
+constexpr bool reduces_rows(int kind) { return kind == kInputGrad || kind == kSumGrad || over_rows(kind); }
 
 struct ProductParams {
   const void *a, *b;
@@ -69,6 +72,7 @@ struct ProductParams {
   int32_t class0, classes;  // kLossGrad: the first class of this piece, and how many it has (N: with the zeros behind them)
   const int32_t* targets;   // [rows]
   const float *row_lse, *row_all, *row_loss;   // kLossGrad: lse, dloss + dlse, dloss
+  const float* scale;       // kLossGrad, kSumGrad, kLossWeight
   float *stats, *target_z;  // kLogSum: [tiles_n][M] pairs; [rows]
   // kSumGrad
   float* sum;               // [M][N], nullptr: one product is all
@@ -86,8 +90,9 @@ struct ProductPlan {
 // How a product's operands can be fetched: element by element at their rims; in whole 16-byte pieces (addresses, strides and contiguous extents are
 // multiples of them); in 4-byte words (fp32).  The latter two also want a tile's rows to span less than 2^31 bytes.
 enum Access { kAny = 0, kPieces = 1, kWords = 2 };
-// (in_one: the reduction in one piece, on tiles)
-ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, Access access, bool odd_rows, bool in_one = false);
+// What a forward product is for: kLogits has its reduction in one piece, on tiles; kHalves is a gated unit's, `out` both halves.
+enum ProductUse { kLayer, kHalves, kLogits };
+ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, Access access, bool odd_rows, ProductUse use = kLayer);
 int tile_columns(const ProductPlan& plan);
 std::string product_name(ProductKind kind, int dtype, const ProductPlan& plan, Access access);
 hipError_t launch_product(ProductKind kind, int dtype, const ProductPlan& plan, Access access, ProductParams p, hipStream_t stream);
@@ -127,7 +132,8 @@ struct XentRowsParams {
   const float *lse_in, *dloss, *dlse;        // nullptr: no gradient; ones; zeros
   void* rows_x;                              // [rows][x_ld], zeros behind column `features`
   int32_t *index, *span, *row_target;
-  float *row_lse, *row_all, *row_loss;
+  int32_t* counts;                           // of many rows: those that count of each block of them, and the largest |dloss| of each
+  float *row_lse, *row_all, *row_loss, *scale;
   float *loss, *lse;                         // forward: 0 where a row does not count
   void* dx;                                  // backward: the same
   int64_t x_row, x_ld;
@@ -137,7 +143,9 @@ hipError_t launch_xent_rows(int dtype, const XentRowsParams& p, hipStream_t stre
 // loss and lse from the tiles' parts
 struct XentJoinParams {
   const float *stats, *target_z;
-  const int32_t *index, *span;
+  const int32_t *index, *span;               // nullptr: the rows are where they were, `targets` says which of them count
+  const int32_t* targets;
+  int32_t classes;
   float *loss, *lse;
   int32_t rows, tiles;
 };

@@ -26,9 +26,9 @@ struct stripe_xent {
   int64_t piece = 0, pieces = 0;             // classes of a piece of the backward pass
   int64_t x_ld = 0, dz_ld = 0;
   // the workspace: rows' numbers and values, x's rows; then, forward: the tiles' sums, backward: dz, dx in fp32, partial images
-  int64_t row_bytes = 0, x_bytes = 0, stats_bytes = 0, dz_bytes = 0, sum_bytes = 0, partial_bytes = 0;
+  int64_t count_bytes = 0, row_bytes = 0, x_bytes = 0, stats_bytes = 0, dz_bytes = 0, sum_bytes = 0, partial_bytes = 0;
   Workspace ws;
-  int64_t ws_bytes() const { return 256 + 6 * row_bytes + x_bytes + std::max(stats_bytes, dz_bytes + sum_bytes + partial_bytes); }
+  int64_t ws_bytes() const { return 256 + 256 + count_bytes + 6 * row_bytes + x_bytes + std::max(stats_bytes, dz_bytes + sum_bytes + partial_bytes); }
 };
 
 struct stripe_adamw {
@@ -48,6 +48,7 @@ constexpr int64_t kNear = (int64_t)1 << 20;      // row strides up to which a ti
 // dz of a piece: what the products that follow read again is still in the 256 MB of the last level cache.
 constexpr int64_t kPieceBytes = (int64_t)128 << 20, kMaxPiece = (int64_t)1 << 19;
 constexpr int64_t kMaxElements = (int64_t)1 << 34;
+constexpr int64_t kFewRows = 64;
 
 // a launch holds fewer than 2^32 lanes: 2^24 workgroups of 256, counted in tiles of 64 x 64 outputs, the smallest
 bool too_many_tiles(int64_t images, int64_t m, int64_t n) { return ((__int128)images + m / 64 + 1) * (n / 64 + 1) >= 1 << 24; }
@@ -92,7 +93,7 @@ stripe_status_t gated_create(const stripe_gated_desc_t* desc, stripe_gated_t** o
   const bool odd = d.w_row * e % 4 != 0;
   for (const Access access : {gated->best, gated->otherwise})
     for (int k = 0; k < 3; ++k) {
-      gated->plan[access][k] = plan_product((ProductKind)k, d.dtype, d.rows, d.in_features, both, d.groups, access, odd);
+      gated->plan[access][k] = plan_product((ProductKind)k, d.dtype, d.rows, d.in_features, both, d.groups, access, odd, kHalves);
       gated->partial_bytes = std::max(gated->partial_bytes, round_up_256(gated->plan[access][k].ws_bytes));
     }
   gated->dz_bytes = round_up_256(d.rows * gated->dz_row * e);
@@ -213,7 +214,7 @@ stripe_status_t xent_create(const stripe_xent_desc_t* desc, stripe_xent_t** out)
   xent->dw = plan_product(kWeightGrad, d.dtype, d.rows, d.in_features, xent->piece, 0, xent->copies, odd);
   xent->partial_bytes = xent->dw.ws_bytes;
   for (const Access access : {xent->best, xent->otherwise}) {
-    xent->logits[access] = plan_product(kForward, d.dtype, d.rows, d.in_features, d.classes, 0, access, odd, true);
+    xent->logits[access] = plan_product(kForward, d.dtype, d.rows, d.in_features, d.classes, 0, access, odd, kLogits);
     xent->dx[access] = plan_product(kInputGrad, d.dtype, d.rows, d.in_features, xent->piece, 0, access, odd);
     xent->partial_bytes = std::max(xent->partial_bytes, xent->dx[access].ws_bytes);
     const int64_t bn = tile_columns(xent->logits[access]);
@@ -221,6 +222,7 @@ stripe_status_t xent_create(const stripe_xent_desc_t* desc, stripe_xent_t** out)
   }
   xent->partial_bytes = round_up_256(xent->partial_bytes);
   xent->row_bytes = round_up_256(d.rows * 4);
+  xent->count_bytes = round_up_256(d.rows / 1024 * 8 + 8);
   xent->x_bytes = round_up_256(d.rows * xent->x_ld * e);
   xent->dz_bytes = round_up_256(d.rows * xent->dz_ld * e);
   xent->sum_bytes = xent->pieces > 1 ? round_up_256(d.rows * d.in_features * 4) : 0;
@@ -239,6 +241,8 @@ XentParts xent_parts(const stripe_xent_t* xent, unsigned char* ws) {
   XentRowsParams& p = parts.rows;
   auto take = [&](int64_t bytes) { return ws += bytes, ws - bytes; };
   p.span = (int32_t*)take(256);
+  p.scale = (float*)take(256);
+  p.counts = (int32_t*)take(xent->count_bytes);
   p.index = (int32_t*)take(xent->row_bytes);
   p.row_target = (int32_t*)take(xent->row_bytes);
   p.row_lse = (float*)take(xent->row_bytes);
@@ -275,16 +279,26 @@ stripe_status_t xent_run(stripe_xent_t* xent, const void* x, const void* w, cons
   unsigned char* ws = nullptr;
   if (const stripe_status_t st = xent->ws.get(xent->ws_bytes(), stream, &ws); st != STRIPE_OK) return st;
   XentParts parts = xent_parts(xent, ws);
-  parts.rows.x = x; parts.rows.targets = targets; parts.rows.loss = loss; parts.rows.lse = lse;
-  if (const stripe_status_t st = launched(launch_xent_rows(d.dtype, parts.rows, stream)); st != STRIPE_OK) return st;
-  const Access access = misaligned(w, 16) ? xent->otherwise : xent->best;
+  // Rows that fit one tile: leaving some out would save nothing, so x is read where it lies (a launch less: 16 rows, 4096 -> 32768 bf16 64.0 us, 58.9).
+  const bool in_place = d.rows <= kFewRows && d.x_row <= kNear;
+  Access access = misaligned(w, 16) ? xent->otherwise : xent->best;
+  if (in_place) {
+    if (misaligned(x, 16) || d.x_row % (16 / e)) access = xent->otherwise;
+  } else {
+    parts.rows.x = x; parts.rows.targets = targets; parts.rows.loss = loss; parts.rows.lse = lse; parts.rows.scale = nullptr;
+    if (const stripe_status_t st = launched(launch_xent_rows(d.dtype, parts.rows, stream)); st != STRIPE_OK) return st;
+  }
   const ProductPlan& plan = xent->logits[access];
   ProductParams p = xent_logits(xent, parts, w);
   p.N = (int32_t)d.classes;
+  if (in_place) p.a = x, p.a_ld = d.x_row, p.targets = targets, p.offsets = nullptr, p.groups = 0;
   p.stats = (float*)parts.rest; p.target_z = parts.target_z;
   if (const stripe_status_t st = launched(launch_xent(kLogSum, d.dtype, plan, access, p, stream)); st != STRIPE_OK) return st;
   XentJoinParams j = {};
-  j.stats = p.stats; j.target_z = p.target_z; j.index = parts.rows.index; j.span = parts.rows.span;
+  j.stats = p.stats; j.target_z = p.target_z;
+  if (in_place) j.targets = targets;
+  else j.index = parts.rows.index, j.span = parts.rows.span;
+  j.classes = (int32_t)d.classes;
   j.loss = loss; j.lse = lse;
   j.rows = (int32_t)d.rows; j.tiles = (int32_t)((d.classes + tile_columns(plan) - 1) / tile_columns(plan));
   return launched(launch_xent_join(j, stream));
@@ -327,11 +341,11 @@ stripe_status_t xent_backward(stripe_xent_t* xent, const void* x, const void* w,
     ProductParams p = xent_logits(xent, parts, rows);
     p.c = dz; p.c_ld = xent->dz_ld;
     p.N = (int32_t)((count + 7) / 8 * 8); p.class0 = (int32_t)first; p.classes = (int32_t)count;
-    p.row_lse = r.row_lse; p.row_all = r.row_all; p.row_loss = r.row_loss;
+    p.row_lse = r.row_lse; p.row_all = r.row_all; p.row_loss = r.row_loss; p.scale = r.scale;
     p.vec = 1;
     if (const stripe_status_t st = launched(launch_xent(kLossGrad, d.dtype, xent->logits[access], access, p, stream)); st != STRIPE_OK) return st;
     p = {};
-    p.a = dz; p.a_ld = xent->dz_ld; p.offsets = r.span; p.groups = 1; p.partial = partial;
+    p.a = dz; p.a_ld = xent->dz_ld; p.offsets = r.span; p.groups = 1; p.partial = partial; p.scale = r.scale;
     p.rows = (int32_t)d.rows; p.N = (int32_t)d.in_features;
     if (dx) {
       p.b = rows; p.b_ld = d.w_row;
@@ -346,7 +360,7 @@ stripe_status_t xent_backward(stripe_xent_t* xent, const void* x, const void* w,
       p.c = (char*)dw + first * d.w_row * e; p.c_ld = d.w_row;
       p.M = (int32_t)count; p.K = (int32_t)d.rows;
       p.vec = vec_w;
-      if (const stripe_status_t st = launched(launch_product(kWeightGrad, d.dtype, xent->dw, xent->copies, p, stream)); st != STRIPE_OK) return st;
+      if (const stripe_status_t st = launched(launch_xent(kLossWeight, d.dtype, xent->dw, xent->copies, p, stream)); st != STRIPE_OK) return st;
     }
   }
   return STRIPE_OK;

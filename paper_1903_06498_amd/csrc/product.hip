@@ -143,7 +143,7 @@ RowsTime rows_time(int dtype, int64_t rows, int64_t in, int64_t out, int groups,
 
 // The tile and the slices of the reduction with the smallest estimated time: the workgroups of the CU that has most of them one after the other,
 // or in pairs where two fit.
-ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, Access access, bool odd_rows, bool in_one) {
+ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, Access access, bool odd_rows, ProductUse use) {
   ProductPlan plan;
   plan.tile = kSmallTile;
   if (!rows) return plan;
@@ -166,7 +166,7 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
                              : groups            ? (double)m / (double)bm + 0.5 * std::min<double>(groups, (double)m)
                                                  : (double)((m + bm - 1) / bm);
     const double tiles = row_tiles * (double)((n + bn - 1) / bn);
-    for (int splits = 1; splits <= (in_one ? 1 : 16); ++splits) {
+    for (int splits = 1; splits <= (use == kLogits ? 1 : 16); ++splits) {
       if (splits > 1 && (k_tiles < 2 * splits || (forced_splits && splits != forced_splits))) continue;
       const int64_t bytes = splits > 1 ? splits * images * m * n * 4 : 0;
       if (bytes > (64 << 20)) continue;
@@ -175,6 +175,12 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
       double us = 4;
       if (s.resident == 1) us += most * (kt * (t.k_few + (t.k_full - t.k_few) * full) + t.store_few + (t.store_full - t.store_few) * full);
       else us += std::floor(most / 2) * (kt * t.k_full + t.store_full) + std::fmod(most, 2) * (kt * t.k_few + t.store_few);
+      if (use == kLogits) {
+        // Few rows read W from memory, a workgroup with a stage less a half of its tile on its way, about 2.2 us each.  16 rows, 4096 -> 32768 bf16 (268 MB): tiles 0
+        // to 3 106, 64, 62 and 54 us; by this 102, 64, 64 and 57.
+        const double way = (s.stages - 0.5) * (double)bn * 128, held = std::min(256.0, workgroups) * (workgroups > 256 ? s.resident : 1) * way / 2.2;
+        us = std::max(us, 6 + (double)n * (double)k * (f32 ? 4 : 2) / std::min(5.3e6, held));
+      }
       // the join: a launch, and its bytes written and read (300^3 fp32: 8.9 us in one piece, 9.6 in the five that would win without the launch;
       // 1000 x 777 x 1283's dW: 40.9 in one, 34.8 in three)
       if (splits > 1) us += 3.2 + (double)bytes * 1.5 / 4e6;
@@ -189,12 +195,13 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
       }
     }
   }
-  if (kind == kForward && !in_one && rows <= (groups ? 8 * (int64_t)groups : 64)) {
+  if (kind == kForward && use != kLogits && rows <= (groups ? 8 * (int64_t)groups : 64)) {
     const RowsTime few = rows_time(dtype, rows, in, out, groups, odd_rows);
-    if (best_workgroups > 256) best = std::max(best, few.floor);
+    // (a gated unit, 1 row, 4096 -> 2 x 8192 bf16: 36.8 us on tiles, 29.9)
+    if (best_workgroups > 256 || use == kHalves) best = std::max(best, few.floor);
     plan.few = few.us <= 1.05 * best;
   }
-  if (const int forced = tune_int("product_few", -1); forced >= 0 && kind == kForward && !in_one) plan.few = forced != 0;
+  if (const int forced = tune_int("product_few", -1); forced >= 0 && kind == kForward && use != kLogits) plan.few = forced != 0;
   if ((groups ? rows / 16 + std::min<int64_t>(groups, rows) : (rows + 15) / 16) * ((out + 15) / 16) >= 1 << 23) plan.few = false;      // 2^32 lanes
   if (plan.few) plan.splits = 1, plan.ws_bytes = 0;
   return plan;

@@ -332,13 +332,15 @@ struct Tile {
   int k0, k;                    // kWeightGrad: first row of the reduction, and its length
 };
 
+constexpr unsigned kSpreadTiles = 32;      // of a matrix: from here on the XCDs' shares of it differ by an eighth at most
+
 // Tiles in patches of PATCH row tiles by all column tiles: neighbouring numbers (one XCD's) share panels of both operands.
 template <int KIND, int BM, int BN>
 __device__ __forceinline__ bool place(const ProductParams& p, Tile* t) {
   constexpr unsigned PATCH = BM >= 256 ? 4 : 8;
   unsigned row_tiles = (unsigned)p.tiles_m, total, l;
   GroupChunk chunk;      // of up to 64 groups: all of them
-  if (KIND != kWeightGrad && p.groups) {
+  if (!over_rows(KIND) && p.groups) {
     if (p.groups <= 64) {
       chunk = group_chunk(p.offsets, p.groups, p.rows, 0, limited(p.offsets[0], p.rows), 0, BM);
       row_tiles = (unsigned)lane_value(chunk.through, 63);
@@ -347,13 +349,22 @@ __device__ __forceinline__ bool place(const ProductParams& p, Tile* t) {
     }
   }
   total = row_tiles * (unsigned)p.tiles_n;
-  if (KIND == kWeightGrad && p.groups) total *= (unsigned)p.groups;
-  if (!logical_number(blockIdx.x, total, &l)) return false;
   t->group = 0;
-  if (KIND == kWeightGrad && p.groups) {
-    const unsigned each = row_tiles * (unsigned)p.tiles_n;
-    t->group = (int)(l / each);
-    l %= each;
+  if (over_rows(KIND) && p.groups && total >= kSpreadTiles) {
+    // An eighth of every group's tiles to each XCD: the groups' reductions are of very different lengths (8192 rows in 16 uneven groups, 1024 x 4096 features: 137 us
+    // where an XCD had whole groups, 100 here).
+    const unsigned x = blockIdx.x & 7u, i = blockIdx.x >> 3, first = total * x >> 3, own = (total * (x + 1) >> 3) - first;
+    if (i >= own * (unsigned)p.groups) return false;
+    t->group = (int)(i / own);
+    l = first + i % own;
+  } else {
+    if (over_rows(KIND) && p.groups) total *= (unsigned)p.groups;
+    if (!logical_number(blockIdx.x, total, &l)) return false;
+    if (over_rows(KIND) && p.groups) {
+      const unsigned each = row_tiles * (unsigned)p.tiles_n;
+      t->group = (int)(l / each);
+      l %= each;
+    }
   }
   const unsigned per = PATCH * (unsigned)p.tiles_n, patch = l / per, w = l % per;
   const unsigned high = row_tiles - patch * PATCH < PATCH ? row_tiles - patch * PATCH : PATCH;
@@ -361,7 +372,7 @@ __device__ __forceinline__ bool place(const ProductParams& p, Tile* t) {
   t->n0 = tn * (KIND == kGated ? BN / 2 : BN);
   t->k0 = 0;
   t->k = p.K;
-  if (KIND != kWeightGrad && p.groups) {
+  if (!over_rows(KIND) && p.groups) {
     RowTile r = {0, 0, 0};
     if (p.groups <= 64) tile_in_chunk(chunk, 0, BM, tm, &r);
     else r = find_row_tile(p.offsets, p.groups, p.rows, BM, tm);
@@ -371,7 +382,7 @@ __device__ __forceinline__ bool place(const ProductParams& p, Tile* t) {
   } else {
     t->m0 = tm * BM;
     t->m = p.M - t->m0 < BM ? p.M - t->m0 : BM;
-    if (KIND == kWeightGrad && p.groups) {
+    if (over_rows(KIND) && p.groups) {
       int end, unused;
       group_rows(p.offsets, p.groups, p.rows, t->group, 1, &t->k0, &end, &unused);
       t->k = end - t->k0;
@@ -423,8 +434,10 @@ struct Eight {
   }
 };
 
+constexpr bool scaled(int kind) { return kind == kSumGrad || kind == kLossWeight; }
+
 template <typename T, int KIND>
-__device__ __forceinline__ void finish(const ProductParams& p, int row, int col, int64_t at, int n, float (&v)[8], const float (&bias)[8], const Eight<T>& r) {
+__device__ __forceinline__ void finish(const ProductParams& p, float scale, int row, int col, int64_t at, int n, float (&v)[8], const float (&bias)[8], const Eight<T>& r) {
   const bool whole = p.vec && n >= 8;
   Eight<T> out;
   if constexpr (KIND == kSumGrad) {
@@ -445,6 +458,10 @@ __device__ __forceinline__ void finish(const ProductParams& p, int row, int col,
       }
     }
     at = (int64_t)p.index[row] * p.c_ld + col;
+  }
+  if constexpr (scaled(KIND)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= scale;
   }
   if constexpr (KIND == kForward) {
 #pragma unroll
@@ -478,10 +495,11 @@ __device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / (WAVES / 2), wn = wave % (WAVES / 2);
   unsigned char* buf = lds + wave * (ROWS * COLS * 4);
   const int fr = lane & 15, fq = lane >> 4, sp = lane / LANES, sc = lane % LANES;
-  const int64_t image = KIND == kWeightGrad ? (int64_t)t.group * p.M : 0;
-  const int64_t images = KIND == kWeightGrad && p.groups ? (int64_t)p.groups * p.M : p.M;
-  const int64_t base = (KIND == kWeightGrad ? t.group * p.c_group : 0) + (int64_t)t.m0 * p.c_ld;
+  const int64_t image = over_rows(KIND) ? (int64_t)t.group * p.M : 0;
+  const int64_t images = over_rows(KIND) && p.groups ? (int64_t)p.groups * p.M : p.M;
+  const int64_t base = (over_rows(KIND) ? t.group * p.c_group : 0) + (int64_t)t.m0 * p.c_ld;
   auto key = [](int row) { return COLS == 64 ? row & 15 : (row >> 1) & 7; };
+  const float scale = scaled(KIND) ? *p.scale : 1.f;
 #pragma unroll
   for (int jp = 0; jp < C * 16 / COLS; ++jp) {
     const int col = t.n0 + wn * C * 16 + jp * COLS + 8 * sc, n = p.N - col;
@@ -530,7 +548,7 @@ __device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t
               out.set(v);
               out.store(p.partial + ((int64_t)blockIdx.y * images + image + t.m0 + row) * p.N + col, n, false);
             } else {
-              finish<T, KIND>(p, t.m0 + row, col, base + (int64_t)row * p.c_ld + col, n, v, bias, now[q]);
+              finish<T, KIND>(p, scale, t.m0 + row, col, base + (int64_t)row * p.c_ld + col, n, v, bias, now[q]);
             }
           }
         }
@@ -609,10 +627,13 @@ __device__ __forceinline__ void store_gated(const ProductParams& p, const Tile& 
   }
 }
 
-// Of each row of a tile of logits: the largest, and the sum of the exponentials of their distances from it (from 0 where it is infinite, so that the sum
-// is 0, infinite or NaN as the formula has it); the target's logit where it lies in this tile.  NaN is in the sum only.
-template <typename T, int FM, int C, int WAVES>
-__device__ __forceinline__ void store_log_sums(const ProductParams& p, const Tile& t, unsigned char* lds, const f32x4 (&acc)[2 * FM][C]) {
+// Of each row of a tile of logits: the largest times log2 e, and the sum of the exponentials of their distances from it (from 0 where it is infinite, so
+// that the sum is 0, infinite or NaN as the formula has it); the target's logit where it lies in this tile.  NaN is in the sum only.  What an element costs
+// is an exponential and three instructions more: only tiles at the last class look at each column, only fragments with a target look for it.
+constexpr float kLog2E = 1.44269504f;
+
+template <int FM, int C, int WAVES>
+__device__ __forceinline__ void store_log_sums(const ProductParams& p, const Tile& t, unsigned char* lds, f32x4 (&acc)[2 * FM][C]) {
   constexpr int R = 2 * FM, WN = WAVES / 2, BM = 64 * FM, BN = 16 * C * WN;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN, fr = lane & 15;
   const int col = t.n0 + wn * C * 16 + 4 * (lane >> 4);      // the lane's first column
@@ -621,31 +642,45 @@ __device__ __forceinline__ void store_log_sums(const ProductParams& p, const Til
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int row = wm * R * 16 + 16 * i + fr;
-    target[i] = p.targets[t.m0 + (row < t.m ? row : t.m - 1)] - col;
+    target[i] = row < t.m ? (int)((uint32_t)p.targets[t.m0 + row] - (uint32_t)col) : -1;      // (may be none of the classes)
+  }
+  if (t.n0 + BN > p.N) {
+#pragma unroll
+    for (int j = 0; j < C; ++j)
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        if (col + 16 * j + v >= p.N) {
+#pragma unroll
+          for (int i = 0; i < R; ++i) acc[i][j][v] = -__builtin_inff();
+        }
   }
   __syncthreads();      // every wavefront is done with the ring
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int row = wm * R * 16 + 16 * i + fr;
-    float top = -__builtin_inff();
+    if (__any((unsigned)target[i] < 16u * C)) {
+#pragma unroll
+      for (int j = 0; j < C; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          if (target[i] == 16 * j + v) p.target_z[t.m0 + row] = acc[i][j][v];      // (of a column behind the last class: nobody reads it)
+    }
+    float top = acc[i][0][0];
 #pragma unroll
     for (int j = 0; j < C; ++j)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        if (col + 16 * j + v < p.N) top = fmaxf(top, acc[i][j][v]);
-        if (target[i] == 16 * j + v && row < t.m) p.target_z[t.m0 + row] = acc[i][j][v];
-      }
+      for (int v = 0; v < 4; ++v) top = fmaxf(top, acc[i][j][v]);
     top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
+    top = fmaxf(top, __shfl_xor(top, 32)) * kLog2E;
     const float from = __builtin_fabsf(top) < __builtin_inff() ? top : 0.f;
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < C; ++j)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) sum += col + 16 * j + v < p.N ? exp_of<T>(acc[i][j][v] - from) : 0.f;
+      for (int v = 0; v < 4; ++v) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][v], kLog2E, -from));
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
-    if (lane < 16) sums[row * WN + wn] = make_float2(top, sum);
+    if (lane < 16) sums[row * WN + wn] = make_float2(top == top ? top : -__builtin_inff(), sum);
   }
   __syncthreads();
   for (int row = threadIdx.x; row < BM && row < t.m; row += 64 * WAVES) {
@@ -655,30 +690,47 @@ __device__ __forceinline__ void store_log_sums(const ProductParams& p, const Til
     for (int w = 0; w < WN; ++w) s[w] = sums[row * WN + w], top = fmaxf(top, s[w].x);
     const float from = __builtin_fabsf(top) < __builtin_inff() ? top : 0.f;
 #pragma unroll
-    for (int w = 0; w < WN; ++w) sum += s[w].y * exp_of<T>(s[w].x - from);
+    for (int w = 0; w < WN; ++w) sum += s[w].y * __builtin_amdgcn_exp2f(s[w].x - from);
     ((float2*)p.stats)[(int64_t)(t.n0 / BN) * p.M + t.m0 + row] = make_float2(top, sum);
   }
 }
 
-// The gradient of the logits in place of the logits.
+// The gradient of the logits, divided by the scale, in place of the logits; zeros behind the last class.
 template <typename T, int FM, int C, int WAVES>
 __device__ __forceinline__ void loss_gradient(const ProductParams& p, const Tile& t, f32x4 (&acc)[2 * FM][C]) {
   constexpr int R = 2 * FM, WN = WAVES / 2;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / WN, wn = wave % WN, fr = lane & 15;
   const int col = t.n0 + wn * C * 16 + 4 * (lane >> 4);
+  const float inverse = 1.f / *p.scale;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     int row = wm * R * 16 + 16 * i + fr;
     row = t.m0 + (row < t.m ? row : t.m - 1);
     const int target = p.targets[row] - p.class0 - col;
-    const float lse = p.row_lse[row], all = p.row_all[row], one = p.row_loss[row];
+    const float lse = p.row_lse[row], all = p.row_all[row] * inverse, one = p.row_loss[row] * inverse;
 #pragma unroll
     for (int j = 0; j < C; ++j)
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        const float d = exp_of<T>(acc[i][j][v] - lse) * all - (target == 16 * j + v ? one : 0.f);
-        acc[i][j][v] = col + 16 * j + v < p.classes ? d : 0.f;
+        if constexpr (sizeof(T) == 2) acc[i][j][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][v], kLog2E, -lse * kLog2E)) * all;
+        else acc[i][j][v] = expf(acc[i][j][v] - lse) * all;
       }
+    if (__any((unsigned)target < 16u * C)) {
+#pragma unroll
+      for (int j = 0; j < C; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) acc[i][j][v] -= target == 16 * j + v ? one : 0.f;
+    }
+  }
+  if (t.n0 + 16 * C * WN > p.classes) {
+#pragma unroll
+    for (int j = 0; j < C; ++j)
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        if (col + 16 * j + v >= p.classes) {
+#pragma unroll
+          for (int i = 0; i < R; ++i) acc[i][j][v] = 0.f;
+        }
   }
 }
 
@@ -688,7 +740,7 @@ __device__ __forceinline__ void finish_tile(const ProductParams& p, const Tile& 
   if constexpr (KIND == kGated) {
     store_gated<T, FM, C, WAVES>(p, t, lds, acc);
   } else if constexpr (KIND == kLogSum) {
-    store_log_sums<T, FM, C, WAVES>(p, t, lds, acc);
+    store_log_sums<FM, C, WAVES>(p, t, lds, acc);
   } else {
     if constexpr (KIND == kLossGrad) loss_gradient<T, FM, C, WAVES>(p, t, acc);
     store_tile<T, KIND, FM, C, WAVES>(p, t, lds, acc);
@@ -697,7 +749,7 @@ __device__ __forceinline__ void finish_tile(const ProductParams& p, const Tile& 
 
 template <typename T, int KIND, typename A, typename B>
 __device__ __forceinline__ void init_operands(const ProductParams& p, const Tile& t, A& a, B& b) {
-  if constexpr (KIND == kWeightGrad) {
+  if constexpr (over_rows(KIND)) {
     a.init((const T*)p.a + (int64_t)t.k0 * p.a_ld + t.m0, p.M - t.m0, t.m0, p.a_ld);
     b.init((const T*)p.b + (int64_t)t.k0 * p.b_ld + t.n0, p.N - t.n0, t.n0, p.b_ld);
   } else {
@@ -726,7 +778,7 @@ __device__ __forceinline__ void own_k_tiles(const ProductParams& p, int all, int
 template <typename T, int KIND, int FM, int FN>
 __global__ __launch_bounds__(256, 2) void product_kernel(const ProductParams p) {
   constexpr int BM = 64 * FM, BN = 64 * FN, R = 2 * FM, C = 2 * FN;      // fragments of a wavefront
-  using A = Fetch<T, BM, KIND == kWeightGrad>;
+  using A = Fetch<T, BM, over_rows(KIND)>;
   using B = FetchOf<T, KIND, BN, 16 * C>;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   unsigned char *const lds_a = lds, *const lds_b = lds + 2 * A::STAGE;
@@ -749,7 +801,7 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductParams p) 
   u32x4 ra[2][A::LOADS], rb[2][B::LOADS];      // of tiles kt0, kt0 + 2 ..., and of the others
   bool native = true;
   if constexpr (sizeof(T) == 4) {
-    using SA = Split<BM, KIND == kWeightGrad>;
+    using SA = Split<BM, over_rows(KIND)>;
     using SB = Split<BN, reduces_rows(KIND)>;
     unsigned char *const split_a = lds, *const split_b = lds + 2 * SA::STAGE;
     const unsigned first_a = SA::first(wm * R * 16), first_b = SB::first(wn * C * 16);
@@ -886,7 +938,7 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductParams p) 
 template <typename T, int KIND, int FM, int FN, int S, int WAVES, int PIECE>
 __global__ __launch_bounds__(64 * WAVES, S * 64 * (FM + FN) * kDepthBytes > 80 * 1024 ? 1 : 2) void product_stream_kernel(const ProductParams p) {
   constexpr int BM = 64 * FM, BN = 64 * FN, R = 2 * FM, C = 8 * FN / WAVES;      // fragments of a wavefront
-  using A = Stream<T, BM, KIND == kWeightGrad, WAVES, PIECE>;
+  using A = Stream<T, BM, over_rows(KIND), WAVES, PIECE>;
   using B = StreamOf<T, KIND, BN, 16 * C, WAVES, PIECE>;
   constexpr int LOADS = A::LOADS + B::LOADS, HALF = R / 2;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -1009,10 +1061,10 @@ __global__ __launch_bounds__(64 * WAVES, S * 64 * (FM + FN) * kDepthBytes > 80 *
 template <typename T, int KIND>
 __global__ __launch_bounds__(256) void product_join_kernel(const ProductParams p, int strips) {
   const int row = (int)(blockIdx.x / (unsigned)strips), col = ((int)(blockIdx.x % (unsigned)strips) * 256 + (int)threadIdx.x) * 8, n = p.N - col;
-  const int64_t images = KIND == kWeightGrad && p.groups ? (int64_t)p.groups * p.M : p.M;
+  const int64_t images = over_rows(KIND) && p.groups ? (int64_t)p.groups * p.M : p.M;
   int group = 0;
   int64_t at = (int64_t)row * p.c_ld + col;
-  if (KIND == kWeightGrad) {
+  if (over_rows(KIND)) {
     group = row / p.M;
     at = group * p.c_group + (int64_t)(row % p.M) * p.c_ld + col;
   } else if (p.groups) {
@@ -1054,7 +1106,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(const ProductParams p
     }
     if (p.residual) r.load((const T*)p.residual + at, n, p.vec && n >= 8);
   }
-  finish<T, KIND>(p, row, col, at, n, v, bias, r);
+  finish<T, KIND>(p, scaled(KIND) ? *p.scale : 1.f, row, col, at, n, v, bias, r);
 }
 
 // ---- host ---------------------------------------------------------------------
@@ -1103,7 +1155,7 @@ hipError_t launch_kind(const ProductPlan& plan, Access access, ProductParams& p,
   int64_t total = (int64_t)p.tiles_m * p.tiles_n;
   if (p.groups) {
     // every group's last tile may be part of one
-    if (KIND == kWeightGrad) total *= p.groups;
+    if (over_rows(KIND)) total = (total >= kSpreadTiles ? (total + 7) / 8 * 8 : total) * p.groups;
     else total = ((int64_t)p.M / bm + std::min<int64_t>(p.groups, p.M)) * p.tiles_n;
   }
   const dim3 grid((unsigned)((total + 7) / 8 * 8), (unsigned)plan.splits);
@@ -1126,7 +1178,7 @@ hipError_t launch_kind(const ProductPlan& plan, Access access, ProductParams& p,
   }
   if (e != hipSuccess || plan.splits == 1) return e;
   const int strips = (p.N + 2047) / 2048;
-  const int64_t rows = KIND == kWeightGrad ? (int64_t)std::max(1, p.groups) * p.M : p.M;
+  const int64_t rows = over_rows(KIND) ? (int64_t)std::max(1, p.groups) * p.M : p.M;
   product_join_kernel<T, KIND><<<dim3((unsigned)(rows * strips)), dim3(256), 0, stream>>>(p, strips);
   return hipGetLastError();
 }

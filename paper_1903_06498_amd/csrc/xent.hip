@@ -3,7 +3,7 @@
 // Forward: one product whose epilogue keeps, of each row of a tile, the largest logit and the sum of the exponentials of the distances from it;
 // a second launch joins the tiles.  Backward, a piece of the vocabulary at a time: the same product again with dz = exp(z - lse) (dloss + dlse) -
 // [target] dloss as its epilogue, rounded to the operands' type for the matrix instructions; dx += dz W (an fp32 image, written out by the last piece);
-// the piece's rows of dW = dz^T x.
+// the piece's rows of dW = dz^T x.  A bf16 dz is divided by a scale for its rounding, by which dx and dW are multiplied.
 // Rows that do not count are taken out before: the kernels see the others, one after the other, as the one group of rows [0, their number), a number
 // that stays on the device.
 #include "product_tiles.hpp"
@@ -11,83 +11,157 @@
 namespace stripe {
 namespace {
 
-// Which rows count: one workgroup, a run of rows for each thread.
-__global__ __launch_bounds__(1024) void xent_index_kernel(const XentRowsParams p) {
-  __shared__ int waves[16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t each = (p.rows + 1023) / 1024, first = threadIdx.x * each, last = first + each < p.rows ? first + each : p.rows;
-  int mine = 0;
-  for (int64_t r = first; r < last; ++r) mine += (uint32_t)p.targets[r] < (uint32_t)p.classes;
-  int through = mine;
+constexpr int kCountBlock = 1024;      // rows of a count
+constexpr int kRowsEach = 4;           // rows of a workgroup that copies
+constexpr int64_t kManyRows = 16384;   // more of them are counted in blocks before
+
+__device__ __forceinline__ bool counts(const XentRowsParams& p, int64_t row) { return (uint32_t)p.targets[row] < (uint32_t)p.classes; }
+// What a row's dz is divided by at most: its dloss, where that is finite.
+__device__ __forceinline__ float weight(const XentRowsParams& p, int64_t row) {
+  const float w = !counts(p, row) ? 0.f : p.dloss ? __builtin_fabsf(p.dloss[row]) : 1.f;
+  return w < __builtin_inff() ? w : 0.f;
+}
+// A workgroup's total, and its largest value.
+__device__ __forceinline__ int block_sum(int v, int* shared) {
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int o = __shfl_up(through, d);
-    if (lane >= d) through += o;
-  }
-  if (lane == 63) waves[wave] = through;
+  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
   __syncthreads();
-  int before = through - mine;
-  for (int w = 0; w < wave; ++w) before += waves[w];
-  if (threadIdx.x == 1023) p.span[0] = 0, p.span[1] = before + mine;
-  for (int64_t r = first; r < last; ++r)
-    if ((uint32_t)p.targets[r] < (uint32_t)p.classes) p.index[before++] = (int)r;
+  v = shared[0] + shared[1] + shared[2] + shared[3];
+  __syncthreads();
+  return v;
+}
+__device__ __forceinline__ float block_largest(float v, int* shared) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
+  float* const f = (float*)shared;
+  if ((threadIdx.x & 63) == 0) f[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3]));
+  __syncthreads();
+  return v;
 }
 
-// A row of the copies, and of the outputs where a row does not count: a wavefront each.
+__global__ __launch_bounds__(256) void xent_count_kernel(const XentRowsParams p) {
+  __shared__ int shared[4];
+  int n = 0;
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < kCountBlock / 256; ++i) {
+    const int64_t row = (int64_t)blockIdx.x * kCountBlock + i * 256 + threadIdx.x;
+    if (row >= p.rows) break;
+    n += counts(p, row);
+    if (p.scale) top = fmaxf(top, weight(p, row));
+  }
+  n = block_sum(n, shared);
+  top = block_largest(top, shared);
+  if (threadIdx.x == 0) p.counts[2 * blockIdx.x] = n, p.counts[2 * blockIdx.x + 1] = __builtin_bit_cast(int, top);
+}
+
+// A few rows a workgroup, a wavefront copies one at a time: its place is the number of rows before it that count, which every workgroup counts for itself
+// (8192 x 2048 bf16: 17 us; counted by one workgroup in a launch of its own before, 12 and 15).  The first workgroup finds the scale, the last one the number of all.
 template <typename T>
 __global__ __launch_bounds__(256) void xent_rows_kernel(const XentRowsParams p) {
-  constexpr int VEC = kVec<T>;
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= p.rows) return;
-  if ((uint32_t)p.targets[row] >= (uint32_t)p.classes) {
-    if (lane == 0) {
-      if (p.loss) p.loss[row] = 0.f;
-      if (p.lse) p.lse[row] = 0.f;
+  constexpr int VEC = kVec<T>, ROWS = kRowsEach, AHEAD = 4;
+  __shared__ int shared[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row0 = (int64_t)blockIdx.x * ROWS;
+  const bool many = p.rows > kManyRows;
+  int n = 0;
+  if (many)
+    for (int64_t b = threadIdx.x; b < row0 / kCountBlock; b += 256) n += p.counts[2 * b];
+#pragma unroll 8
+  for (int64_t r = (many ? row0 / kCountBlock * kCountBlock : 0) + threadIdx.x; r < row0; r += 256) n += counts(p, r);
+  int before = block_sum(n, shared);
+  const bool mine = lane < ROWS && row0 + lane < p.rows && counts(p, row0 + lane);
+  const uint64_t all = __ballot(mine);      // of the workgroup's rows, in every wavefront
+  if (threadIdx.x == 0 && row0 + ROWS >= p.rows) p.span[0] = 0, p.span[1] = before + __builtin_popcountll(all);
+  if (p.scale && blockIdx.x == 0) {
+    // bf16: dz is divided by the largest dloss, so that a target's dz, the value that matters most, lies in the upper half of a power of two, where
+    // rounding is half as coarse (equal weights and unsure targets: dz = -1 + p)
+    float top = 0.f;
+    if (sizeof(T) == 2) {
+      if (many)
+        for (int64_t b = threadIdx.x; b < (p.rows + kCountBlock - 1) / kCountBlock; b += 256) top = fmaxf(top, __builtin_bit_cast(float, p.counts[2 * b + 1]));
+      else
+#pragma unroll 4
+        for (int64_t r = threadIdx.x; r < p.rows; r += 256) top = fmaxf(top, weight(p, r));
     }
-    if (p.dx)
-      for (int64_t c = lane * VEC; c < p.features; c += 64 * VEC) store_piece<T>((T*)p.dx + row * p.x_row + c, (u32x4){0, 0, 0, 0}, (int)(p.features - c));
+    top = block_largest(top, shared);
+    if (threadIdx.x == 0) *p.scale = top > 0x1p-100f ? top : 1.f;
   }
-  if (row >= p.span[1]) return;
-  const int64_t from = p.index[row];
-  const T* const x = (const T*)p.x + from * p.x_row;
-  T* const to = (T*)p.rows_x + row * p.x_ld;
-  for (int64_t c = lane * VEC; c < p.features; c += 64 * VEC) *(u32x4*)(to + c) = load_piece<T>(x + c, (int)(p.features - c));
-  if (lane == 0) {
-    p.row_target[row] = p.targets[from];
-    if (p.lse_in) {
-      const float one = p.dloss ? p.dloss[from] : 1.f;
-      p.row_lse[row] = p.lse_in[from];
-      p.row_loss[row] = one;
-      p.row_all[row] = p.dlse ? one + p.dlse[from] : one;
+  for (int i = wave; i < ROWS && row0 + i < p.rows; i += 4) {
+    const int64_t row = row0 + i;
+    if (!(all >> i & 1)) {
+      if (lane == 0) {
+        if (p.loss) p.loss[row] = 0.f;
+        if (p.lse) p.lse[row] = 0.f;
+      }
+      if (p.dx)
+        for (int64_t c = lane * VEC; c < p.features; c += 64 * VEC) store_piece<T>((T*)p.dx + row * p.x_row + c, (u32x4){0, 0, 0, 0}, (int)(p.features - c));
+      continue;
+    }
+    const int64_t at = before + __builtin_popcountll(all & (((uint64_t)1 << i) - 1));
+    const T* const x = (const T*)p.x + row * p.x_row;
+    T* const to = (T*)p.rows_x + at * p.x_ld;
+    int64_t c = lane * VEC;
+    for (; c + (AHEAD - 1) * 64 * VEC + VEC <= p.features; c += AHEAD * 64 * VEC) {
+      u32x4 v[AHEAD];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) __builtin_memcpy(&v[k], x + c + k * 64 * VEC, 16);
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) *(u32x4*)(to + c + k * 64 * VEC) = v[k];
+    }
+    for (; c < p.features; c += 64 * VEC) *(u32x4*)(to + c) = load_piece<T>(x + c, (int)(p.features - c));
+    if (lane == 0) {
+      p.index[at] = (int)row;
+      p.row_target[at] = p.targets[row];
+      if (p.lse_in) {
+        const float one = p.dloss ? p.dloss[row] : 1.f;
+        p.row_lse[at] = p.lse_in[row];
+        p.row_loss[at] = one;
+        p.row_all[at] = p.dlse ? one + p.dlse[row] : one;
+      }
     }
   }
 }
 
-// A row's lse and loss: 64 rows, four wavefronts that share the tiles out.
+// A row's lse and loss from the tiles' parts: 16 rows a workgroup, 16 threads to a row, four tiles of each on their way at a time.
 __global__ __launch_bounds__(256) void xent_join_kernel(const XentJoinParams p) {
-  __shared__ float2 part[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, count = p.span[1];
-  const int row = (int)blockIdx.x * 64 + lane;
-  if ((int)blockIdx.x * 64 >= count) return;
+  __shared__ float2 part[16][17];
+  const int r = threadIdx.x & 15, slice = threadIdx.x >> 4, count = p.span ? p.span[1] : p.rows;
+  const int row = (int)blockIdx.x * 16 + r;
+  if ((int)blockIdx.x * 16 >= count) return;
   float top = -__builtin_inff(), sum = 0.f;
-  auto add = [&](float2 s) {
-    const float high = fmaxf(top, s.x), from = __builtin_fabsf(high) < __builtin_inff() ? high : 0.f;
-    sum = sum * expf(top - from) + s.y * expf(s.x - from);
+  auto add = [&](const float2* s, int n) {
+    float high = top;
+    for (int i = 0; i < n; ++i) high = fmaxf(high, s[i].x);
+    const float from = __builtin_fabsf(high) < __builtin_inff() ? high : 0.f;
+    sum *= __builtin_amdgcn_exp2f(top - from);
+    for (int i = 0; i < n; ++i) sum += s[i].y * __builtin_amdgcn_exp2f(s[i].x - from);
     top = high;
   };
   if (row < count) {
-#pragma unroll 4
-    for (int t = wave; t < p.tiles; t += 4) add(((const float2*)p.stats)[(int64_t)t * p.rows + row]);
+    for (int t = slice; t < p.tiles; t += 64) {
+      float2 s[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] = t + 16 * i < p.tiles ? ((const float2*)p.stats)[(int64_t)(t + 16 * i) * p.rows + row] : make_float2(-__builtin_inff(), 0.f);
+      add(s, 4);
+    }
   }
-  part[wave][lane] = make_float2(top, sum);
+  part[slice][r] = make_float2(top, sum);
   __syncthreads();
-  if (wave || row >= count) return;
-  for (int w = 1; w < 4; ++w) add(part[w][lane]);
-  const float lse = (__builtin_fabsf(top) < __builtin_inff() ? top : 0.f) + logf(sum);
-  const int at = p.index[row];
-  if (p.lse) p.lse[at] = lse;
-  if (p.loss) p.loss[at] = lse - p.target_z[row];
+  if (slice || row >= count) return;
+  top = -__builtin_inff(), sum = 0.f;
+  float2 s[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s[i] = part[i][r];
+  add(s, 16);
+  const float lse = ((__builtin_fabsf(top) < __builtin_inff() ? top : 0.f) + log2f(sum)) * 0.693147181f;
+  const int at = p.index ? p.index[row] : row;
+  const bool counts = p.index || (uint32_t)p.targets[row] < (uint32_t)p.classes;
+  if (p.lse) p.lse[at] = counts ? lse : 0.f;
+  if (p.loss) p.loss[at] = counts ? lse - p.target_z[row] : 0.f;
 }
 
 template <typename T>
@@ -95,22 +169,23 @@ hipError_t launch_xent_type(ProductKind kind, const ProductPlan& plan, Access ac
   switch (kind) {
     case kLogSum: return launch_kind<T, kLogSum>(plan, access, p, stream);
     case kLossGrad: return launch_kind<T, kLossGrad>(plan, access, p, stream);
-    default: return launch_kind<T, kSumGrad>(plan, access, p, stream);
+    case kSumGrad: return launch_kind<T, kSumGrad>(plan, access, p, stream);
+    default: return launch_kind<T, kLossWeight>(plan, access, p, stream);
   }
 }
 
 }  // namespace
 
 hipError_t launch_xent_rows(int dtype, const XentRowsParams& p, hipStream_t stream) {
-  xent_index_kernel<<<dim3(1), dim3(1024), 0, stream>>>(p);
-  const dim3 grid((unsigned)(((int64_t)p.rows + 3) / 4));
+  if (p.rows > kManyRows) xent_count_kernel<<<dim3((unsigned)((p.rows + kCountBlock - 1) / kCountBlock)), dim3(256), 0, stream>>>(p);
+  const dim3 grid((unsigned)(((int64_t)p.rows + kRowsEach - 1) / kRowsEach));
   if (dtype == STRIPE_F32) xent_rows_kernel<float><<<grid, dim3(256), 0, stream>>>(p);
   else xent_rows_kernel<__bf16><<<grid, dim3(256), 0, stream>>>(p);
   return hipGetLastError();
 }
 
 hipError_t launch_xent_join(const XentJoinParams& p, hipStream_t stream) {
-  xent_join_kernel<<<dim3((unsigned)(((int64_t)p.rows + 63) / 64)), dim3(256), 0, stream>>>(p);
+  xent_join_kernel<<<dim3((unsigned)(((int64_t)p.rows + 15) / 16)), dim3(256), 0, stream>>>(p);
   return hipGetLastError();
 }
 

@@ -270,3 +270,15 @@ def test_wrapper_refuses_other_tensors():
         t.op.run(t.x, t.w, y, offsets=torch.zeros(1, dtype=torch.int32, device="cuda"))
     with pytest.raises(B.StripeError):
         t.op.backward(t.dy, t.x, t.w, t.pre_in, dx=t.x)
+
+
+@pytest.mark.parametrize("offsets", [None, [0, 0, 300, 300, 1000, 4000, 4001, 4400, 4350], list(range(0, 4352, 68))], ids=["dense", "9", "64"])
+@pytest.mark.parametrize("cin", [8, 64, 328])
+def test_more_tiles_than_compute_units(monkeypatch, cin, offsets):
+    """Several tiles of 256 x 256 for each compute unit, dense and with groups."""
+    monkeypatch.setenv("STRIPE_TUNE", "product_tile=0,product_splits=1,product_few=0")
+    t = Gated(4360, cin, 2200 if offsets is None else 1100, "bf16", offsets=offsets, seed=15)
+    assert "256x256" in t.op.info["forward"]
+    t.forward()
+    t.backward()
+    t.check()

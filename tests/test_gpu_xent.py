@@ -323,3 +323,60 @@ def test_wrapper_refuses_other_tensors():
         t.op.run(t.x, t.w, t.targets, t.loss, t.loss)
     with pytest.raises(B.StripeError):
         t.op.backward(t.x, t.w, t.targets, t.lse, dx=t.x)
+
+
+@pytest.mark.parametrize("rows", [300, 20000])
+@pytest.mark.parametrize("weights", ["zeros", "tiny", "mixed"])
+def test_sizes_of_dloss(weights, rows):
+    """dz is divided by the largest dloss before its rounding: whatever that is."""
+    t = Xent(rows, 48, 130, "bf16", seed=16)
+    t.dloss.mul_({"zeros": 0.0, "tiny": 2.0 ** -120, "mixed": 1.0}[weights])
+    if weights == "tiny":
+        t.dlse.mul_(2.0 ** -120)
+    if weights == "mixed":
+        t.dloss.mul_(torch.pow(2.0, torch.arange(rows, device="cuda") % 40 - 20.0))
+    t.backward()
+    t.check_backward()
+
+
+def test_a_weight_that_is_not_finite_stays_in_its_row():
+    t = Xent(40, 64, 100, "bf16", ignored=0.0, seed=17)
+    t.dloss[7], t.dloss[8] = float("inf"), NAN
+    t.op.backward(t.x, t.w, t.targets, t.lse_in(), dloss=t.dloss, dlse=t.dlse, dx=t.outs["dx"][1])
+    got = t.outs["dx"][1]
+    assert not torch.isfinite(got[7:9]).any() and torch.isfinite(got[:7]).all() and torch.isfinite(got[9:]).all()
+
+
+def test_many_rows():
+    """More rows than are counted in one launch, a block without any that counts among them."""
+    t = Xent(40000, 16, 70, "bf16", ignored=0.5, seed=18)
+    t.targets[2048:5000] = -1
+    t.counts[2048:5000] = False
+    t.z, t.lse_ref = t.x[t.counts].double() @ t.w.double().t(), None
+    t.lse_ref = torch.logsumexp(t.z, 1)
+    t.forward()
+    t.check_forward()
+    t.backward()
+    t.check_backward()
+
+
+@pytest.mark.parametrize("ignored", [0.0, 0.4, 1.0])
+def test_more_tiles_than_compute_units(monkeypatch, ignored):
+    """Several tiles of 256 x 256 for each compute unit in all four products; with no row that counts the sums have no terms."""
+    monkeypatch.setenv("STRIPE_TUNE", "product_tile=0,product_splits=1")
+    t = Xent(4360, 4190 if ignored < 1 else 4200, 4300, "bf16", ignored=ignored, pad=2 if ignored < 1 else 0, seed=19, scale=0.5)
+    t.forward()
+    t.check_forward()
+    t.backward()
+    t.check_backward()
+
+
+def test_many_tiles_of_short_sums(monkeypatch):
+    """One K tile, a part of one, and two to a tile of outputs."""
+    monkeypatch.setenv("STRIPE_TUNE", "product_tile=0,product_splits=1,xent_pieces=2")
+    for cin in (8, 64, 136):
+        t = Xent(4500, cin, 9500, "bf16", ignored=0.1, seed=20, pieces=2)
+        t.forward()
+        t.check_forward()
+        t.backward()
+        t.check_backward()
