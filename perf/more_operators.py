@@ -219,7 +219,12 @@ def _prepare_adamw(case, seed, g):
         s["op"] = StripeAdamW(sizes, grads=case["grads"], states=case["states"], betas=BETAS, eps=EPS, weight_decay=decay)
         s["op"].bind(parts(s["p"]), parts(s["grad"]), parts(s["m"]), parts(s["v"]), m_scales=scales(s["m_scale"]), v_scales=scales(s["v_scale"]),
                      copies=parts(s["copy"]))
-        s["outs"] = (parts(s["m_out"]), parts(s["v_out"])) if eight else None
+        s["outs"] = None
+        if eight:
+            # read() writes the tensors' elements and not what lies between them, which is returned too
+            s["m_out"].zero_()
+            s["v_out"].zero_()
+            s["outs"] = (parts(s["m_out"]), parts(s["v_out"]))
     return s
 
 
