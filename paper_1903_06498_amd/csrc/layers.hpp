@@ -90,7 +90,7 @@ struct ProductPlan {
 // How a product's operands can be fetched: element by element at their rims; in whole 16-byte pieces (addresses, strides and contiguous extents are
 // multiples of them); in 4-byte words (fp32).  The latter two also want a tile's rows to span less than 2^31 bytes.
 enum Access { kAny = 0, kPieces = 1, kWords = 2 };
-// What a forward product is for: kLogits has its reduction in one piece, on tiles; kHalves is a gated unit's, `out` both halves.
+// What a forward product is for: kLogits are made on tiles, in slices only where they are few; kHalves is a gated unit's, `out` both halves.
 enum ProductUse { kLayer, kHalves, kLogits };
 ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, Access access, bool odd_rows, ProductUse use = kLayer);
 int tile_columns(const ProductPlan& plan);
@@ -142,13 +142,15 @@ struct XentRowsParams {
 hipError_t launch_xent_rows(int dtype, const XentRowsParams& p, hipStream_t stream);
 // loss and lse from the tiles' parts
 struct XentJoinParams {
-  const float *stats, *target_z;
+  float *stats, *target_z;                   // [tiles][rows] pairs, [rows]
+  const float* partial;                      // [splits][rows][classes]: slices of the logits, from which stats and target_z are made first
   const int32_t *index, *span;               // nullptr: the rows are where they were, `targets` says which of them count
   const int32_t* targets;
-  int32_t classes;
+  int32_t classes, splits;
   float *loss, *lse;
   int32_t rows, tiles;
 };
+int xent_slice_blocks(int64_t classes);     // `tiles` of logits in slices
 hipError_t launch_xent_join(const XentJoinParams& p, hipStream_t stream);
 hipError_t launch_xent(ProductKind kind, int dtype, const ProductPlan& plan, Access access, ProductParams p, hipStream_t stream);
 

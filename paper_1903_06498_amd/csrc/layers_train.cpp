@@ -25,10 +25,10 @@ struct stripe_xent {
   ProductPlan logits[3], dx[3], dw;          // [Access]
   int64_t piece = 0, pieces = 0;             // classes of a piece of the backward pass
   int64_t x_ld = 0, dz_ld = 0;
-  // the workspace: rows' numbers and values, x's rows; then, forward: the tiles' sums, backward: dz, dx in fp32, partial images
+  // the workspace: rows' numbers and values, x's rows; then, forward: the tiles' sums, backward: dz, dx in fp32; partial images
   int64_t count_bytes = 0, row_bytes = 0, x_bytes = 0, stats_bytes = 0, dz_bytes = 0, sum_bytes = 0, partial_bytes = 0;
   Workspace ws;
-  int64_t ws_bytes() const { return 256 + 256 + count_bytes + 6 * row_bytes + x_bytes + std::max(stats_bytes, dz_bytes + sum_bytes + partial_bytes); }
+  int64_t ws_bytes() const { return 256 + 256 + count_bytes + 6 * row_bytes + x_bytes + std::max(stats_bytes, dz_bytes + sum_bytes) + partial_bytes; }
 };
 
 struct stripe_adamw {
@@ -216,9 +216,11 @@ stripe_status_t xent_create(const stripe_xent_desc_t* desc, stripe_xent_t** out)
   for (const Access access : {xent->best, xent->otherwise}) {
     xent->logits[access] = plan_product(kForward, d.dtype, d.rows, d.in_features, d.classes, 0, access, odd, kLogits);
     xent->dx[access] = plan_product(kInputGrad, d.dtype, d.rows, d.in_features, xent->piece, 0, access, odd);
-    xent->partial_bytes = std::max(xent->partial_bytes, xent->dx[access].ws_bytes);
+    // (a piece's logits in slices: its classes end in zeros up to a multiple of 8)
+    const int64_t slices = xent->logits[access].splits > 1 ? xent->logits[access].splits * d.rows * xent->dz_ld * 4 : 0;
+    xent->partial_bytes = std::max({xent->partial_bytes, xent->dx[access].ws_bytes, xent->logits[access].ws_bytes, slices});
     const int64_t bn = tile_columns(xent->logits[access]);
-    xent->stats_bytes = std::max(xent->stats_bytes, round_up_256((d.classes + bn - 1) / bn * d.rows * 8));
+    xent->stats_bytes = std::max(xent->stats_bytes, round_up_256(std::max((d.classes + bn - 1) / bn, (int64_t)xent_slice_blocks(d.classes)) * d.rows * 8));
   }
   xent->partial_bytes = round_up_256(xent->partial_bytes);
   xent->row_bytes = round_up_256(d.rows * 4);
@@ -293,14 +295,17 @@ stripe_status_t xent_run(stripe_xent_t* xent, const void* x, const void* w, cons
   p.N = (int32_t)d.classes;
   if (in_place) p.a = x, p.a_ld = d.x_row, p.targets = targets, p.offsets = nullptr, p.groups = 0;
   p.stats = (float*)parts.rest; p.target_z = parts.target_z;
+  p.partial = (float*)(parts.rest + std::max(xent->stats_bytes, xent->dz_bytes + xent->sum_bytes));
   if (const stripe_status_t st = launched(launch_xent(kLogSum, d.dtype, plan, access, p, stream)); st != STRIPE_OK) return st;
   XentJoinParams j = {};
   j.stats = p.stats; j.target_z = p.target_z;
-  if (in_place) j.targets = targets;
-  else j.index = parts.rows.index, j.span = parts.rows.span;
+  if (plan.splits > 1) j.partial = p.partial, j.splits = plan.splits;
+  j.targets = p.targets;
+  if (!in_place) j.index = parts.rows.index, j.span = parts.rows.span;
   j.classes = (int32_t)d.classes;
   j.loss = loss; j.lse = lse;
-  j.rows = (int32_t)d.rows; j.tiles = (int32_t)((d.classes + tile_columns(plan) - 1) / tile_columns(plan));
+  j.rows = (int32_t)d.rows;
+  j.tiles = plan.splits > 1 ? xent_slice_blocks(d.classes) : (int32_t)((d.classes + tile_columns(plan) - 1) / tile_columns(plan));
   return launched(launch_xent_join(j, stream));
 }
 
@@ -333,7 +338,7 @@ stripe_status_t xent_backward(stripe_xent_t* xent, const void* x, const void* w,
   if (const stripe_status_t st = launched(launch_xent_rows(d.dtype, r, stream)); st != STRIPE_OK) return st;
   void* const dz = parts.rest;
   float* const sum = (float*)(parts.rest + xent->dz_bytes);
-  float* const partial = (float*)(parts.rest + xent->dz_bytes + xent->sum_bytes);
+  float* const partial = (float*)(parts.rest + std::max(xent->stats_bytes, xent->dz_bytes + xent->sum_bytes));
   const Access access = misaligned(w, 16) ? xent->otherwise : xent->best;
   for (int64_t first = 0; first < d.classes; first += xent->piece) {
     const int64_t count = std::min(xent->piece, d.classes - first);
@@ -342,7 +347,7 @@ stripe_status_t xent_backward(stripe_xent_t* xent, const void* x, const void* w,
     p.c = dz; p.c_ld = xent->dz_ld;
     p.N = (int32_t)((count + 7) / 8 * 8); p.class0 = (int32_t)first; p.classes = (int32_t)count;
     p.row_lse = r.row_lse; p.row_all = r.row_all; p.row_loss = r.row_loss; p.scale = r.scale;
-    p.vec = 1;
+    p.vec = 1; p.partial = partial;
     if (const stripe_status_t st = launched(launch_xent(kLossGrad, d.dtype, xent->logits[access], access, p, stream)); st != STRIPE_OK) return st;
     p = {};
     p.a = dz; p.a_ld = xent->dz_ld; p.offsets = r.span; p.groups = 1; p.partial = partial; p.scale = r.scale;

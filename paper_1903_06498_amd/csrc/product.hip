@@ -141,6 +141,9 @@ RowsTime rows_time(int dtype, int64_t rows, int64_t in, int64_t out, int groups,
 
 }  // namespace
 
+// Logits that are made in slices of the reduction are in memory as a whole, for a moment: 4 MB for each slice at most.  With more of them there are tiles enough.
+constexpr int64_t kFewLogits = (int64_t)1 << 20;
+
 // The tile and the slices of the reduction with the smallest estimated time: the workgroups of the CU that has most of them one after the other,
 // or in pairs where two fit.
 ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, int64_t out, int groups, Access access, bool odd_rows, ProductUse use) {
@@ -166,7 +169,7 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
                              : groups            ? (double)m / (double)bm + 0.5 * std::min<double>(groups, (double)m)
                                                  : (double)((m + bm - 1) / bm);
     const double tiles = row_tiles * (double)((n + bn - 1) / bn);
-    for (int splits = 1; splits <= (use == kLogits ? 1 : 16); ++splits) {
+    for (int splits = 1; splits <= (use == kLogits && m * n > kFewLogits ? 1 : 16); ++splits) {
       if (splits > 1 && (k_tiles < 2 * splits || (forced_splits && splits != forced_splits))) continue;
       const int64_t bytes = splits > 1 ? splits * images * m * n * 4 : 0;
       if (bytes > (64 << 20)) continue;

@@ -627,10 +627,11 @@ __device__ __forceinline__ void store_gated(const ProductParams& p, const Tile& 
   }
 }
 
-// Of each row of a tile of logits: the largest times log2 e, and the sum of the exponentials of their distances from it (from 0 where it is infinite, so
-// that the sum is 0, infinite or NaN as the formula has it); the target's logit where it lies in this tile.  NaN is in the sum only.  What an element costs
-// is an exponential and three instructions more: only tiles at the last class look at each column, only fragments with a target look for it.
-constexpr float kLog2E = 1.44269504f;
+// Of each row of a tile of logits: the largest, and the sum of the exponentials of their distances from it (from 0 where it is infinite, so that the sum is
+// 0, infinite or NaN as the formula has it); the target's logit where it lies in this tile.  NaN is in the sum only.  What an element costs is an
+// exponential and three instructions more: z log2 e - (largest log2 e) is one of them, with the rounding of the bracket taken out of the sum; only tiles
+// at the last class look at each column, only fragments with a target look for it.
+constexpr float kLog2E = 1.44269504f, kLn2 = 0.693147181f;
 
 template <int FM, int C, int WAVES>
 __device__ __forceinline__ void store_log_sums(const ProductParams& p, const Tile& t, unsigned char* lds, f32x4 (&acc)[2 * FM][C]) {
@@ -671,8 +672,9 @@ __device__ __forceinline__ void store_log_sums(const ProductParams& p, const Til
 #pragma unroll
       for (int v = 0; v < 4; ++v) top = fmaxf(top, acc[i][j][v]);
     top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32)) * kLog2E;
-    const float from = __builtin_fabsf(top) < __builtin_inff() ? top : 0.f;
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const bool finite = __builtin_fabsf(top) < __builtin_inff();
+    const float from = finite ? top * kLog2E : 0.f, off = finite ? __builtin_fmaf(top, kLog2E, -from) : 0.f;
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < C; ++j)
@@ -680,6 +682,7 @@ __device__ __forceinline__ void store_log_sums(const ProductParams& p, const Til
       for (int v = 0; v < 4; ++v) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][v], kLog2E, -from));
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
+    sum = finite ? __builtin_fmaf(sum, off * -kLn2, sum) : sum;
     if (lane < 16) sums[row * WN + wn] = make_float2(top == top ? top : -__builtin_inff(), sum);
   }
   __syncthreads();
@@ -690,7 +693,7 @@ __device__ __forceinline__ void store_log_sums(const ProductParams& p, const Til
     for (int w = 0; w < WN; ++w) s[w] = sums[row * WN + w], top = fmaxf(top, s[w].x);
     const float from = __builtin_fabsf(top) < __builtin_inff() ? top : 0.f;
 #pragma unroll
-    for (int w = 0; w < WN; ++w) sum += s[w].y * __builtin_amdgcn_exp2f(s[w].x - from);
+    for (int w = 0; w < WN; ++w) sum += s[w].y * __builtin_amdgcn_exp2f((s[w].x - from) * kLog2E);
     ((float2*)p.stats)[(int64_t)(t.n0 / BN) * p.M + t.m0 + row] = make_float2(top, sum);
   }
 }
@@ -739,10 +742,11 @@ template <typename T, int KIND, int FM, int C, int WAVES>
 __device__ __forceinline__ void finish_tile(const ProductParams& p, const Tile& t, unsigned char* lds, f32x4 (&acc)[2 * FM][C]) {
   if constexpr (KIND == kGated) {
     store_gated<T, FM, C, WAVES>(p, t, lds, acc);
-  } else if constexpr (KIND == kLogSum) {
-    store_log_sums<FM, C, WAVES>(p, t, lds, acc);
   } else {
-    if constexpr (KIND == kLossGrad) loss_gradient<T, FM, C, WAVES>(p, t, acc);
+    if constexpr (KIND == kLogSum)
+      if (p.splits == 1) return store_log_sums<FM, C, WAVES>(p, t, lds, acc);
+    if constexpr (KIND == kLossGrad)
+      if (p.splits == 1) loss_gradient<T, FM, C, WAVES>(p, t, acc);
     store_tile<T, KIND, FM, C, WAVES>(p, t, lds, acc);
   }
 }
@@ -1097,6 +1101,12 @@ __global__ __launch_bounds__(256) void product_join_kernel(const ProductParams p
 #pragma unroll
   for (int e = 0; e < 8; ++e) bias[e] = 0.f;
   total(v, images * p.N, p.partial + (int64_t)row * p.N + col);
+  if constexpr (KIND == kLossGrad) {
+    const float inverse = 1.f / *p.scale, lse = p.row_lse[row], all = p.row_all[row] * inverse, one = p.row_loss[row] * inverse;
+    const int target = p.targets[row] - p.class0 - col;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = col + e < p.classes ? exp_of<T>(v[e] - lse) * all - (target == e ? one : 0.f) : 0.f;
+  }
   Eight<T> r;
   if constexpr (KIND == kForward) {
     if (p.bias) {
@@ -1176,7 +1186,7 @@ hipError_t launch_kind(const ProductPlan& plan, Access access, ProductParams& p,
     product_kernel<T, KIND, s.fm, s.fn><<<grid, dim3(256), bytes, stream>>>(p);
     e = hipGetLastError();
   }
-  if (e != hipSuccess || plan.splits == 1) return e;
+  if (e != hipSuccess || plan.splits == 1 || KIND == kLogSum) return e;      // (its join is xent.hip's)
   const int strips = (p.N + 2047) / 2048;
   const int64_t rows = over_rows(KIND) ? (int64_t)std::max(1, p.groups) * p.M : p.M;
   product_join_kernel<T, KIND><<<dim3((unsigned)(rows * strips)), dim3(256), 0, stream>>>(p, strips);

@@ -380,3 +380,30 @@ def test_many_tiles_of_short_sums(monkeypatch):
         t.check_forward()
         t.backward()
         t.check_backward()
+
+
+@pytest.mark.parametrize("rows", [5, 100])
+def test_infinities_and_nan_in_slices_of_the_reduction(monkeypatch, rows):
+    """Logits that are added up from slices, where rows are read in place and where they are copied."""
+    monkeypatch.setenv("STRIPE_TUNE", "product_splits=2")
+    inf = float("inf")
+    x, w = torch.ones(rows, 512, device="cuda"), torch.zeros(300, 512, device="cuda")
+    w[:, 0] = torch.linspace(-1, 1, 300)
+    w[7, 300] = inf
+    x[1:, 300] = 0.0
+    x[2] = NAN
+    x[4, 300] = NAN
+    targets = torch.full((rows,), 3, dtype=torch.int32, device="cuda")
+    targets[4] = -1
+    loss, lse = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    op = B.StripeXent(rows, 512, 300, "f32")
+    op.run(x, w, targets, loss, lse)
+    assert lse[0] == inf and loss[0] == inf and torch.isnan(lse[1:4]).all() and torch.isnan(loss[1:4]).all() and lse[4] == 0 and loss[4] == 0
+    w[7, 300], w[:, 400] = 0, -inf
+    op.run(torch.ones_like(x), w, targets, loss, lse)
+    assert (lse[:4] == -inf).all() and torch.isnan(loss[:4]).all()
+    w[:, 400] = 0
+    w[250:, 400] = -inf
+    op.run(torch.ones_like(x), w, targets, loss, lse)
+    want = torch.logsumexp(w[:250, 0].double(), 0)
+    assert (abs(lse[:4].double() - want) <= 64 * U * (1 + want.abs())).all()
