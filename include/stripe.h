@@ -310,6 +310,7 @@ stripe_status_t stripe_device_mfma(const void* operands, void* out, int iters, i
  *  - outputs must not overlap inputs or one another, except where stated (the same
  *    address is refused with STRIPE_ERR_INVALID_DESC, other overlaps are not looked for);
  *  - the same call on the same inputs gives the same bits (no atomics);
+ *  - a bf16 gated unit and cross entropy round their dz as the linear layer does;
  *  - a call that needs a workspace and has none of the caller's allocates it, once per
  *    device, and keeps it until the handle is destroyed; under graph capture such a first call
  *    is refused with STRIPE_ERR_NOMEM before anything is launched.  Calls (or
@@ -439,7 +440,8 @@ void stripe_gated_destroy(stripe_gated_t* gated);
  * x [rows][in_features], W [classes][in_features]; targets [rows]: int32 on the DEVICE; loss, lse, dloss, dlse [rows]: fp32.
  * A row whose target is not one of 0 .. classes - 1 does not count: x is not read there (it may hold anything), loss, lse and dx are 0, and dW
  * has nothing of it.  The backward pass computes z again, a piece of the vocabulary at a time; a piece's dz is in the workspace, rounded
- * to the operands' type.  dx is added up in fp32 over the pieces.
+ * to the operands' type.  In bf16 it is divided by the rows' largest |dloss| or |dloss + dlse| before and multiplied by it in dx and dW: of rows
+ * whose weights are less than 2^-110 of that, digits may be lost.  dx is added up in fp32 over the pieces.
  */
 typedef struct {
   int64_t rows;             /* 0 .. 2^24 */

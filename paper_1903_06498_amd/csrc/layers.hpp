@@ -132,7 +132,7 @@ struct XentRowsParams {
   const float *lse_in, *dloss, *dlse;        // nullptr: no gradient; ones; zeros
   void* rows_x;                              // [rows][x_ld], zeros behind column `features`
   int32_t *index, *span, *row_target;
-  int32_t* counts;                           // of many rows: those that count of each block of them, and the largest |dloss| of each
+  int32_t* counts;                           // of many rows: those that count of each block of them, and the largest weight of each
   float *row_lse, *row_all, *row_loss, *scale;
   float *loss, *lse;                         // forward: 0 where a row does not count
   void* dx;                                  // backward: the same

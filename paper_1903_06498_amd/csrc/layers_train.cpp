@@ -45,7 +45,8 @@ namespace {
 
 constexpr int64_t kMaxLayerRows = (int64_t)1 << 28, kMaxXentRows = (int64_t)1 << 24, kMaxXentFeatures = (int64_t)1 << 20;
 constexpr int64_t kNear = (int64_t)1 << 20;      // row strides up to which a tile's rows span less than 2^31 bytes
-// dz of a piece: what the products that follow read again is still in the 256 MB of the last level cache.
+// dz of a piece: what the products that follow read again is still in the 256 MB of the last level cache (8192 rows, 2048 -> 65536 bf16 with gradients: 8
+// pieces of 128 MB 6.47 ms, 2 of them 6.61, 4 6.49, 16 6.82).
 constexpr int64_t kPieceBytes = (int64_t)128 << 20, kMaxPiece = (int64_t)1 << 19;
 constexpr int64_t kMaxElements = (int64_t)1 << 34;
 constexpr int64_t kFewRows = 64;
@@ -80,7 +81,7 @@ stripe_status_t gated_create(const stripe_gated_desc_t* desc, stripe_gated_t** o
   if (!d.w_group) d.w_group = both * d.w_row;
   if (d.groups && d.w_group < (both - 1) * d.w_row + d.in_features) return api_fail(STRIPE_ERR_INVALID_DESC, "w_group is shorter than a matrix");
   if (beyond(d.groups, d.w_group)) return api_fail(STRIPE_ERR_INVALID_DESC, "a buffer spans more than 2^56 elements");
-  if (too_many_tiles(d.groups, d.rows, both) || too_many_tiles(d.groups, d.rows, d.in_features) || d.rows / 16 * (d.out_features / 256 + 1) >= 1 << 24 ||
+  if (too_many_tiles(d.groups, d.rows, both) || too_many_tiles(d.groups, d.rows, d.in_features) || (d.rows + 15) / 16 * (d.out_features / 256 + 1) >= 1 << 24 ||
       ((__int128)both / 64 + 1) * (d.in_features / 64 + 1) * std::max(1, d.groups) >= 1 << 24)
     return api_fail(STRIPE_ERR_UNSUPPORTED, "more than 2^24 tiles of outputs");
   auto gated = std::make_unique<stripe_gated>();
@@ -201,7 +202,7 @@ stripe_status_t xent_create(const stripe_xent_desc_t* desc, stripe_xent_t** out)
   // pieces of equal size, whole tiles of classes
   const int64_t most = std::min(kMaxPiece, std::max<int64_t>(256, kPieceBytes / e / std::max<int64_t>(1, d.rows) / 256 * 256));
   xent->pieces = (d.classes + most - 1) / most;
-  if (const int forced = tune_int("xent_pieces", 0); forced > 0) xent->pieces = std::max<int64_t>(xent->pieces, forced);
+  if (const int forced = tune_int("xent_pieces", 0); forced > 0) xent->pieces = std::max<int64_t>(forced, (d.classes + kMaxPiece - 1) / kMaxPiece);
   xent->piece = std::min(d.classes, ((d.classes + xent->pieces - 1) / xent->pieces + 255) / 256 * 256);
   xent->pieces = (d.classes + xent->piece - 1) / xent->piece;
   xent->x_ld = (d.in_features + v - 1) / v * v;

@@ -332,7 +332,8 @@ struct Tile {
   int k0, k;                    // kWeightGrad: first row of the reduction, and its length
 };
 
-constexpr unsigned kSpreadTiles = 32;      // of a matrix: from here on the XCDs' shares of it differ by an eighth at most
+// Whether every XCD takes its share of every group's tiles: shares of 4 of a matrix's tiles at least, and no more workgroups than a launch holds.
+__host__ __device__ constexpr bool spread(uint64_t tiles, uint64_t groups) { return tiles >= 32 && tiles * groups < 1 << 22; }
 
 // Tiles in patches of PATCH row tiles by all column tiles: neighbouring numbers (one XCD's) share panels of both operands.
 template <int KIND, int BM, int BN>
@@ -350,7 +351,7 @@ __device__ __forceinline__ bool place(const ProductParams& p, Tile* t) {
   }
   total = row_tiles * (unsigned)p.tiles_n;
   t->group = 0;
-  if (over_rows(KIND) && p.groups && total >= kSpreadTiles) {
+  if (over_rows(KIND) && p.groups && spread(total, (unsigned)p.groups)) {
     // An eighth of every group's tiles to each XCD: the groups' reductions are of very different lengths (8192 rows in 16 uneven groups, 1024 x 4096 features: 137 us
     // where an XCD had whole groups, 100 here).
     const unsigned x = blockIdx.x & 7u, i = blockIdx.x >> 3, first = total * x >> 3, own = (total * (x + 1) >> 3) - first;
@@ -1165,7 +1166,7 @@ hipError_t launch_kind(const ProductPlan& plan, Access access, ProductParams& p,
   int64_t total = (int64_t)p.tiles_m * p.tiles_n;
   if (p.groups) {
     // every group's last tile may be part of one
-    if (over_rows(KIND)) total = (total >= kSpreadTiles ? (total + 7) / 8 * 8 : total) * p.groups;
+    if (over_rows(KIND)) total = (spread((uint64_t)total, (uint64_t)p.groups) ? (total + 7) / 8 * 8 : total) * p.groups;
     else total = ((int64_t)p.M / bm + std::min<int64_t>(p.groups, p.M)) * p.tiles_n;
   }
   const dim3 grid((unsigned)((total + 7) / 8 * 8), (unsigned)plan.splits);

@@ -16,9 +16,10 @@ constexpr int kRowsEach = 4;           // rows of a workgroup that copies
 constexpr int64_t kManyRows = 16384;   // more of them are counted in blocks before
 
 __device__ __forceinline__ bool counts(const XentRowsParams& p, int64_t row) { return (uint32_t)p.targets[row] < (uint32_t)p.classes; }
-// What a row's dz is divided by at most: its dloss, where that is finite.
+// What a row's dz is divided by at most: the larger of its dloss and dloss + dlse, where they are finite.
 __device__ __forceinline__ float weight(const XentRowsParams& p, int64_t row) {
-  const float w = !counts(p, row) ? 0.f : p.dloss ? __builtin_fabsf(p.dloss[row]) : 1.f;
+  if (!counts(p, row)) return 0.f;
+  const float one = p.dloss ? p.dloss[row] : 1.f, all = p.dlse ? one + p.dlse[row] : one, w = fmaxf(__builtin_fabsf(one), __builtin_fabsf(all));
   return w < __builtin_inff() ? w : 0.f;
 }
 // A workgroup's total, and its largest value.
@@ -77,7 +78,7 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(const XentRowsParams p) 
   const uint64_t all = __ballot(mine);      // of the workgroup's rows, in every wavefront
   if (threadIdx.x == 0 && row0 + ROWS >= p.rows) p.span[0] = 0, p.span[1] = before + __builtin_popcountll(all);
   if (p.scale && blockIdx.x == 0) {
-    // bf16: dz is divided by the largest dloss, so that a target's dz, the value that matters most, lies in the upper half of a power of two, where
+    // bf16: dz is divided by the largest weight, so that a target's dz, the value that matters most, lies in the upper half of a power of two, where
     // rounding is half as coarse (equal weights and unsure targets: dz = -1 + p)
     float top = 0.f;
     if (sizeof(T) == 2) {

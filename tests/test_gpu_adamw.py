@@ -43,7 +43,7 @@ def encode(value, most, bits, least):
     return c.reshape(-1)[:n].astype(np.int32), scale[:, 0]
 
 
-def step8(m, ms, v, vs, g, number, seed, betas=(0.9, 0.999), factor=1.0):
+def step8(m, ms, v, vs, g, number, seed, betas=(0.9, 0.999), factor=1.0, first=0):
     """m, v before coding, and the new codes and factors."""
     block = np.arange(len(m)) // 256
     c, k = m.astype(F), v.astype(F)
@@ -55,7 +55,7 @@ def step8(m, ms, v, vs, g, number, seed, betas=(0.9, 0.999), factor=1.0):
     r = np.sqrt(vf)
     with np.errstate(over="ignore"):
         key = mix(np.array([(seed + number) & 0xFFFFFFFF], dtype=np.uint64))[0]
-        bits = mix((np.arange(len(m), dtype=np.uint64) + np.uint64(key)) & np.uint64(0xFFFFFFFF))
+        bits = mix((np.arange(first, first + len(m), dtype=np.uint64) + np.uint64(key)) & np.uint64(0xFFFFFFFF))
     cm, ms = encode(np.abs(mf), 127, bits & np.uint32(0xFFFF), 0)
     cv, vs = encode(r, 255, bits >> np.uint32(16), 1)
     return mf, vf, np.where(mf < 0, -cm, cm).astype(np.int8), ms, cv.astype(np.uint8), vs
@@ -223,6 +223,41 @@ def test_values_that_are_not_finite():
     t.g[0][300] = NAN
     t.op.run(1e-2, 1)
     assert torch.isnan(t.p[0]).sum() == torch.isnan(t.m[0]).sum() == torch.isnan(t.v[0]).sum() == 1
+
+
+def test_a_tensor_beyond_32_bits():
+    n = (1 << 32) + 777
+    p, grad = torch.zeros(n, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    m, v = torch.zeros(n, dtype=torch.int8, device="cuda"), torch.zeros(n, dtype=torch.uint8, device="cuda")
+    ms, vs = (torch.zeros(-(-n // 256), device="cuda") for _ in range(2))
+    parts = [slice(0, 1024), slice(1 << 31, (1 << 31) + 512), slice((1 << 32) - 256, n)]      # (each from a block's first element on)
+    g = torch.Generator(device="cuda").manual_seed(10)
+    for s in parts:
+        grad[s] = torch.randn(s.stop - s.start, generator=g, device="cuda").to(torch.bfloat16)
+    op = B.StripeAdamW([n], grads="bf16", states="8bit")
+    op.bind([p], [grad], [m], [v], [ms], [vs])
+    op.run(1e-2, 1, seed=77)
+    for s in parts:
+        count = s.stop - s.start
+        zero8, zeros = np.zeros(count, dtype=np.int8), np.zeros(-(-count // 256), dtype=F)
+        # the element's number enters the hash modulo 2^32
+        mf, vf, cm, sm, cv, sv = step8(zero8, zeros, zero8.astype(np.uint8), zeros, grad[s].float().cpu().numpy(), 0, 77, first=s.start)
+        b = slice(s.start // 256, -(-s.stop // 256))
+        for got, want in ((m[s], cm), (v[s], cv), (ms[b], sm), (vs[b], sv)):
+            assert np.array_equal(got.cpu().numpy(), want)
+        q = 1e-2 * mf.astype(np.float64) / 0.1 / (np.sqrt(vf.astype(np.float64) / 0.001) + 1e-8)
+        assert (abs(p[s].cpu().numpy() + q) <= 16 * U * abs(q)).all()
+    assert int((m != 0).sum()) <= sum(s.stop - s.start for s in parts) and int((p != 0).sum()) <= sum(s.stop - s.start for s in parts)
+
+
+def test_states_in_8_bits_of_more_tensors_than_a_launch_holds():
+    t = Tensors([(i * 37) % 700 + 1 for i in range(100)], states="8bit", seed=11)
+    p, g, m, v, ms, vs = t.host()
+    t.op.run(1e-2, 7, seed=5)
+    for i in range(100):
+        mf, vf, cm, sm, cv, sv = step8(m[i], ms[i], v[i], vs[i], g[i], i, 5)
+        for got, want in ((t.m, cm), (t.v, cv), (t.ms, sm), (t.vs, sv)):
+            assert np.array_equal(got[i].cpu().numpy(), want), i
 
 
 def test_more_tensors_than_a_launch_holds():

@@ -282,3 +282,39 @@ def test_more_tiles_than_compute_units(monkeypatch, cin, offsets):
     t.forward()
     t.backward()
     t.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_buffers_beyond_32_bits(dtype):
+    """Rows of every buffer so far apart that the last lies more than 2^32 elements in."""
+    rows, cin, n, dt = 90, 40, 48, TYPES[dtype]
+    far = (1 << 32) // 85
+    t = Gated(rows, cin, n, dtype, seed=16)
+
+    def spread(v, like):
+        s = torch.empty(v.shape[0] * far, dtype=dt, device="cuda").as_strided(v.shape, (far, 1))
+        return s.copy_(v) if like else s
+
+    op = B.StripeGated(rows, cin, n, dtype, x_row=far, w_row=far, y_row=far, pre_row=far)
+    x, w, dy, pre_in = (spread(v, True) for v in (t.x, t.w, t.dy, t.pre_in))
+    y, pre, dx, dw = (spread(t.outs[k][1], False) for k in ("y", "pre", "dx", "dw"))
+    op.run(x, w, y, pre=pre)
+    op.backward(dy, x, w, pre_in, dx=dx, dw=dw)
+    for k, v in (("y", y), ("pre", pre), ("dx", dx), ("dw", dw)):
+        t.outs[k][1].copy_(v)
+    t.check()
+
+
+def test_experts_far_apart_and_many_of_their_tiles():
+    """Weight gradients whose matrices' tiles are spread over the XCDs, matrices beyond 2^32 elements, groups without rows."""
+    rows, cin, n, groups = 700, 520, 1100, 5
+    offsets = [0, 0, 500, 512, 512, 700]
+    far = 1 << 30
+    t = Gated(rows, cin, n, "bf16", offsets=offsets, seed=17)
+    w, dw = (torch.empty(groups * far, dtype=torch.bfloat16, device="cuda").as_strided((groups, 2 * n, cin), (far, cin, 1)) for _ in range(2))
+    w.copy_(t.w)
+    op = B.StripeGated(rows, cin, n, "bf16", groups=groups, w_group=far)
+    op.run(t.x, w, t.outs["y"][1], offsets=t.offsets, pre=t.outs["pre"][1])
+    op.backward(t.dy, t.x, w, t.pre_in, offsets=t.offsets, dx=t.outs["dx"][1], dw=dw)
+    t.outs["dw"][1].copy_(dw)
+    t.check()

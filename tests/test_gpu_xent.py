@@ -407,3 +407,44 @@ def test_infinities_and_nan_in_slices_of_the_reduction(monkeypatch, rows):
     op.run(torch.ones_like(x), w, targets, loss, lse)
     want = torch.logsumexp(w[:250, 0].double(), 0)
     assert (abs(lse[:4].double() - want) <= 64 * U * (1 + want.abs())).all()
+
+
+def test_dlse_much_larger_than_dloss():
+    """dz is divided by the larger of the two weights: nothing overflows."""
+    t = Xent(60, 64, 100, "bf16", seed=21)
+    t.dloss.mul_(1e-25)
+    t.dlse.mul_(1e20)
+    t.backward()
+    t.check_backward()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_buffers_beyond_32_bits(dtype):
+    """Rows of W and dW 2^20 elements apart, the last of them more than 2^32 elements into its buffer."""
+    rows, cin, classes, far = 70, 40, 4200, 1 << 20
+    t = Xent(rows, cin, classes, dtype, seed=22)
+    w = torch.empty(classes * far, dtype=TYPES[dtype], device="cuda").as_strided((classes, cin), (far, 1))
+    dw = torch.empty(classes * far, dtype=TYPES[dtype], device="cuda").as_strided((classes, cin), (far, 1))
+    w.copy_(t.w)
+    op = B.StripeXent(rows, cin, classes, dtype, w_row=far)
+    op.run(t.x, w, t.targets, t.loss, t.lse)
+    t.check_forward()
+    op.backward(t.x, w, t.targets, t.lse_in(), dloss=t.dloss, dlse=t.dlse, dx=t.outs["dx"][1], dw=dw)
+    t.outs["dw"][1].copy_(dw)
+    t.check_backward()
+
+
+@pytest.mark.parametrize("rows", [40, 300])
+def test_rows_beyond_32_bits(rows):
+    """Rows of x and dx so far apart that the last lies more than 2^32 elements in."""
+    cin, classes, far = 40, 90, (1 << 32) // 36
+    t = Xent(rows, cin, classes, "bf16", seed=23)
+    far = far if rows == 40 else (1 << 32) // 290
+    x, dx = (torch.empty(rows * far, dtype=torch.bfloat16, device="cuda").as_strided((rows, cin), (far, 1)) for _ in range(2))
+    x.copy_(t.x)
+    op = B.StripeXent(rows, cin, classes, "bf16", x_row=far)
+    op.run(x, t.w, t.targets, t.loss, t.lse)
+    t.check_forward()
+    op.backward(x, t.w, t.targets, t.lse_in(), dloss=t.dloss, dlse=t.dlse, dx=dx, dw=t.outs["dw"][1])
+    t.outs["dx"][1].copy_(dx)
+    t.check_backward()

@@ -22,6 +22,7 @@ def _status(call):
     (dict(groups=4097), "ERR_INVALID_DESC"), (dict(dtype="i8"), "ERR_UNSUPPORTED"), (dict(x_row=31), "ERR_INVALID_DESC"), (dict(w_row=31), "ERR_INVALID_DESC"),
     (dict(y_row=47), "ERR_INVALID_DESC"), (dict(pre_row=95), "ERR_INVALID_DESC"), (dict(groups=2, w_group=96 * 32 - 1), "ERR_INVALID_DESC"),
     (dict(pre_row=(1 << 40) + 8), "ERR_INVALID_DESC"), (dict(rows=1 << 28, out_features=1 << 20), "ERR_UNSUPPORTED"), (dict(rows=1 << 28), "ERR_UNSUPPORTED"),
+    (dict(rows=(1 << 28) - 1), "ERR_UNSUPPORTED"),
 ])
 def test_gated_create_refuses(change, status):
     args = dict(rows=16, in_features=32, out_features=48, dtype="bf16")
