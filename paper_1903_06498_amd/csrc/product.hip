@@ -108,7 +108,7 @@ TileTime tile_time(int tile, int dtype, Access access, bool parts) {
     return tile == kLeastTile ? TileTime{0.5, 1.0, 2, 4} : TileTime{0.95, 1.95, 3, 5};
   }
   if (access != kPieces) return {0.75, 1.1, 3, 5};
-  constexpr TileTime t[] = {{1.1, 1.45, 6, 9}, {0.56, 0.76, 4, 5}, {0.28, 0.5, 3, 5}, {0.22, 0.35, 2, 4}};
+  constexpr TileTime t[] = {{1.03, 1.36, 6, 9}, {0.56, 0.76, 4, 5}, {0.28, 0.5, 3, 5}, {0.22, 0.35, 2, 4}};
   return t[tile];
 }
 

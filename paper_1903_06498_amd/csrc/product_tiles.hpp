@@ -938,14 +938,20 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductParams p) 
 //   rows R + R/2 .. 2 R - 1     the fragment reads of tile kt + 1's step 0, and the first half of tile kt + S's loads, into tile kt's stage.
 // (All of a tile's loads behind the barrier: 4096^3 on zeros 94 us instead of 87; over three quarters of a tile: 90.)
 // Behind the last tile the loop loads zeros and reads fragments that nobody uses: the counts then never change.
+// Tiles of 256 x 256, whose two stages leave 32 KB of LDS: a third stage of B (SB = S + 1), the operand that more often comes from memory (weights; A's
+// panels are shared by more tiles).  Both loads of a tile are then for K tile kt + 2, B's with 1 3/4 tiles of time to arrive instead of 3/4
+// (inputs from memory, bf16: a gated unit of 4096 rows, 4096 -> 8192 432 -> 405 us; 8192 rows in 16 groups, 1024 -> 2048 with gradients 347 -> 321; the cross
+// entropy of 8192 rows, 2048 -> 65536 with gradients 6.45 -> 6.30 ms).
 #define PRODUCT_FENCE() __builtin_amdgcn_sched_barrier(0)
 
-template <typename T, int KIND, int FM, int FN, int S, int WAVES, int PIECE>
+template <typename T, int KIND, int FM, int FN, int S, int SB, int WAVES, int PIECE>
 __global__ __launch_bounds__(64 * WAVES, S * 64 * (FM + FN) * kDepthBytes > 80 * 1024 ? 1 : 2) void product_stream_kernel(const ProductParams p) {
   constexpr int BM = 64 * FM, BN = 64 * FN, R = 2 * FM, C = 8 * FN / WAVES;      // fragments of a wavefront
   using A = Stream<T, BM, over_rows(KIND), WAVES, PIECE>;
   using B = StreamOf<T, KIND, BN, 16 * C, WAVES, PIECE>;
   constexpr int LOADS = A::LOADS + B::LOADS, HALF = R / 2;
+  constexpr bool MORE = SB == S + 1;
+  static_assert(MORE ? S == 2 && A::LOADS == B::LOADS : SB == S, "the first half of a tile's loads is A's, the second B's");
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   unsigned char *const lds_a = lds, *const lds_b = lds + S * A::STAGE;
   Tile t;
@@ -992,14 +998,18 @@ __global__ __launch_bounds__(64 * WAVES, S * 64 * (FM + FN) * kDepthBytes > 80 *
       b.base += b.step;
     };
 #pragma unroll
-    for (int i = 0; i < S - 1; ++i) {
+    for (int i = 0; i < S - !MORE; ++i) {
       cut(0, LOADS, left);
       load(0, LOADS, i);
       next();
     }
-    cut(0, LOADS / 2, left);
-    load(0, LOADS / 2, S - 1);
-    wait_loads<LOADS / 2 + (S - 2) * LOADS>();
+    if constexpr (MORE) {
+      wait_loads<LOADS>();
+    } else {
+      cut(0, LOADS / 2, left);
+      load(0, LOADS / 2, S - 1);
+      wait_loads<LOADS / 2 + (S - 2) * LOADS>();
+    }
     asm volatile("s_barrier" ::: "memory");
     const unsigned first_a = A::first(wm * R * 16), first_b = B::first(wn * C * 16);
     u32x4 fa[R], fb[2][C];
@@ -1009,14 +1019,15 @@ __global__ __launch_bounds__(64 * WAVES, S * 64 * (FM + FN) * kDepthBytes > 80 *
     for (int i = 0; i < R; ++i) fa[i] = A::fragment(lds_a, first_a, i, 0);
 
     const int tiles = kt1 - kt0;
-    int cur = 0, before = S - 1;      // stages of tile kt and of tile kt - 1
+    int cur = 0, before = SB - 1;              // stages of tile kt and, of B, of tile kt - 1
+    int at_b = 0;                              // B's stage of tile kt
     for (int kt = 0; kt < tiles; ++kt) {
-      const int nxt = cur + 1 == S ? 0 : cur + 1;
-      if (left < 2 * A::DEPTH) {      // (here and not beside the loads: the rest of the loop is one block)
+      const int nxt = cur + 1 == S ? 0 : cur + 1, next_b = at_b + 1 == SB ? 0 : at_b + 1;
+      if (left < (MORE ? 1 : 2) * A::DEPTH) {      // (here and not beside the loads: the rest of the loop is one block)
         cut(LOADS / 2, LOADS, left);
-        cut(0, LOADS / 2, left - A::DEPTH);
+        cut(0, LOADS / 2, MORE ? left : left - A::DEPTH);
       }
-      unsigned cur_a = first_a + cur * A::STAGE, cur_b = first_b + cur * B::STAGE, nxt_a = first_a + nxt * A::STAGE, nxt_b = first_b + nxt * B::STAGE;
+      unsigned cur_a = first_a + cur * A::STAGE, cur_b = first_b + at_b * B::STAGE, nxt_a = first_a + nxt * A::STAGE, nxt_b = first_b + next_b * B::STAGE;
       // (opaque: else every fragment's address would be kept in a register of its own over the whole loop)
       asm volatile("" : "+v"(cur_a), "+v"(cur_b), "+v"(nxt_a), "+v"(nxt_b));
       auto read_b = [&](int st, unsigned at, int first, int last) {
@@ -1033,7 +1044,7 @@ __global__ __launch_bounds__(64 * WAVES, S * 64 * (FM + FN) * kDepthBytes > 80 *
       for (int row = 0; row < 2 * R; ++row) {
         const int st = row / R, i = row % R;
         if (row == R + HALF) {
-          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((S - 2) * LOADS) : "memory");
+          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((S - 2) * LOADS + (MORE ? LOADS / 2 : 0)) : "memory");
           asm volatile("s_barrier" ::: "memory");
           PRODUCT_FENCE();
         }
@@ -1052,9 +1063,10 @@ __global__ __launch_bounds__(64 * WAVES, S * 64 * (FM + FN) * kDepthBytes > 80 *
           load(at * (LOADS / 2) / HALF, (at + 1) * (LOADS / 2) / HALF, cur);
         }
         PRODUCT_FENCE();
-        if (row == HALF - 1) next();
+        if (row == (MORE ? 2 * R - 1 : HALF - 1)) next();
       }
-      before = cur;
+      before = at_b;
+      at_b = next_b;
       cur = nxt;
     }
     wait_loads<0>();
@@ -1122,14 +1134,14 @@ __global__ __launch_bounds__(256) void product_join_kernel(const ProductParams p
 
 // ---- host ---------------------------------------------------------------------
 struct TileShape {
-  int fm, fn, stages, resident, waves;      // resident: workgroups that fit a CU
+  int fm, fn, stages, stages_b, resident, waves;      // resident: workgroups that fit a CU
 };
 // What each is for, bf16: 0 many outputs (4096^3: 100 us, 112 and 150 on the next two); 1 half as many, or groups of a few hundred rows (8192 rows of
 // 32 groups, 2048 -> 4096: 216, 199, 274; 2048 x 4096 x 4096: 83, 57, 76); 2 few of them, and fp32, whose matrix instructions take so long that
 // nothing else matters; 3 so few that tile 2's would leave CUs idle (1024^3: 8.5 us on tile 2, 6.9; fp32 1000^3: 27.3 and 21.5; 777 rows of 5
 // groups, 200 -> 328, fp32: 12.0 and 8.2).  Operands that are no whole 16-byte pieces: fp32 loads words into LDS instead (1000 x 777 x 1283: 31 us
 // and 32 through the registers; 333 x 555 x 777: 12.7 and 15.0), bf16 runs on product_kernel in tile 2's shape.
-constexpr TileShape kTiles[] = {{4, 4, 2, 1, 8}, {2, 4, 3, 1, 8}, {1, 2, 3, 2, 4}, {1, 1, 4, 2, 4}};
+constexpr TileShape kTiles[] = {{4, 4, 2, 3, 1, 8}, {2, 4, 3, 3, 1, 8}, {1, 2, 3, 3, 2, 4}, {1, 1, 4, 4, 2, 4}};
 constexpr int kTileCount = 4, kSmallTile = 2, kLeastTile = 3;
 
 // A kernel's LDS beyond 64 KB has to be allowed once on each device.
@@ -1147,12 +1159,12 @@ hipError_t allow_lds(K kernel, int bytes, std::atomic<uint64_t>& done) {
 template <typename T, int KIND, int TILE, int PIECE = 16>
 hipError_t launch_stream(const ProductParams& p, dim3 grid, hipStream_t stream) {
   constexpr TileShape s = kTiles[TILE];
-  constexpr int bytes = s.stages * 64 * (s.fm + s.fn) * kDepthBytes;
+  constexpr int bytes = 64 * (s.stages * s.fm + s.stages_b * s.fn) * kDepthBytes;
   if constexpr (bytes > 65536) {
     static std::atomic<uint64_t> done{0};
-    if (const hipError_t e = allow_lds(product_stream_kernel<T, KIND, s.fm, s.fn, s.stages, s.waves, PIECE>, bytes, done); e != hipSuccess) return e;
+    if (const hipError_t e = allow_lds(product_stream_kernel<T, KIND, s.fm, s.fn, s.stages, s.stages_b, s.waves, PIECE>, bytes, done); e != hipSuccess) return e;
   }
-  product_stream_kernel<T, KIND, s.fm, s.fn, s.stages, s.waves, PIECE><<<grid, dim3(64 * s.waves), bytes, stream>>>(p);
+  product_stream_kernel<T, KIND, s.fm, s.fn, s.stages, s.stages_b, s.waves, PIECE><<<grid, dim3(64 * s.waves), bytes, stream>>>(p);
   return hipGetLastError();
 }
 
