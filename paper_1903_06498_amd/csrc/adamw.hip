@@ -55,7 +55,10 @@ __device__ __forceinline__ void load4(const T* q, int n, T (&to)[4]) {
 template <typename T>
 __device__ __forceinline__ void store4(T* q, int n, const T (&from)[4]) {
   if (n >= 4) {
-    __builtin_memcpy(q, from, 4 * sizeof(T));
+    typedef T vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    vec v;
+    __builtin_memcpy(&v, from, 4 * sizeof(T));
+    __builtin_nontemporal_store(v, (vec*)q);
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
