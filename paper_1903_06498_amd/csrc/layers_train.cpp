@@ -49,7 +49,7 @@ constexpr int64_t kNear = (int64_t)1 << 20;      // row strides up to which a ti
 // pieces of 128 MB 6.47 ms, 2 of them 6.61, 4 6.49, 16 6.82).
 constexpr int64_t kPieceBytes = (int64_t)128 << 20, kMaxPiece = (int64_t)1 << 19;
 constexpr int64_t kMaxElements = (int64_t)1 << 34;
-constexpr int64_t kFewRows = 64;
+constexpr int64_t kFewRows = 64, kHalfRows = 512, kMostSlices = (int64_t)128 << 20;
 
 // a launch holds fewer than 2^32 lanes: 2^24 workgroups of 256, counted in tiles of 64 x 64 outputs, the smallest
 bool too_many_tiles(int64_t images, int64_t m, int64_t n) { return ((__int128)images + m / 64 + 1) * (n / 64 + 1) >= 1 << 24; }
@@ -217,6 +217,13 @@ stripe_status_t xent_create(const stripe_xent_desc_t* desc, stripe_xent_t** out)
   for (const Access access : {xent->best, xent->otherwise}) {
     xent->logits[access] = plan_product(kForward, d.dtype, d.rows, d.in_features, d.classes, 0, access, odd, kLogits);
     xent->dx[access] = plan_product(kInputGrad, d.dtype, d.rows, d.in_features, xent->piece, 0, access, odd);
+    if (xent->dx[access].splits > 1 && d.rows <= kHalfRows) {
+      // So few rows that the reduction is split: for half of them, as many may count (205 of 512 rows, 50001 -> 4096 bf16: 193 us in slices for all, 122; 900 of
+      // 1000 fp32, 10007 -> 333, would lose: 67 us, 83).
+      ProductPlan half = plan_product(kInputGrad, d.dtype, (d.rows + 1) / 2, d.in_features, xent->piece, 0, access, odd);
+      half.ws_bytes = half.splits > 1 ? half.splits * d.rows * d.in_features * 4 : 0;
+      if (half.ws_bytes <= kMostSlices) xent->dx[access] = half;
+    }
     // (a piece's logits in slices: its classes end in zeros up to a multiple of 8)
     const int64_t slices = xent->logits[access].splits > 1 ? xent->logits[access].splits * d.rows * xent->dz_ld * 4 : 0;
     xent->partial_bytes = std::max({xent->partial_bytes, xent->dx[access].ws_bytes, xent->logits[access].ws_bytes, slices});
