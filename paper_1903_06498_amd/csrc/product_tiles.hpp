@@ -341,8 +341,17 @@ __device__ __forceinline__ bool place(const ProductParams& p, Tile* t) {
   constexpr unsigned PATCH = BM >= 256 ? 4 : 8;
   unsigned row_tiles = (unsigned)p.tiles_m, total, l;
   GroupChunk chunk;      // of up to 64 groups: all of them
+  const bool one = KIND >= kLogSum && p.groups;      // a cross entropy's rows are one group, which needs no search
+  int start = 0, end = p.M;
+  if (one) {
+    start = limited(p.offsets[0], p.rows);
+    end = limited(p.offsets[1], p.rows);
+    end = end > start ? end : start;
+  }
   if (!over_rows(KIND) && p.groups) {
-    if (p.groups <= 64) {
+    if (one) {
+      row_tiles = (unsigned)((end - start + BM - 1) / BM);
+    } else if (p.groups <= 64) {
       chunk = group_chunk(p.offsets, p.groups, p.rows, 0, limited(p.offsets[0], p.rows), 0, BM);
       row_tiles = (unsigned)lane_value(chunk.through, 63);
     } else {
@@ -373,7 +382,10 @@ __device__ __forceinline__ bool place(const ProductParams& p, Tile* t) {
   t->n0 = tn * (KIND == kGated ? BN / 2 : BN);
   t->k0 = 0;
   t->k = p.K;
-  if (!over_rows(KIND) && p.groups) {
+  if (!over_rows(KIND) && one) {
+    t->m0 = start + tm * BM;
+    t->m = end - t->m0 < BM ? end - t->m0 : BM;
+  } else if (!over_rows(KIND) && p.groups) {
     RowTile r = {0, 0, 0};
     if (p.groups <= 64) tile_in_chunk(chunk, 0, BM, tm, &r);
     else r = find_row_tile(p.offsets, p.groups, p.rows, BM, tm);
@@ -384,8 +396,9 @@ __device__ __forceinline__ bool place(const ProductParams& p, Tile* t) {
     t->m0 = tm * BM;
     t->m = p.M - t->m0 < BM ? p.M - t->m0 : BM;
     if (over_rows(KIND) && p.groups) {
-      int end, unused;
-      group_rows(p.offsets, p.groups, p.rows, t->group, 1, &t->k0, &end, &unused);
+      int unused;
+      if (one) t->k0 = start;
+      else group_rows(p.offsets, p.groups, p.rows, t->group, 1, &t->k0, &end, &unused);
       t->k = end - t->k0;
     }
   }
