@@ -1155,8 +1155,8 @@ __global__ __launch_bounds__(256) void product_join_kernel(const ProductParams p
 struct TileShape {
   int fm, fn, stages, stages_b, resident, waves;      // resident: workgroups that fit a CU
 };
-// What each is for, bf16: 0 many outputs (4096^3: 100 us, 112 and 150 on the next two); 1 half as many, or groups of a few hundred rows (8192 rows of
-// 32 groups, 2048 -> 4096: 216, 199, 274; 2048 x 4096 x 4096: 83, 57, 76); 2 few of them, and fp32, whose matrix instructions take so long that
+// What each is for, bf16: 0 many outputs (4096^3: 101 us, 105 and 146 on the next two); 1 half as many, or groups of a few hundred rows (8192 rows of
+// 32 groups, 2048 -> 4096: 216, 199, 274; 2048 x 4096 x 4096: 73, 54, 73); 2 few of them, and fp32, whose matrix instructions take so long that
 // nothing else matters; 3 so few that tile 2's would leave CUs idle (1024^3: 8.5 us on tile 2, 6.9; fp32 1000^3: 27.3 and 21.5; 777 rows of 5
 // groups, 200 -> 328, fp32: 12.0 and 8.2).  Operands that are no whole 16-byte pieces: fp32 loads words into LDS instead (1000 x 777 x 1283: 31 us
 // and 32 through the registers; 333 x 555 x 777: 12.7 and 15.0), bf16 runs on product_kernel in tile 2's shape.
