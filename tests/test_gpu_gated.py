@@ -318,3 +318,14 @@ def test_experts_far_apart_and_many_of_their_tiles():
     op.backward(t.dy, t.x, w, t.pre_in, offsets=t.offsets, dx=t.outs["dx"][1], dw=dw)
     t.outs["dw"][1].copy_(dw)
     t.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("groups", [65, 130, 4096])
+def test_more_groups_than_a_wavefront_has_lanes(groups, dtype):
+    rows = 600
+    ends = [0] + sorted(int(v) for v in torch.randint(0, rows + 1, (groups - 1,), generator=torch.Generator().manual_seed(groups))) + [rows]
+    t = Gated(rows, 24, 20, dtype, offsets=ends, seed=18)
+    t.forward()
+    t.backward()
+    t.check()

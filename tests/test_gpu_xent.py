@@ -448,3 +448,13 @@ def test_rows_beyond_32_bits(rows):
     op.backward(x, t.w, t.targets, t.lse_in(), dloss=t.dloss, dlse=t.dlse, dx=dx, dw=t.outs["dw"][1])
     t.outs["dx"][1].copy_(dx)
     t.check_backward()
+
+
+@pytest.mark.parametrize("rows", [1, 3, 70])
+def test_more_classes_than_a_piece_holds(rows):
+    """More than 2^19 classes: pieces, however few the rows are."""
+    t = Xent(rows, 16, 600011, "bf16", ignored=0.0, seed=24, pieces=2)
+    t.forward()
+    t.check_forward()
+    t.backward()
+    t.check_backward()
