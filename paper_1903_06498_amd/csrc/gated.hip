@@ -55,7 +55,30 @@ __global__ __launch_bounds__(256) void gated_grad_kernel(const GatedGradParams p
   }
 }
 
+// A thread copies four pieces, a workgroup's pieces one after the other.
+__global__ __launch_bounds__(256) void pad_kernel(const PadParams p) {
+  const unsigned pieces = (unsigned)(p.to_row / 8);
+  const int64_t total = p.rows * pieces, first = (int64_t)blockIdx.x * 1024 + threadIdx.x;
+  u32x4 v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t at = first + 256 * i;
+    if (at >= total) break;
+    const int64_t row = at / pieces, c = (at - row * pieces) * 8, m = row / p.each;
+    v[i] = load_piece<__bf16>((const __bf16*)p.from + m * p.from_matrix + (row - m * p.each) * p.from_row + c, (int)(p.cols - c));
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (first + 256 * i < total) *(u32x4*)((__bf16*)p.to + (first + 256 * i) * 8) = v[i];
+}
+
 }  // namespace
+
+hipError_t launch_pad(const PadParams& p, hipStream_t stream) {
+  const int64_t total = p.rows * (p.to_row / 8);
+  pad_kernel<<<dim3((unsigned)((total + 1023) / 1024)), dim3(256), 0, stream>>>(p);
+  return hipGetLastError();
+}
 
 hipError_t launch_gated(int dtype, const ProductPlan& plan, Access access, ProductParams p, hipStream_t stream) {
   if (plan.few) return launch_product_rows(kGated, dtype, p, stream);

@@ -86,6 +86,7 @@ struct ProductPlan {
   bool parts = false;       // fp32 in three bf16 parts
   bool few = false;         // kForward: the kernel for few rows (product_rows.hip)
   int64_t ws_bytes = 0;     // partial images
+  double us = 0;            // estimated time
 };
 // How a product's operands can be fetched: element by element at their rims; in whole 16-byte pieces (addresses, strides and contiguous extents are
 // multiples of them); in 4-byte words (fp32).  The latter two also want a tile's rows to span less than 2^31 bytes.
@@ -120,6 +121,14 @@ struct GatedGradParams {
   int64_t y_row, pre_row, dz_row;
   int32_t rows, out, act;
 };
+// Rows of bf16 that start anywhere, copied to rows of whole 16-byte pieces, zeros behind column `cols`.  Row r comes from matrix r / each, row r % each.
+struct PadParams {
+  const void* from;
+  void* to;
+  int64_t rows, each, from_row, from_matrix, to_row;
+  int32_t cols;
+};
+hipError_t launch_pad(const PadParams& p, hipStream_t stream);
 hipError_t launch_gated(int dtype, const ProductPlan& plan, Access access, ProductParams p, hipStream_t stream);
 hipError_t launch_gated_grad(int dtype, const GatedGradParams& p, hipStream_t stream);
 

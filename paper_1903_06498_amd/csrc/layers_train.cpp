@@ -14,21 +14,25 @@ struct stripe_gated {
   Access best = kAny, otherwise = kAny;      // with W and x aligned to 16 bytes, and else
   ProductPlan plan[3][3];                    // [Access][forward, dx, dW]
   int64_t dz_row = 0, dz_bytes = 0, partial_bytes = 0;
+  bool copies[3] = {false, false, false};    // this product reads copies of W and x (forward), of W (dx), of x (dW) in whole pieces
+  int64_t copy_row = 0, w_bytes = 0, x_bytes = 0;
   Workspace ws;
-  int64_t ws_bytes() const { return dz_bytes + partial_bytes; }
+  int64_t ws_bytes() const { return dz_bytes + partial_bytes + w_bytes + x_bytes; }
 };
 
 struct stripe_xent {
   stripe_xent_desc_t d;
   Access best = kAny, otherwise = kAny;      // with W aligned to 16 bytes, and else
   Access copies = kAny;                      // of products that read the workspace only
+  bool w_copy[2] = {false, false};           // forward, backward: W is copied to rows of whole pieces
+  int64_t w_bytes = 0;
   ProductPlan logits[3], dx[3], dw;          // [Access]
   int64_t piece = 0, pieces = 0;             // classes of a piece of the backward pass
   int64_t x_ld = 0, dz_ld = 0;
   // the workspace: rows' numbers and values, x's rows; then, forward: the tiles' sums, backward: dz, dx in fp32; partial images
   int64_t count_bytes = 0, row_bytes = 0, x_bytes = 0, stats_bytes = 0, dz_bytes = 0, sum_bytes = 0, partial_bytes = 0;
   Workspace ws;
-  int64_t ws_bytes() const { return 256 + 256 + count_bytes + 6 * row_bytes + x_bytes + std::max(stats_bytes, dz_bytes + sum_bytes) + partial_bytes; }
+  int64_t ws_bytes() const { return 256 + 256 + count_bytes + 6 * row_bytes + x_bytes + std::max(stats_bytes, dz_bytes + sum_bytes) + partial_bytes + w_bytes; }
 };
 
 struct stripe_adamw {
@@ -50,6 +54,17 @@ constexpr int64_t kNear = (int64_t)1 << 20;      // row strides up to which a ti
 constexpr int64_t kPieceBytes = (int64_t)128 << 20, kMaxPiece = (int64_t)1 << 19;
 constexpr int64_t kMaxElements = (int64_t)1 << 34;
 constexpr int64_t kFewRows = 64, kHalfRows = 512, kMostSlices = (int64_t)128 << 20;
+
+// Rows of bf16 that are no whole pieces go through registers, on the smallest tiles.  Where the estimates say so they are copied first: a launch, and the bytes
+// read and written (a gated unit of 8192 rows, 4095 -> 4096: 986 us forward and 2095 backward through registers, 430 and 845; the cross entropy of 4096 rows,
+// 1324 -> 15104: 293 and 760, 175 and 473).
+constexpr int64_t kMostCopied = (int64_t)2 << 30;
+double copy_time(int64_t bytes) { return 4 + 2 * (double)bytes / 4.5e6; }
+// (STRIPE_TUNE's layers_copy: 0 never, 1 wherever it can be)
+bool copy_pays(double with, double without) {
+  const int forced = tune_int("layers_copy", -1);
+  return forced < 0 ? with < without : forced != 0;
+}
 
 // a launch holds fewer than 2^32 lanes: 2^24 workgroups of 256, counted in tiles of 64 x 64 outputs, the smallest
 bool too_many_tiles(int64_t images, int64_t m, int64_t n) { return ((__int128)images + m / 64 + 1) * (n / 64 + 1) >= 1 << 24; }
@@ -98,6 +113,20 @@ stripe_status_t gated_create(const stripe_gated_desc_t* desc, stripe_gated_t** o
       gated->partial_bytes = std::max(gated->partial_bytes, round_up_256(gated->plan[access][k].ws_bytes));
     }
   gated->dz_bytes = round_up_256(d.rows * gated->dz_row * e);
+  gated->copy_row = (d.in_features + v - 1) / v * v;
+  const int64_t matrices = std::max(1, d.groups) * both, w_bytes = round_up_256(matrices * gated->copy_row * e), x_bytes = round_up_256(d.rows * gated->copy_row * e);
+  if (d.rows && d.dtype == STRIPE_BF16 && gated->best == kAny && gated->copy_row <= kNear && gated->dz_row <= kNear && w_bytes + x_bytes <= kMostCopied) {
+    for (int k = 0; k < 3; ++k) {
+      const ProductPlan plan = plan_product((ProductKind)k, d.dtype, d.rows, d.in_features, both, d.groups, kPieces, odd, kHalves);
+      const int64_t bytes = k == kForward ? w_bytes + x_bytes : k == kInputGrad ? w_bytes : x_bytes;
+      if (plan.few || !copy_pays(plan.us + copy_time(bytes) + (k == kForward ? 4 : 0), gated->plan[kAny][k].us)) continue;
+      gated->copies[k] = true;
+      gated->plan[kPieces][k] = plan;
+      gated->partial_bytes = std::max(gated->partial_bytes, round_up_256(plan.ws_bytes));
+      if (k != kWeightGrad) gated->w_bytes = w_bytes;
+      if (k != kInputGrad) gated->x_bytes = x_bytes;
+    }
+  }
   *out = gated.release();
   return STRIPE_OK;
 }
@@ -107,6 +136,24 @@ stripe_status_t check_offsets(int groups, const int32_t* offsets) {
   if (!groups && offsets) return api_fail(STRIPE_ERR_INVALID_DESC, "offsets without groups");
   if (misaligned(offsets, 4)) return api_fail(STRIPE_ERR_MISALIGNED, "offsets are not aligned to 4 bytes");
   return STRIPE_OK;
+}
+
+// A copy of x or of W in whole pieces, which the product is to read.
+stripe_status_t gated_copy(const stripe_gated_t* gated, const void* x, const void* w, unsigned char* ws, ProductParams& p, hipStream_t stream) {
+  const stripe_gated_desc_t& d = gated->d;
+  unsigned char* const w_copy = ws + gated->dz_bytes + gated->partial_bytes;
+  PadParams c = {};
+  c.to_row = gated->copy_row; c.cols = (int32_t)d.in_features;
+  if (w) {
+    c.from = w; c.to = w_copy;
+    c.each = 2 * d.out_features; c.rows = std::max(1, d.groups) * c.each; c.from_row = d.w_row; c.from_matrix = d.w_group;
+    p.b = c.to; p.b_ld = c.to_row; p.b_group = c.each * c.to_row;
+  } else {
+    c.from = x; c.to = w_copy + gated->w_bytes;
+    c.each = c.rows = d.rows; c.from_row = d.x_row;
+    p.a = c.to; p.a_ld = c.to_row;
+  }
+  return launched(launch_pad(c, stream));
 }
 
 stripe_status_t gated_run(stripe_gated_t* gated, const void* x, const void* w, const int32_t* offsets, void* y, void* pre, void* hip_stream) {
@@ -119,16 +166,21 @@ stripe_status_t gated_run(stripe_gated_t* gated, const void* x, const void* w, c
     return api_fail(STRIPE_ERR_MISALIGNED, "a buffer is not aligned to its element type");
   if (!d.rows) return STRIPE_OK;
   if (shared({y, pre}, {x, w, offsets})) return api_fail(STRIPE_ERR_INVALID_DESC, "y or pre is an input, or one another");
-  const Access access = misaligned(x, 16) || misaligned(w, 16) ? gated->otherwise : gated->best;
+  const bool copies = gated->copies[kForward];
+  const Access access = copies ? kPieces : misaligned(x, 16) || misaligned(w, 16) ? gated->otherwise : gated->best;
   const ProductPlan& plan = gated->plan[access][kForward];
   unsigned char* ws = nullptr;
-  if (plan.ws_bytes)
+  if (plan.ws_bytes || copies)
     if (const stripe_status_t st = gated->ws.get(gated->ws_bytes(), (hipStream_t)hip_stream, &ws); st != STRIPE_OK) return st;
   ProductParams p = {};
   p.a = x; p.b = w; p.c = y; p.pre = pre; p.offsets = offsets;
   p.partial = ws ? (float*)(ws + gated->dz_bytes) : nullptr;
   p.a_ld = d.x_row; p.b_ld = d.w_row; p.c_ld = d.y_row; p.pre_ld = d.pre_row; p.b_group = d.w_group;
-  p.half = d.out_features * d.w_row;
+  if (copies) {
+    if (const stripe_status_t st = gated_copy(gated, x, nullptr, ws, p, (hipStream_t)hip_stream); st != STRIPE_OK) return st;
+    if (const stripe_status_t st = gated_copy(gated, nullptr, w, ws, p, (hipStream_t)hip_stream); st != STRIPE_OK) return st;
+  }
+  p.half = d.out_features * p.b_ld;
   p.rows = p.M = (int32_t)d.rows; p.N = (int32_t)d.out_features; p.K = (int32_t)d.in_features;
   p.groups = d.groups; p.act = d.activation;
   p.vec = d.y_row % v == 0 && !misaligned(y, 16);
@@ -151,7 +203,8 @@ stripe_status_t gated_backward(stripe_gated_t* gated, const void* dy, const void
   unsigned char* ws = nullptr;
   if (d.rows)
     if (const stripe_status_t st = gated->ws.get(gated->ws_bytes(), stream, &ws); st != STRIPE_OK) return st;
-  const Access w_access = misaligned(w, 16) ? gated->otherwise : gated->best, x_access = misaligned(x, 16) ? gated->otherwise : gated->best;
+  const Access w_access = gated->copies[kInputGrad] ? kPieces : misaligned(w, 16) ? gated->otherwise : gated->best;
+  const Access x_access = gated->copies[kWeightGrad] ? kPieces : misaligned(x, 16) ? gated->otherwise : gated->best;
   if (d.rows) {
     GatedGradParams p = {};
     p.dy = dy; p.pre = pre; p.dz = ws;
@@ -166,13 +219,21 @@ stripe_status_t gated_backward(stripe_gated_t* gated, const void* dy, const void
   p.a = ws; p.a_ld = gated->dz_row;
   if (dx && d.rows) {
     p.b = w; p.b_ld = d.w_row; p.b_group = d.w_group;
+    if (gated->copies[kInputGrad])
+      if (const stripe_status_t st = gated_copy(gated, nullptr, w, ws, p, stream); st != STRIPE_OK) return st;
     p.c = dx; p.c_ld = d.x_row;
     p.M = (int32_t)d.rows; p.N = (int32_t)d.in_features; p.K = (int32_t)(2 * d.out_features);
     p.vec = d.x_row % v == 0 && !misaligned(dx, 16);
     if (const stripe_status_t st = launched(launch_product(kInputGrad, d.dtype, gated->plan[w_access][kInputGrad], w_access, p, stream)); st != STRIPE_OK) return st;
   }
   if (dw) {
-    p.b = x; p.b_ld = d.x_row; p.b_group = 0;
+    p.b = x; p.b_ld = d.x_row;
+    if (gated->copies[kWeightGrad] && d.rows) {
+      ProductParams copy = {};
+      if (const stripe_status_t st = gated_copy(gated, x, nullptr, ws, copy, stream); st != STRIPE_OK) return st;
+      p.b = copy.a; p.b_ld = copy.a_ld;
+    }
+    p.b_group = 0;
     p.c = dw; p.c_ld = d.w_row; p.c_group = d.w_group;
     p.M = (int32_t)(2 * d.out_features); p.N = (int32_t)d.in_features; p.K = (int32_t)d.rows;
     p.vec = d.w_row % v == 0 && (!d.groups || d.w_group % v == 0) && !misaligned(dw, 16);
@@ -230,6 +291,22 @@ stripe_status_t xent_create(const stripe_xent_desc_t* desc, stripe_xent_t** out)
     const int64_t bn = tile_columns(xent->logits[access]);
     xent->stats_bytes = std::max(xent->stats_bytes, round_up_256(std::max((d.classes + bn - 1) / bn, (int64_t)xent_slice_blocks(d.classes)) * d.rows * 8));
   }
+  const int64_t w_bytes = round_up_256(d.classes * xent->x_ld * e);
+  if (d.rows && d.dtype == STRIPE_BF16 && xent->best == kAny && w_bytes <= kMostCopied) {
+    const ProductPlan logits = plan_product(kForward, d.dtype, d.rows, d.in_features, d.classes, 0, kPieces, odd, kLogits);
+    const ProductPlan dx = plan_product(kInputGrad, d.dtype, d.rows, d.in_features, xent->piece, 0, kPieces, odd);
+    const double any = xent->logits[kAny].us, pieces = (double)xent->pieces;
+    xent->w_copy[0] = copy_pays(logits.us + copy_time(w_bytes), any);
+    xent->w_copy[1] = copy_pays(logits.us + dx.us * pieces + copy_time(w_bytes), any + xent->dx[kAny].us * pieces);
+    if (xent->w_copy[0] || xent->w_copy[1]) {
+      xent->w_bytes = w_bytes;
+      xent->logits[kPieces] = logits;
+      xent->dx[kPieces] = dx;
+      const int64_t bn = tile_columns(logits);
+      xent->stats_bytes = std::max(xent->stats_bytes, round_up_256(std::max((d.classes + bn - 1) / bn, (int64_t)xent_slice_blocks(d.classes)) * d.rows * 8));
+      xent->partial_bytes = std::max({xent->partial_bytes, dx.ws_bytes, logits.ws_bytes, logits.splits > 1 ? logits.splits * d.rows * xent->dz_ld * 4 : 0});
+    }
+  }
   xent->partial_bytes = round_up_256(xent->partial_bytes);
   xent->row_bytes = round_up_256(d.rows * 4);
   xent->count_bytes = round_up_256(d.rows / 1024 * 8 + 8);
@@ -275,6 +352,16 @@ ProductParams xent_logits(const stripe_xent_t* xent, const XentParts& parts, con
   return p;
 }
 
+// A copy of W in whole pieces in its place.
+stripe_status_t xent_copy(const stripe_xent_t* xent, const XentParts& parts, const void** w, int64_t* w_row, hipStream_t stream) {
+  PadParams c = {};
+  c.from = *w; c.to = parts.rest + std::max(xent->stats_bytes, xent->dz_bytes + xent->sum_bytes) + xent->partial_bytes;
+  c.rows = c.each = xent->d.classes; c.from_row = xent->d.w_row; c.to_row = xent->x_ld; c.cols = (int32_t)xent->d.in_features;
+  *w = c.to;
+  *w_row = c.to_row;
+  return launched(launch_pad(c, stream));
+}
+
 stripe_status_t xent_run(stripe_xent_t* xent, const void* x, const void* w, const int32_t* targets, float* loss, float* lse, void* hip_stream) {
   if (!xent) return api_fail(STRIPE_ERR_NULL, "xent is NULL");
   const stripe_xent_desc_t& d = xent->d;
@@ -290,8 +377,11 @@ stripe_status_t xent_run(stripe_xent_t* xent, const void* x, const void* w, cons
   if (const stripe_status_t st = xent->ws.get(xent->ws_bytes(), stream, &ws); st != STRIPE_OK) return st;
   XentParts parts = xent_parts(xent, ws);
   // Rows that fit one tile: leaving some out would save nothing, so x is read where it lies (a launch less: 16 rows, 4096 -> 32768 bf16 64.0 us, 58.9).
-  const bool in_place = d.rows <= kFewRows && d.x_row <= kNear;
-  Access access = misaligned(w, 16) ? xent->otherwise : xent->best;
+  const bool copied = xent->w_copy[0], in_place = !copied && d.rows <= kFewRows && d.x_row <= kNear;
+  Access access = copied ? kPieces : misaligned(w, 16) ? xent->otherwise : xent->best;
+  int64_t w_row = d.w_row;
+  if (copied)
+    if (const stripe_status_t st = xent_copy(xent, parts, &w, &w_row, stream); st != STRIPE_OK) return st;
   if (in_place) {
     if (misaligned(x, 16) || d.x_row % (16 / e)) access = xent->otherwise;
   } else {
@@ -300,6 +390,7 @@ stripe_status_t xent_run(stripe_xent_t* xent, const void* x, const void* w, cons
   }
   const ProductPlan& plan = xent->logits[access];
   ProductParams p = xent_logits(xent, parts, w);
+  p.b_ld = w_row;
   p.N = (int32_t)d.classes;
   if (in_place) p.a = x, p.a_ld = d.x_row, p.targets = targets, p.offsets = nullptr, p.groups = 0;
   p.stats = (float*)parts.rest; p.target_z = parts.target_z;
@@ -347,11 +438,15 @@ stripe_status_t xent_backward(stripe_xent_t* xent, const void* x, const void* w,
   void* const dz = parts.rest;
   float* const sum = (float*)(parts.rest + xent->dz_bytes);
   float* const partial = (float*)(parts.rest + std::max(xent->stats_bytes, xent->dz_bytes + xent->sum_bytes));
-  const Access access = misaligned(w, 16) ? xent->otherwise : xent->best;
+  const Access access = xent->w_copy[1] ? kPieces : misaligned(w, 16) ? xent->otherwise : xent->best;
+  int64_t w_row = d.w_row;
+  if (xent->w_copy[1])
+    if (const stripe_status_t st = xent_copy(xent, parts, &w, &w_row, stream); st != STRIPE_OK) return st;
   for (int64_t first = 0; first < d.classes; first += xent->piece) {
     const int64_t count = std::min(xent->piece, d.classes - first);
-    const void* const rows = (const char*)w + first * d.w_row * e;
+    const void* const rows = (const char*)w + first * w_row * e;
     ProductParams p = xent_logits(xent, parts, rows);
+    p.b_ld = w_row;
     p.c = dz; p.c_ld = xent->dz_ld;
     p.N = (int32_t)((count + 7) / 8 * 8); p.class0 = (int32_t)first; p.classes = (int32_t)count;
     p.row_lse = r.row_lse; p.row_all = r.row_all; p.row_loss = r.row_loss; p.scale = r.scale;
@@ -361,7 +456,7 @@ stripe_status_t xent_backward(stripe_xent_t* xent, const void* x, const void* w,
     p.a = dz; p.a_ld = xent->dz_ld; p.offsets = r.span; p.groups = 1; p.partial = partial; p.scale = r.scale;
     p.rows = (int32_t)d.rows; p.N = (int32_t)d.in_features;
     if (dx) {
-      p.b = rows; p.b_ld = d.w_row;
+      p.b = rows; p.b_ld = w_row;
       p.c = dx; p.c_ld = d.x_row;
       p.M = (int32_t)d.rows; p.K = (int32_t)count;
       p.sum = xent->pieces > 1 ? sum : nullptr; p.index = r.index; p.first = first == 0; p.last = first + count == d.classes;
@@ -550,8 +645,11 @@ stripe_status_t stripe_gated_query(const stripe_gated_t* gated, stripe_linear_in
     if (!gated || !info) return api_fail(STRIPE_ERR_NULL, "gated or info is NULL");
     std::memset(info, 0, sizeof *info);
     char* names[3] = {info->forward, info->input_grad, info->weight_grad};
-    for (int k = 0; k < 3; ++k)
-      std::snprintf(names[k], sizeof info->forward, "%s%s", k ? "" : "gated_", product_name((ProductKind)k, gated->d.dtype, gated->plan[gated->best][k], gated->best).c_str());
+    for (int k = 0; k < 3; ++k) {
+      const Access access = gated->copies[k] ? kPieces : gated->best;
+      std::snprintf(names[k], sizeof info->forward, "%s%s%s", k ? "" : "gated_", product_name((ProductKind)k, gated->d.dtype, gated->plan[access][k], access).c_str(),
+                    gated->copies[k] ? "_copied" : "");
+    }
     info->workspace_bytes = gated->ws_bytes();
     return STRIPE_OK;
   });

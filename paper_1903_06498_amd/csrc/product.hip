@@ -195,6 +195,7 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
         plan.splits = splits;
         plan.ws_bytes = bytes;
         best_workgroups = workgroups;
+        plan.us = us;
       }
     }
   }
@@ -203,6 +204,7 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
     // (a gated unit, 1 row, 4096 -> 2 x 8192 bf16: 36.8 us on tiles, 29.9)
     if (best_workgroups > 256 || use == kHalves) best = std::max(best, few.floor);
     plan.few = few.us <= 1.05 * best;
+    if (plan.few) plan.us = few.us;
   }
   if (const int forced = tune_int("product_few", -1); forced >= 0 && kind == kForward && use != kLogits) plan.few = forced != 0;
   if ((groups ? rows / 16 + std::min<int64_t>(groups, rows) : (rows + 15) / 16) * ((out + 15) / 16) >= 1 << 23) plan.few = false;      // 2^32 lanes

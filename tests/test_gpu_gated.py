@@ -329,3 +329,29 @@ def test_more_groups_than_a_wavefront_has_lanes(groups, dtype):
     t.forward()
     t.backward()
     t.check()
+
+
+@pytest.mark.parametrize("offsets", [None, [0, 30, 30, 200, 333]], ids=["dense", "groups"])
+@pytest.mark.parametrize("size", [(333, 777, 130), (333, 70, 67), (340, 1, 5)], ids=lambda s: "x".join(map(str, s)))
+def test_rows_copied_to_whole_pieces(monkeypatch, size, offsets):
+    """bf16 rows that are no multiple of 16 bytes, with strides of their own."""
+    monkeypatch.setenv("STRIPE_TUNE", "layers_copy=1,product_few=0")
+    t = Gated(*size, "bf16", offsets=offsets, pad=3, shift=1, seed=19)
+    assert all(v.endswith("_copied") for k, v in t.op.info.items() if k != "workspace_bytes")
+    t.forward()
+    t.backward()
+    t.check()
+
+
+def test_rows_that_are_no_whole_pieces_at_sizes_of_either_kind():
+    """Whichever way the estimates send them: these sizes through registers, larger ones by copies."""
+    t = Gated(1500, 1023, 1000, "bf16", seed=20)
+    t.forward()
+    t.backward()
+    t.check()
+    t = Gated(4100, 1324, 2000, "bf16", seed=21)
+    assert t.op.info["forward"].endswith("_copied")
+    t.forward()
+    t.backward()
+    t.check()
+    assert not B.StripeGated(64, 63, 64, "bf16").info["forward"].endswith("_copied")

@@ -458,3 +458,24 @@ def test_more_classes_than_a_piece_holds(rows):
     t.check_forward()
     t.backward()
     t.check_backward()
+
+
+@pytest.mark.parametrize("rows", [40, 333])
+@pytest.mark.parametrize("cin,classes", [(777, 1300), (70, 515), (1, 9)])
+def test_weights_copied_to_whole_pieces(monkeypatch, rows, cin, classes):
+    """bf16 rows that are no multiple of 16 bytes, with strides of their own."""
+    monkeypatch.setenv("STRIPE_TUNE", "layers_copy=1")
+    t = Xent(rows, cin, classes, "bf16", pad=3, shift=1, seed=25)
+    t.forward()
+    t.check_forward()
+    t.backward()
+    t.check_backward()
+
+
+def test_copied_weights_in_pieces_of_the_vocabulary(monkeypatch):
+    monkeypatch.setenv("STRIPE_TUNE", "layers_copy=1,xent_pieces=3")
+    t = Xent(300, 333, 2000, "bf16", seed=26, pieces=3)
+    t.forward()
+    t.check_forward()
+    t.backward()
+    t.check_backward()
