@@ -157,11 +157,15 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
   double best = __builtin_huge_val(), best_workgroups = 0;
   const int forced_tile = tune_int("product_tile", -1), forced_splits = tune_int("product_splits", 0);
   const bool f32 = dtype == STRIPE_F32;
+  // A gated unit's few rows read W from memory at the same rate on every tile, but for what its slices cost: 16 rows, 4096 -> 2 x 8192 bf16, tiles 0 to 3 33.4 (four
+  // slices), 30.9 (four), 37.9 (two) and 30.6 us; 8192 -> 2 x 8192 71.3, 68.9, 64.3, 60.5; 2048 -> 2 x 4096 16.8, 14.7, 12.5, 9.9.
+  const bool streams = use == kHalves && kind == kForward && !groups && !f32 && access == kPieces && rows <= 64 && n >= 128 * 64 && forced_tile < 0 && !forced_splits;
   for (int variant = 0; variant < kTileCount; ++variant) {
     // loads into LDS: bf16 any tile, fp32 the small ones; the kernel for any alignment has the small one's shape, for fp32 in parts (variant 1)
     const bool parts = f32 && variant == 1;
     const int tile = parts ? kSmallTile : variant;
     if (access == kAny ? (f32 ? !parts : tile != kSmallTile) : (f32 && variant == 0) || (forced_tile >= 0 && forced_tile != variant)) continue;
+    if (streams && tile != kLeastTile) continue;
     const TileShape s = kTiles[tile];
     const TileTime t = tile_time(tile, dtype, access, parts);
     const int64_t bm = 64 * s.fm, bn = 64 * s.fn;
@@ -169,7 +173,7 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
                              : groups            ? (double)m / (double)bm + 0.5 * std::min<double>(groups, (double)m)
                                                  : (double)((m + bm - 1) / bm);
     const double tiles = row_tiles * (double)((n + bn - 1) / bn);
-    for (int splits = 1; splits <= (use == kLogits && m * n > kFewLogits ? 1 : 16); ++splits) {
+    for (int splits = 1; splits <= (streams || (use == kLogits && m * n > kFewLogits) ? 1 : 16); ++splits) {
       if (splits > 1 && (k_tiles < 2 * splits || (forced_splits && splits != forced_splits))) continue;
       const int64_t bytes = splits > 1 ? splits * images * m * n * 4 : 0;
       if (bytes > (64 << 20)) continue;
@@ -201,10 +205,11 @@ ProductPlan plan_product(ProductKind kind, int dtype, int64_t rows, int64_t in, 
   }
   if (kind == kForward && use != kLogits && rows <= (groups ? 8 * (int64_t)groups : 64)) {
     const RowsTime few = rows_time(dtype, rows, in, out, groups, odd_rows);
-    // (a gated unit, 1 row, 4096 -> 2 x 8192 bf16: 36.8 us on tiles, 29.9)
     if (best_workgroups > 256 || use == kHalves) best = std::max(best, few.floor);
-    plan.few = few.us <= 1.05 * best;
-    if (plan.few) plan.us = few.us;
+    // A gated unit, 4096 -> 2 x 8192 bf16, 1, 4, 8 and 16 rows: here 29.9, 31.5, 34.1 and 39.7 us, as every workgroup reads x, on tiles 3 30.5 to 30.7.
+    const double x_us = use == kHalves ? std::max(1.0, (double)((out + 15) / 16) / 256) * (double)std::min<int64_t>(rows, 16) * (double)in * (f32 ? 4 : 2) / 52e3 : 0;
+    plan.few = few.us + x_us <= 1.05 * best;
+    if (plan.few) plan.us = few.us + x_us;
   }
   if (const int forced = tune_int("product_few", -1); forced >= 0 && kind == kForward && use != kLogits) plan.few = forced != 0;
   if ((groups ? rows / 16 + std::min<int64_t>(groups, rows) : (rows + 15) / 16) * ((out + 15) / 16) >= 1 << 23) plan.few = false;      // 2^32 lanes
