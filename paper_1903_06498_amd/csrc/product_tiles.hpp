@@ -648,10 +648,10 @@ __device__ __forceinline__ void store_gated(const ProductParams& p, const Tile& 
 }
 
 // Of each row of a tile of logits: the largest, and the sum of the exponentials of their distances from it (from 0 where it is infinite, so that the sum is
-// 0, infinite or NaN as the formula has it); the target's logit where it lies in this tile.  NaN is in the sum only.  What an element costs is an
-// exponential and three instructions more: z log2 e - (largest log2 e) is one of them, with the rounding of the bracket taken out of the sum; only tiles
-// at the last class look at each column, only fragments with a target look for it.
-constexpr float kLog2E = 1.44269504f, kLn2 = 0.693147181f;
+// 0, infinite or NaN as the formula has it); the target's logit where it lies in this tile.  NaN is in the sum only.  The distance is taken first and scaled
+// then: its error is half an ulp of the distance, whatever the logits' size, and a part whose largest logit is a mask's -1e30 has the sum 1 or more, as any
+// other.  Only tiles at the last class look at each column, only fragments with a target look for it.
+constexpr float kLog2E = 1.44269504f;
 
 template <int FM, int C, int WAVES>
 __device__ __forceinline__ void store_log_sums(const ProductParams& p, const Tile& t, unsigned char* lds, f32x4 (&acc)[2 * FM][C]) {
@@ -693,16 +693,14 @@ __device__ __forceinline__ void store_log_sums(const ProductParams& p, const Til
       for (int v = 0; v < 4; ++v) top = fmaxf(top, acc[i][j][v]);
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
-    const bool finite = __builtin_fabsf(top) < __builtin_inff();
-    const float from = finite ? top * kLog2E : 0.f, off = finite ? __builtin_fmaf(top, kLog2E, -from) : 0.f;
+    const float from = __builtin_fabsf(top) < __builtin_inff() ? top : 0.f;
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < C; ++j)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][v], kLog2E, -from));
+      for (int v = 0; v < 4; ++v) sum += __builtin_amdgcn_exp2f((acc[i][j][v] - from) * kLog2E);
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
-    sum = finite ? __builtin_fmaf(sum, off * -kLn2, sum) : sum;
     if (lane < 16) sums[row * WN + wn] = make_float2(top == top ? top : -__builtin_inff(), sum);
   }
   __syncthreads();
