@@ -716,6 +716,13 @@ __device__ __forceinline__ void store_log_sums(const ProductParams& p, const Til
   }
 }
 
+// exp(z - lse), a class's part of its row.  Distance first, as above: z log2 e - lse log2 e in fp32 is off by 8 % at logits of 1e6, by everything at 1e8.  No logit
+// is above its row's lse; z, added up here in another order than the one that lse came from, may be, by its rounding (NaN stays NaN).
+template <typename T>
+__device__ __forceinline__ float probability(float z, float lse) {
+  return exp_of<T>(__builtin_elementwise_minimum(z - lse, 0.f));
+}
+
 // The gradient of the logits, divided by the scale, in place of the logits; zeros behind the last class.
 template <typename T, int FM, int C, int WAVES>
 __device__ __forceinline__ void loss_gradient(const ProductParams& p, const Tile& t, f32x4 (&acc)[2 * FM][C]) {
@@ -732,10 +739,7 @@ __device__ __forceinline__ void loss_gradient(const ProductParams& p, const Tile
 #pragma unroll
     for (int j = 0; j < C; ++j)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        if constexpr (sizeof(T) == 2) acc[i][j][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][v], kLog2E, -lse * kLog2E)) * all;
-        else acc[i][j][v] = expf(acc[i][j][v] - lse) * all;
-      }
+      for (int v = 0; v < 4; ++v) acc[i][j][v] = probability<T>(acc[i][j][v], lse) * all;
     if (__any((unsigned)target < 16u * C)) {
 #pragma unroll
       for (int j = 0; j < C; ++j)
@@ -1135,7 +1139,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(const ProductParams p
     const float inverse = 1.f / *p.scale, lse = p.row_lse[row], all = p.row_all[row] * inverse, one = p.row_loss[row] * inverse;
     const int target = p.targets[row] - p.class0 - col;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = col + e < p.classes ? exp_of<T>(v[e] - lse) * all - (target == e ? one : 0.f) : 0.f;
+    for (int e = 0; e < 8; ++e) v[e] = col + e < p.classes ? probability<T>(v[e], lse) * all - (target == e ? one : 0.f) : 0.f;
   }
   Eight<T> r;
   if constexpr (KIND == kForward) {

@@ -4,7 +4,7 @@ Tolerances, u = 2^-24, r = the result type's half step.  The logits of `exact` c
 nothing below depends on their size but where lse itself is rounded:
   lse      (3 |z - lse| + 8) u weighted with p, (32 + classes / 256) 8 u of the sums, 3 u (1 + rest) of the logarithm, rest = lse - the largest logit; and its own rounding, u |lse|
   loss     the same without lse's rounding, but with that of the difference, u |loss|
-  dz       p (dloss + dlse): lse comes rounded, p = exp(z - lse) off by expm1(u |lse|), (3 |z - lse| + 8) u; 4 u of the terms; rounded to the operands' type
+  dz       p (dloss + dlse): lse comes rounded, p = exp(z - lse) off by expm1(u |lse|) unless lse is one of fp32's values, (3 |z - lse| + 8) u; 4 u of the terms; rounded to the operands' type
   dx, dW   the terms' errors, (terms + 2) u sum |terms|, one rounding
 The reference takes distances from the largest logit too: even in 64 bits 10^30 + log n is 10^30.
 Other cases add e = (n + 2) u sum |terms| of the logits that are not masked (a masked one has p = 0, whatever it is)."""
@@ -60,8 +60,9 @@ class Case:
         off, tolerance = (self.got["lse"].double() - lse).abs(), tol + U * lse.abs()
         assert (off <= tolerance).all(), f"lse: {float((off / tolerance).max()):.3g} of the tolerance"
 
-    def check_backward(self):
-        r, x, w, lse = HALF[self.dtype], self.x.double(), self.w.double(), self.lse[:, None]
+    def check_backward(self, lse_exact=False):
+        r, x, w = HALF[self.dtype], self.x.double(), self.w.double()
+        lse_off = 0.0 if lse_exact else U * self.lse.abs()[:, None]
         one = self.dloss.double()
         both = one + self.dlse.double() if self.dlse is not None else one
         p = self.d.exp()
@@ -70,7 +71,7 @@ class Case:
         size = p * both.abs()[:, None]
         size.scatter_add_(1, self.at, one.abs()[:, None])
         d = self.d.abs().clamp(max=1e4)
-        dzt = p * both.abs()[:, None] * (torch.expm1(self.e + U * lse.abs()) + 3 * U * d + 8 * U) + 4 * U * size
+        dzt = p * both.abs()[:, None] * (torch.expm1(self.e + lse_off) + 3 * U * d + 8 * U) + 4 * U * size
         dzt = dzt + r * (dz.abs() + dzt)
         for name, got, want, tol in (("dx", self.dx, dz @ w, (dzt + (len(w) + 3) * U * dz.abs()) @ w.abs()),
                                      ("dw", self.dw, dz.t() @ x, (dzt + (len(x) + 2) * U * dz.abs()).t() @ x.abs())):
@@ -100,6 +101,34 @@ def test_loss_of_sure_rows(monkeypatch, dtype, plan, power):
     top = t.x[:, 0].float()
     assert torch.equal(t.got["lse"], top)
     assert torch.equal(t.got["loss"], torch.where(t.targets == 700 // 3, torch.zeros_like(top), 2 * top))
+
+
+@pytest.mark.parametrize("power", [4, 5, 6, 7, 8, 9, 12, 20, 30])
+@pytest.mark.parametrize("dtype,plan", EVERY)
+def test_gradients_of_sure_rows(monkeypatch, dtype, plan, power):
+    """p is 1 for the largest logit and 0 for all others: dz is made of the weights alone."""
+    monkeypatch.setenv("STRIPE_TUNE", plan)
+    t = Case(*sure(70, 700, 520, dtype, power), dtype)
+    t.backward(t.x[:, 0].float().contiguous())
+    t.check_backward(lse_exact=True)
+
+
+@pytest.mark.parametrize("dtype,plan", EVERY)
+def test_gradients_never_pass_their_weights(monkeypatch, dtype, plan):
+    """Logits of some 1e9 whose last bits are worth 64, added up in one order for lse and in another for dz: still 0 <= p <= 1, so |dz| <= |dloss| + |dlse|."""
+    monkeypatch.setenv("STRIPE_TUNE", "product_splits=2" if "splits=2" not in plan else "product_tile=2,product_splits=1")
+    g = torch.Generator(device="cuda").manual_seed(5)
+    rows, classes, cin = 130, 600, 520
+    args = (torch.randn(rows, cin, generator=g, device="cuda") * 1e4, torch.randn(classes, cin, generator=g, device="cuda") * 1e4, torch.arange(rows, device="cuda") * 3, dtype)
+    first = Case(*args, exact=False)
+    first.forward()
+    monkeypatch.setenv("STRIPE_TUNE", plan)
+    t = Case(*args, exact=False)
+    t.backward(first.got["lse"])
+    weight = t.dloss.abs().double() + t.dlse.abs().double()
+    more = 1 + 2 * HALF[dtype] + (classes + 8) * U      # dz's rounding and the result's, the sums'
+    assert (t.dw.double().abs() <= weight @ t.x.double().abs() * more).all()
+    assert (t.dx.double().abs() <= (weight[:, None] * t.w.double().abs().sum(0)) * more).all()
 
 
 @pytest.mark.parametrize("dtype,plan", EVERY)
@@ -143,6 +172,15 @@ def with_masks(rows, dtype, mask):
     open_classes = torch.arange(classes, device="cuda")[~masked]
     targets = open_classes[torch.randint(0, len(open_classes), (rows,), generator=g, device="cuda")]
     return Case(x, w, targets, dtype, exact=False, masked=masked)
+
+
+@pytest.mark.parametrize("mask", MASKS)
+@pytest.mark.parametrize("dtype,plan", EVERY)
+def test_gradients_with_finite_masks(monkeypatch, dtype, plan, mask):
+    monkeypatch.setenv("STRIPE_TUNE", plan)
+    t = with_masks(150, dtype, mask)
+    t.backward(t.lse.float())
+    t.check_backward()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
