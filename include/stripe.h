@@ -438,8 +438,8 @@ void stripe_gated_destroy(stripe_gated_t* gated);
  *   z = x W^T,  lse = log(sum of exp(z) over the classes),  loss = lse - z[target];
  *   dz = exp(z - lse) (dloss + dlse) - [class = target] dloss,  dx = dz W,  dW = dz^T x.
  * x [rows][in_features], W [classes][in_features]; targets [rows]: int32 on the DEVICE; loss, lse, dloss, dlse [rows]: fp32.
- * A row whose target is not one of 0 .. classes - 1 does not count: x is not read there (it may hold anything), loss, lse and dx are 0, and dW
- * has nothing of it.  The backward pass computes z again, a piece of the vocabulary at a time (exp(z - lse) is at most 1, whatever the
+ * A row whose target is not one of 0 .. classes - 1 does not count: loss, lse and dx are 0, dW has nothing of it, and whatever x holds there
+ * (NaN, too) changes no bit of any result.  The backward pass computes z again, a piece of the vocabulary at a time (exp(z - lse) is at most 1, whatever the
  * two sums' roundings); a piece's dz is in the workspace, rounded to the operands' type.  In bf16 it is divided by the rows' largest |dloss| or |dloss + dlse| before and multiplied by it in dx and dW: of rows
  * whose weights are less than 2^-110 of that, digits may be lost.  dx is added up in fp32 over the pieces.
  */

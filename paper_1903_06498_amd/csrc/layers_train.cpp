@@ -376,15 +376,17 @@ stripe_status_t xent_run(stripe_xent_t* xent, const void* x, const void* w, cons
   unsigned char* ws = nullptr;
   if (const stripe_status_t st = xent->ws.get(xent->ws_bytes(), stream, &ws); st != STRIPE_OK) return st;
   XentParts parts = xent_parts(xent, ws);
-  // Rows that fit one tile: leaving some out would save nothing, so x is read where it lies (a launch less: 16 rows, 4096 -> 32768 bf16 64.0 us, 58.9).
-  const bool copied = xent->w_copy[0], in_place = !copied && d.rows <= kFewRows && d.x_row <= kNear;
+  // Rows that fit one tile: leaving some out would save nothing, so x is read where it lies (a launch less: 16 rows, 4096 -> 32768 bf16 64.0 us, 58.9).  Not by
+  // fp32 in parts, which computes a tile again if any of its rows does not end finite: the others' last bits would hang on rows that do not count.
+  const bool copied = xent->w_copy[0];
   Access access = copied ? kPieces : misaligned(w, 16) ? xent->otherwise : xent->best;
+  const Access there = misaligned(x, 16) || d.x_row % (16 / e) ? xent->otherwise : access;
+  const bool in_place = !copied && d.rows <= kFewRows && d.x_row <= kNear && !xent->logits[there].parts;
+  if (in_place) access = there;
   int64_t w_row = d.w_row;
   if (copied)
     if (const stripe_status_t st = xent_copy(xent, parts, &w, &w_row, stream); st != STRIPE_OK) return st;
-  if (in_place) {
-    if (misaligned(x, 16) || d.x_row % (16 / e)) access = xent->otherwise;
-  } else {
+  if (!in_place) {
     parts.rows.x = x; parts.rows.targets = targets; parts.rows.loss = loss; parts.rows.lse = lse; parts.rows.scale = nullptr;
     if (const stripe_status_t st = launched(launch_xent_rows(d.dtype, parts.rows, stream)); st != STRIPE_OK) return st;
   }

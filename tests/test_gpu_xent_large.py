@@ -193,3 +193,28 @@ def test_loss_of_rows_that_are_masked_altogether(dtype):
         t = Case(x, w, torch.arange(rows, device="cuda"), dtype)
         t.forward()
         t.check_forward()
+
+
+@pytest.mark.parametrize("rows", [7, 64, 65])
+@pytest.mark.parametrize("cin", [520, 333])
+@pytest.mark.parametrize("dtype,plan", EVERY)
+def test_rows_that_do_not_count_reach_no_other(monkeypatch, dtype, plan, cin, rows):
+    """The same bits for the rows that count, whatever the others hold: few rows are read where they lie."""
+    monkeypatch.setenv("STRIPE_TUNE", plan)
+    g = torch.Generator(device="cuda").manual_seed(cin + rows)
+    x, w = torch.randn(rows, cin, generator=g, device="cuda"), torch.randn(700, cin, generator=g, device="cuda")
+    targets = torch.arange(rows, device="cuda") * 5
+    t = Case(x, w, targets, dtype, exact=False)
+    ignored = torch.arange(rows, device="cuda") % 3 == 1
+    t.targets[ignored] = -1
+    results = []
+    for value in (0.0, float("nan"), float("inf"), 3e38):
+        t.x[ignored] = value
+        t.forward()
+        assert (t.got["loss"][ignored] == 0).all() and (t.got["lse"][ignored] == 0).all()
+        lse = t.lse.float()
+        lse[ignored] = t.dloss[ignored] = t.dlse[ignored] = value
+        t.backward(lse)
+        assert (t.dx[ignored] == 0).all()
+        results.append(torch.cat([t.got["loss"][~ignored], t.got["lse"][~ignored], t.dx.float().flatten(), t.dw.float().flatten()]))
+    assert torch.isfinite(results[0]).all() and all(torch.equal(results[0], r) for r in results)
