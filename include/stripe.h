@@ -465,6 +465,8 @@ stripe_status_t stripe_xent_backward(stripe_xent_t* xent, const void* x, const v
 
 stripe_status_t stripe_xent_workspace_size(const stripe_xent_t* xent, size_t* bytes);
 stripe_status_t stripe_xent_set_workspace(stripe_xent_t* xent, void* device_ptr, size_t bytes);
+/* forward: the logits' kernel, which both passes run; input_grad, weight_grad: those of a piece of the vocabulary. */
+stripe_status_t stripe_xent_query(const stripe_xent_t* xent, stripe_linear_info_t* info);
 void stripe_xent_destroy(stripe_xent_t* xent);
 
 /*

@@ -38,7 +38,7 @@ EXPORTS = ("stripe_block_create", "stripe_block_create_for_path", "stripe_block_
            "stripe_norm_workspace_size", "stripe_norm_set_workspace", "stripe_norm_destroy",
            "stripe_gated_create", "stripe_gated_run", "stripe_gated_backward", "stripe_gated_workspace_size", "stripe_gated_set_workspace",
            "stripe_gated_query", "stripe_gated_destroy", "stripe_xent_create", "stripe_xent_run", "stripe_xent_backward",
-           "stripe_xent_workspace_size", "stripe_xent_set_workspace", "stripe_xent_destroy",
+           "stripe_xent_workspace_size", "stripe_xent_set_workspace", "stripe_xent_query", "stripe_xent_destroy",
            "stripe_adamw_create", "stripe_adamw_bind", "stripe_adamw_run", "stripe_adamw_read", "stripe_adamw_destroy")
 
 
@@ -180,7 +180,7 @@ def _load():
                            ("workspace_size", [handle, C.POINTER(C.c_size_t)]), ("set_workspace", [handle, ptr, C.c_size_t]), ("destroy", [handle])):
             f = getattr(lib, f"stripe_{name}_{call}")
             f.restype, f.argtypes = None if call == "destroy" else C.c_int, args
-    for name in ("linear", "gated"):
+    for name in ("linear", "gated", "xent"):
         f = getattr(lib, f"stripe_{name}_query")
         f.restype, f.argtypes = C.c_int, [handle, C.POINTER(stripe_linear_info_t)]
     for call, args in (("create", [C.POINTER(stripe_adamw_desc_t), C.POINTER(handle)]), ("bind", [handle, C.POINTER(stripe_adamw_tensor_t)]),
@@ -510,6 +510,10 @@ def stripe_xent_create(rows: int, in_features: int, classes: int, dtype: str, x_
     return h
 
 
+def stripe_xent_query(handle) -> dict:
+    return _layer_info(lib.stripe_xent_query, handle)
+
+
 _STATES = {"f32": "f32", "8bit": "i8"}
 
 
@@ -721,6 +725,7 @@ class StripeXent(_Layer):
     def __init__(self, rows: int, in_features: int, classes: int, dtype: str = "bf16", x_row: int = 0, w_row: int = 0):
         self.handle = None
         self._open(stripe_xent_create(rows, in_features, classes, dtype, x_row, w_row), dtype)
+        self.info = stripe_xent_query(self.handle)
         self._x, self._w = ((rows, in_features), (x_row or in_features, 1)), ((classes, in_features), (w_row or in_features, 1))
         self._r = ((rows,), (1,))
 

@@ -684,6 +684,23 @@ stripe_status_t stripe_xent_set_workspace(stripe_xent_t* xent, void* device_ptr,
   return guarded([&] { return xent ? xent->ws.set(device_ptr, bytes, xent->d.rows ? xent->ws_bytes() : 0) : api_fail(STRIPE_ERR_NULL, "xent is NULL"); });
 }
 
+stripe_status_t stripe_xent_query(const stripe_xent_t* xent, stripe_linear_info_t* info) {
+  return guarded([&]() -> stripe_status_t {
+    if (!xent || !info) return api_fail(STRIPE_ERR_NULL, "xent or info is NULL");
+    std::memset(info, 0, sizeof *info);
+    const int dtype = xent->d.dtype;
+    auto name = [&](char* to, ProductKind kind, const ProductPlan* plans, bool copied) {
+      const Access access = copied ? kPieces : xent->best;
+      std::snprintf(to, sizeof info->forward, "%s%s", product_name(kind, dtype, plans[access], access).c_str(), copied ? "_copied" : "");
+    };
+    name(info->forward, kForward, xent->logits, xent->w_copy[0]);
+    name(info->input_grad, kInputGrad, xent->dx, xent->w_copy[1]);
+    std::snprintf(info->weight_grad, sizeof info->weight_grad, "%s", product_name(kWeightGrad, dtype, xent->dw, xent->copies).c_str());
+    info->workspace_bytes = xent->d.rows ? xent->ws_bytes() : 0;
+    return STRIPE_OK;
+  });
+}
+
 void stripe_xent_destroy(stripe_xent_t* xent) { delete xent; }
 
 stripe_status_t stripe_adamw_create(const stripe_adamw_desc_t* desc, stripe_adamw_t** out) {

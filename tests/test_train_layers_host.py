@@ -156,3 +156,41 @@ def test_gated_plans_and_workspaces_at_the_edges():
     for args in ((0, 1, 1), (1, 1, 1), (1 << 24, 8, 100), (1, 1 << 20, 3), (1, 8, 1 << 24), (70000, 64, 1 << 12)):
         for dtype in ("bf16", "f32"):
             B.lib.stripe_xent_destroy(B.stripe_xent_create(*args, dtype))
+
+
+def test_xent_query():
+    info = B.stripe_linear_info_t()
+    h = B.stripe_xent_create(16, 32, 48, "bf16")
+    assert B.lib.stripe_xent_query(None, C.byref(info)) == B.lib.stripe_xent_query(h, None) == ERR["ERR_NULL"]
+    n = C.c_size_t()
+    assert B.lib.stripe_xent_workspace_size(h, C.byref(n)) == 0 and B.stripe_xent_query(h)["workspace_bytes"] == n.value
+    B.lib.stripe_xent_destroy(h)
+    h = B.stripe_xent_create(0, 32, 48, "f32")
+    assert B.stripe_xent_query(h)["workspace_bytes"] == 0
+    B.lib.stripe_xent_destroy(h)
+
+
+@pytest.mark.parametrize("splits", [1, 3])
+@pytest.mark.parametrize("tile", range(4))
+def test_xent_runs_on_the_tile_that_is_asked_for(monkeypatch, tile, splits):
+    """The shapes that the GPU tests force tiles for; the logits' reduction of 9 K tiles in 3 slices, dW's of 5 in one."""
+    monkeypatch.setenv("STRIPE_TUNE", f"product_tile={tile},product_splits={splits},xent_pieces=2")
+    h = B.stripe_xent_create(300, 520, 1100, "bf16")
+    info = B.stripe_xent_query(h)
+    shape = ("256x256_s2", "128x256_s3", "64x128_s3", "64x64_s4")[tile]
+    slices = "" if splits == 1 else "_k3"
+    assert info["forward"] == f"product_stream_nt_bf16_{shape}{slices}" and info["input_grad"] == f"product_stream_nn_bf16_{shape}{slices}"
+    assert info["weight_grad"] == f"product_stream_tn_bf16_{shape}"
+    B.lib.stripe_xent_destroy(h)
+
+
+def test_xent_names_parts_and_copies(monkeypatch):
+    monkeypatch.setenv("STRIPE_TUNE", "product_tile=1")
+    h = B.stripe_xent_create(200, 256, 700, "f32")
+    assert all("_parts" in B.stripe_xent_query(h)[name] for name in ("forward", "input_grad", "weight_grad"))
+    B.lib.stripe_xent_destroy(h)
+    monkeypatch.setenv("STRIPE_TUNE", "layers_copy=1")
+    h = B.stripe_xent_create(333, 777, 1300, "bf16")
+    info = B.stripe_xent_query(h)
+    assert info["forward"].endswith("_copied") and info["input_grad"].endswith("_copied")
+    B.lib.stripe_xent_destroy(h)
