@@ -78,6 +78,7 @@ struct ProductParams {
   float* sum;               // [M][N], nullptr: one product is all
   const int32_t* index;     // [rows]
   int32_t first, last;
+  int32_t tile_rows, most_slices;   // of an output tile; of a reduction that is split
 };
 
 struct ProductPlan {

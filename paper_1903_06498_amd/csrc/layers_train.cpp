@@ -53,7 +53,7 @@ constexpr int64_t kNear = (int64_t)1 << 20;      // row strides up to which a ti
 // pieces of 128 MB 6.47 ms, 2 of them 6.61, 4 6.49, 16 6.82).
 constexpr int64_t kPieceBytes = (int64_t)128 << 20, kMaxPiece = (int64_t)1 << 19;
 constexpr int64_t kMaxElements = (int64_t)1 << 34;
-constexpr int64_t kFewRows = 64, kHalfRows = 512, kMostSlices = (int64_t)128 << 20;
+constexpr int64_t kFewRows = 64;
 
 // Rows of bf16 that are no whole pieces go through registers, on the smallest tiles.  Where the estimates say so they are copied first: a launch, and the bytes
 // read and written (a gated unit of 8192 rows, 4095 -> 4096: 986 us forward and 2095 backward through registers, 430 and 845; the cross entropy of 4096 rows,
@@ -278,13 +278,6 @@ stripe_status_t xent_create(const stripe_xent_desc_t* desc, stripe_xent_t** out)
   for (const Access access : {xent->best, xent->otherwise}) {
     xent->logits[access] = plan_product(kForward, d.dtype, d.rows, d.in_features, d.classes, 0, access, odd, kLogits);
     xent->dx[access] = plan_product(kInputGrad, d.dtype, d.rows, d.in_features, xent->piece, 0, access, odd);
-    if (xent->dx[access].splits > 1 && d.rows <= kHalfRows) {
-      // So few rows that the reduction is split: for half of them, as many may count (205 of 512 rows, 50001 -> 4096 bf16: 193 us in slices for all, 122; 900 of
-      // 1000 fp32, 10007 -> 333, would lose: 67 us, 83).
-      ProductPlan half = plan_product(kInputGrad, d.dtype, (d.rows + 1) / 2, d.in_features, xent->piece, 0, access, odd);
-      half.ws_bytes = half.splits > 1 ? half.splits * d.rows * d.in_features * 4 : 0;
-      if (half.ws_bytes <= kMostSlices) xent->dx[access] = half;
-    }
     // (a piece's logits in slices: its classes end in zeros up to a multiple of 8)
     const int64_t slices = xent->logits[access].splits > 1 ? xent->logits[access].splits * d.rows * xent->dz_ld * 4 : 0;
     xent->partial_bytes = std::max({xent->partial_bytes, xent->dx[access].ws_bytes, xent->logits[access].ws_bytes, slices});
@@ -296,8 +289,10 @@ stripe_status_t xent_create(const stripe_xent_desc_t* desc, stripe_xent_t** out)
     const ProductPlan logits = plan_product(kForward, d.dtype, d.rows, d.in_features, d.classes, 0, kPieces, odd, kLogits);
     const ProductPlan dx = plan_product(kInputGrad, d.dtype, d.rows, d.in_features, xent->piece, 0, kPieces, odd);
     const double any = xent->logits[kAny].us, pieces = (double)xent->pieces;
-    xent->w_copy[0] = copy_pays(logits.us + copy_time(w_bytes), any);
-    xent->w_copy[1] = copy_pays(logits.us + dx.us * pieces + copy_time(w_bytes), any + xent->dx[kAny].us * pieces);
+    // An eighth less at least: a copy costs the same however few rows count, and the estimates of large copies beside few rows favour it (157 rows, 3790 -> 30841 with
+    // dx: 227 us by the estimate and 246 through registers, measured 248 and 199; 205 rows, 1023 -> 50001: 122 and 158, 116 and 144).
+    xent->w_copy[0] = copy_pays(logits.us + copy_time(w_bytes), 0.875 * any);
+    xent->w_copy[1] = copy_pays(logits.us + dx.us * pieces + copy_time(w_bytes), 0.875 * (any + xent->dx[kAny].us * pieces));
     if (xent->w_copy[0] || xent->w_copy[1]) {
       xent->w_bytes = w_bytes;
       xent->logits[kPieces] = logits;

@@ -330,7 +330,21 @@ using StreamOf = std::conditional_t<KIND == kGated, StreamHalves<T, WIDTH, COLS 
 struct Tile {
   int group, m0, m, n0;         // first output row (kForward, kInputGrad: of all rows), rows, first column
   int k0, k;                    // kWeightGrad: first row of the reduction, and its length
+  int slice, slices;            // of a split reduction
+  int64_t images;               // rows of a slice's partial image
 };
+
+// The slices of kSumGrad's reduction where `count` of its rows count, a number that the host does not know: p.splits are planned for all rows, and the
+// workgroups and partial images that all would take make more slices for those that count.  The pass with the logits, all rows and half of them: 512 rows, 50001 -> 4096
+// bf16 426 and 249 us (always four slices: 442, 322; always eight: 441, 247); 1500 rows 1085 and 650 (always two: 1169, 827; four: 1177, 672); 512 rows, 32768 -> 2048
+// 134 and 109 (always eight: 135, 112; sixteen: 148, 120); 1000 rows, 10007 -> 333 fp32 140 and 90 (always ten: 140, 107).
+__device__ __forceinline__ int sum_slices(const ProductParams& p, int count) {
+  if (p.splits == 1 || count <= 0) return p.splits;
+  const unsigned tiles = (unsigned)((count + p.tile_rows - 1) / p.tile_rows * p.tiles_n), all = (unsigned)(p.tiles_m * p.tiles_n);
+  const unsigned workgroups = (all + 7u) / 8u * 8u * (unsigned)p.splits / ((tiles + 7u) / 8u * 8u), images = (unsigned)p.splits * (unsigned)p.M / (unsigned)count;
+  const unsigned most = workgroups < images ? workgroups : images;
+  return (int)(most < (unsigned)p.most_slices ? most : (unsigned)p.most_slices);
+}
 
 // Whether every XCD takes its share of every group's tiles: shares of 4 of a matrix's tiles at least, and no more workgroups than a launch holds.
 __host__ __device__ constexpr bool spread(uint64_t tiles, uint64_t groups) { return tiles >= 32 && tiles * groups < 1 << 22; }
@@ -360,6 +374,19 @@ __device__ __forceinline__ bool place(const ProductParams& p, Tile* t) {
   }
   total = row_tiles * (unsigned)p.tiles_n;
   t->group = 0;
+  t->slice = (int)blockIdx.y;
+  t->slices = p.splits;
+  t->images = over_rows(KIND) && p.groups ? (int64_t)p.groups * p.M : p.M;
+  unsigned number = blockIdx.x;
+  if (KIND == kSumGrad) {      // its slices' workgroups follow one another
+    const unsigned each = (total + 7u) / 8u * 8u;
+    if (!total) return false;
+    t->slices = sum_slices(p, end);
+    t->images = end;
+    t->slice = (int)(number / each);
+    if (t->slice >= t->slices) return false;
+    number %= each;
+  }
   if (over_rows(KIND) && p.groups && spread(total, (unsigned)p.groups)) {
     // An eighth of every group's tiles to each XCD: the groups' reductions are of very different lengths (8192 rows in 16 uneven groups, 1024 x 4096 features: 137 us
     // where an XCD had whole groups, 100 here).
@@ -369,7 +396,7 @@ __device__ __forceinline__ bool place(const ProductParams& p, Tile* t) {
     l = first + i % own;
   } else {
     if (over_rows(KIND) && p.groups) total *= (unsigned)p.groups;
-    if (!logical_number(blockIdx.x, total, &l)) return false;
+    if (!logical_number(number, total, &l)) return false;
     if (over_rows(KIND) && p.groups) {
       const unsigned each = row_tiles * (unsigned)p.tiles_n;
       t->group = (int)(l / each);
@@ -516,7 +543,6 @@ __device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t
   unsigned char* buf = lds + wave * (ROWS * COLS * 4);
   const int fr = lane & 15, fq = lane >> 4, sp = lane / LANES, sc = lane % LANES;
   const int64_t image = over_rows(KIND) ? (int64_t)t.group * p.M : 0;
-  const int64_t images = over_rows(KIND) && p.groups ? (int64_t)p.groups * p.M : p.M;
   const int64_t base = (over_rows(KIND) ? t.group * p.c_group : 0) + (int64_t)t.m0 * p.c_ld;
   auto key = [](int row) { return COLS == 64 ? row & 15 : (row >> 1) & 7; };
   const float scale = scaled(KIND) ? *p.scale : 1.f;
@@ -566,7 +592,7 @@ __device__ __forceinline__ void store_tile(const ProductParams& p, const Tile& t
             if (p.splits > 1) {
               Eight<float> out;
               out.set(v);
-              out.store(p.partial + ((int64_t)blockIdx.y * images + image + t.m0 + row) * p.N + col, n, false);
+              out.store(p.partial + (t.slice * t.images + image + t.m0 + row) * p.N + col, n, false);
             } else {
               finish<T, KIND>(p, scale, t.m0 + row, col, base + (int64_t)row * p.c_ld + col, n, v, bias, now[q]);
             }
@@ -632,7 +658,7 @@ __device__ __forceinline__ void store_gated(const ProductParams& p, const Tile& 
       if (row < t.m && n > 0) {
         if (p.splits > 1) {
           Eight<float> out;
-          float* const to = p.partial + ((int64_t)blockIdx.y * p.M + t.m0 + row) * (2 * (int64_t)p.N) + col;
+          float* const to = p.partial + (t.slice * t.images + t.m0 + row) * (2 * (int64_t)p.N) + col;
           out.set(g);
           out.store(to, n, false);
           out.set(u);
@@ -786,12 +812,12 @@ __device__ __forceinline__ void init_operands(const ProductParams& p, const Tile
   }
 }
 // This workgroup's K tiles of `all`.
-__device__ __forceinline__ void own_k_tiles(const ProductParams& p, int all, int* kt0, int* kt1) {
+__device__ __forceinline__ void own_k_tiles(const Tile& t, int all, int* kt0, int* kt1) {
   *kt0 = 0;
   *kt1 = all;
-  if (p.splits > 1) {
-    const int per = (all + p.splits - 1) / p.splits;
-    *kt0 = (int)blockIdx.y * per < all ? (int)blockIdx.y * per : all;
+  if (t.slices > 1) {
+    const int per = (all + t.slices - 1) / t.slices;
+    *kt0 = t.slice * per < all ? t.slice * per : all;
     *kt1 = *kt0 + per < all ? *kt0 + per : all;
   }
 }
@@ -816,7 +842,7 @@ __global__ __launch_bounds__(256, 2) void product_kernel(const ProductParams p) 
   B b;
   init_operands<T, KIND>(p, t, a, b);
   int kt0, kt1;
-  own_k_tiles(p, (t.k + A::DEPTH - 1) / A::DEPTH, &kt0, &kt1);
+  own_k_tiles(t, (t.k + A::DEPTH - 1) / A::DEPTH, &kt0, &kt1);
 
   f32x4 acc[R][C];
 #pragma unroll
@@ -982,7 +1008,7 @@ __global__ __launch_bounds__(64 * WAVES, S * 64 * (FM + FN) * kDepthBytes > 80 *
   B b;
   init_operands<T, KIND>(p, t, a, b);
   int kt0, kt1;
-  own_k_tiles(p, (t.k + A::DEPTH - 1) / A::DEPTH, &kt0, &kt1);
+  own_k_tiles(t, (t.k + A::DEPTH - 1) / A::DEPTH, &kt0, &kt1);
 
   f32x4 acc[R][C];
 #pragma unroll
@@ -1099,8 +1125,8 @@ __global__ __launch_bounds__(64 * WAVES, S * 64 * (FM + FN) * kDepthBytes > 80 *
 template <typename T, int KIND>
 __global__ __launch_bounds__(256) void product_join_kernel(const ProductParams p, int strips) {
   const int row = (int)(blockIdx.x / (unsigned)strips), col = ((int)(blockIdx.x % (unsigned)strips) * 256 + (int)threadIdx.x) * 8, n = p.N - col;
-  const int64_t images = over_rows(KIND) && p.groups ? (int64_t)p.groups * p.M : p.M;
-  int group = 0;
+  int64_t images = over_rows(KIND) && p.groups ? (int64_t)p.groups * p.M : p.M;
+  int group = 0, slices = p.splits;
   int64_t at = (int64_t)row * p.c_ld + col;
   if (over_rows(KIND)) {
     group = row / p.M;
@@ -1108,6 +1134,10 @@ __global__ __launch_bounds__(256) void product_join_kernel(const ProductParams p
   } else if (p.groups) {
     group = group_of_row(p.offsets, p.groups, p.rows, row);
     if (group < 0) return;
+    if (KIND == kSumGrad) {
+      images = limited(p.offsets[1], p.rows);
+      slices = sum_slices(p, (int)images);
+    }
   }
   if (n <= 0) return;
   float v[8], bias[8];
@@ -1115,7 +1145,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(const ProductParams p
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = 0.f;
 #pragma unroll 4
-    for (int s = 0; s < p.splits; ++s) {
+    for (int s = 0; s < slices; ++s) {
       Eight<float> part;
       part.load(from + (int64_t)s * image, n, false);
       float f[8];
@@ -1202,7 +1232,13 @@ hipError_t launch_kind(const ProductPlan& plan, Access access, ProductParams& p,
     if (over_rows(KIND)) total = (spread((uint64_t)total, (uint64_t)p.groups) ? (total + 7) / 8 * 8 : total) * p.groups;
     else total = ((int64_t)p.M / bm + std::min<int64_t>(p.groups, p.M)) * p.tiles_n;
   }
-  const dim3 grid((unsigned)((total + 7) / 8 * 8), (unsigned)plan.splits);
+  dim3 grid((unsigned)((total + 7) / 8 * 8), (unsigned)plan.splits);
+  if (KIND == kSumGrad) {
+    const int depth = kDepthBytes / (int)sizeof(T);
+    p.tile_rows = bm;
+    p.most_slices = std::max(plan.splits, (p.K + depth - 1) / depth / 2);
+    grid = dim3((unsigned)(((int64_t)p.tiles_m * p.tiles_n + 7) / 8 * 8 * plan.splits));
+  }
   hipError_t e = hipSuccess;
   if (access == kWords && !plan.parts) {
     if constexpr (sizeof(T) == 4) e = plan.tile == kLeastTile ? launch_stream<T, KIND, kLeastTile, 4>(p, grid, stream) : launch_stream<T, KIND, kSmallTile, 4>(p, grid, stream);

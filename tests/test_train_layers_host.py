@@ -194,3 +194,22 @@ def test_xent_names_parts_and_copies(monkeypatch):
     info = B.stripe_xent_query(h)
     assert info["forward"].endswith("_copied") and info["input_grad"].endswith("_copied")
     B.lib.stripe_xent_destroy(h)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_xent_plans_its_input_gradient_for_all_rows(dtype):
+    """As a linear layer does whose gradients come in whole pieces, as dz does: of any number of rows, whether W is read where it lies or copied."""
+    for rows in (65, 130, 256, 300, 500, 511, 512, 513, 700, 1000):
+        for cin, classes in ((4096, 50001), (1024, 10007), (333, 10007), (2048, 32768), (1023, 30841)):
+            if rows * classes * (2 if dtype == "bf16" else 4) > 128 << 20:
+                continue          # more than one piece
+            whole = (classes + 7) // 8 * 8
+            h, lin = B.stripe_xent_create(rows, cin, classes, dtype), B.stripe_linear_create(rows, cin, whole, dtype)
+            got, want = B.stripe_xent_query(h)["input_grad"], B.stripe_linear_query(lin)["input_grad"]
+            B.lib.stripe_xent_destroy(h)
+            B.lib.stripe_linear_destroy(lin)
+            if got.endswith("_copied"):
+                lin = B.stripe_linear_create(rows, (cin + 7) // 8 * 8, whole, dtype)
+                want = B.stripe_linear_query(lin)["input_grad"] + "_copied"
+                B.lib.stripe_linear_destroy(lin)
+            assert got == want, (rows, cin, classes)
