@@ -74,8 +74,9 @@ __device__ __forceinline__ void store4(T* q, int n, const T (&from)[4]) {
   }
 }
 
-// Codes of a block's values (not negative), and the factor of their squares.  The root's last bit does not matter: where it decides about a floor, the value
-// is next to a code, which is the one that is chosen from either side.
+// Codes of a block's values (not negative), and the factor of their squares.  The instruction's root gives the codes of an exact one: a floor that is one too
+// large, which it has for values just below a square, is taken back by `past` and `place`, and one that is too small does not occur (looked at on gfx950 for every
+// fp32 value up to 2^16, and all random bits where the floors differ).
 template <int MOST, bool KEEPS>
 __device__ __forceinline__ float encode(const float (&value)[4], const uint32_t (&bits)[4], float (&code)[4]) {
 #pragma clang fp contract(off)
