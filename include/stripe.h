@@ -487,7 +487,7 @@ typedef struct {
   stripe_dtype_t grad_dtype;        /* STRIPE_BF16 or STRIPE_F32 */
   stripe_dtype_t state_dtype;       /* STRIPE_F32 or STRIPE_I8 */
   double beta1, beta2;              /* 0 <= b < 1 */
-  double eps;                       /* >= 0 and finite */
+  double eps;                       /* 0, or at least 2^-126 and finite */
 } stripe_adamw_desc_t;
 
 typedef struct {

@@ -481,7 +481,8 @@ stripe_status_t adamw_create(const stripe_adamw_desc_t* desc, stripe_adamw_t** o
   if (d.grad_dtype != STRIPE_BF16 && d.grad_dtype != STRIPE_F32) return api_fail(STRIPE_ERR_UNSUPPORTED, "gradients are bf16 or f32");
   if (d.state_dtype != STRIPE_F32 && d.state_dtype != STRIPE_I8) return api_fail(STRIPE_ERR_UNSUPPORTED, "states are f32 or i8");
   if (!(d.beta1 >= 0 && d.beta1 < 1 && d.beta2 >= 0 && d.beta2 < 1)) return api_fail(STRIPE_ERR_INVALID_DESC, "beta1 and beta2 are at least 0 and less than 1");
-  if (!(d.eps >= 0) || !std::isfinite((float)d.eps)) return api_fail(STRIPE_ERR_INVALID_DESC, "eps is a finite number, at least 0");
+  // (below, the reciprocal of what divides a state of 0 is infinite)
+  if (!(d.eps == 0 || d.eps >= 0x1p-126) || !std::isfinite((float)d.eps)) return api_fail(STRIPE_ERR_INVALID_DESC, "eps is a finite number, 0 or at least 2^-126");
   auto adamw = std::make_unique<stripe_adamw>();
   adamw->grad = d.grad_dtype;
   adamw->eight = d.state_dtype == STRIPE_I8;

@@ -45,3 +45,15 @@ def test_values_beside_codes(most, top):
     for name, got, want in (("m", m, cm), ("v", v, cv), ("m_scale", ms, sm), ("v_scale", vs, sv)):
         off = np.flatnonzero(got.cpu().numpy() != want)
         assert not len(off), (name, len(off), [(int(got[i]), int(want[i]), float(g[i]), hex(bits[i])) for i in off[:5]])
+
+
+@pytest.mark.parametrize("states", ["f32", "8bit"])
+def test_the_smallest_eps(states):
+    """A gradient of 0 is a step of 0."""
+    f32 = states == "f32"
+    p, g, ms, vs = torch.ones(300, device="cuda"), torch.zeros(300, device="cuda"), torch.zeros(2, device="cuda"), torch.zeros(2, device="cuda")
+    m, v = (torch.zeros(300, dtype=t, device="cuda") for t in ((torch.float32, torch.float32) if f32 else (torch.int8, torch.uint8)))
+    op = B.StripeAdamW([300], states=states, eps=2.0 ** -126)
+    op.bind([p], [g], [m], [v], *([] if f32 else [[ms], [vs]]))
+    op.run(1e-3, 1)
+    assert (p == 1).all()

@@ -213,3 +213,11 @@ def test_xent_plans_its_input_gradient_for_all_rows(dtype):
                 want = B.stripe_linear_query(lin)["input_grad"] + "_copied"
                 B.lib.stripe_linear_destroy(lin)
             assert got == want, (rows, cin, classes)
+
+
+@pytest.mark.parametrize("eps", [2.0 ** -127, 1e-40, 1e-300])
+def test_adamw_refuses_an_eps_whose_reciprocal_is_infinite(eps):
+    """A gradient of 0 would be a step of 0 times infinity."""
+    assert _status(lambda: B.stripe_adamw_create([10], [0.0], eps=eps)) == ERR["ERR_INVALID_DESC"]
+    for fine in (0.0, 2.0 ** -126, 1e-8):
+        B.lib.stripe_adamw_destroy(B.stripe_adamw_create([10], [0.0], eps=fine))
