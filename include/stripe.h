@@ -476,7 +476,7 @@ void stripe_xent_destroy(stripe_xent_t* xent);
  * state_dtype STRIPE_F32: m, v fp32.  STRIPE_I8: blocks of 256 consecutive elements; m is m_scale[block] c |c| with c = m[i] in -127 .. 127 (int8), the square
  * root of v is v_scale[block] c^2 with c = v[i] in 0 .. 255 (uint8); m_scale, v_scale: fp32, ceil(elements / 256).  All zeros is the state before the first
  * step.  A value between two codes becomes one of them at random, such that its mean is kept (a square root of v that is not 0 does not become 0); the random
- * bits are a hash of (seed, the tensor's number, the element's), so that the same call gives the same bits: give every step another seed.  A block whose
+ * bits are a hash of (seed, the tensor's number, the element's modulo 2^32), so that the same call gives the same bits: give every step another seed.  A block whose
  * largest value is at most 1e-30 becomes 0, one that holds a value that is not finite becomes NaN as a whole.  p's update uses m and v
  * before they are coded.
  */
@@ -513,7 +513,7 @@ typedef struct stripe_adamw stripe_adamw_t;
 stripe_status_t stripe_adamw_create(const stripe_adamw_desc_t* desc, stripe_adamw_t** out);
 
 /* The tensors that the steps update, desc.tensors of them (the pointers of one without elements are not looked at): kept until the next call of bind(),
- * which no step may overlap on the host.  No buffer may be bound twice (the same address is refused), but two gradients may be one. */
+ * which no step may overlap on the host.  A call checks every tensor: keep the buffers of gradients and bind once; a program whose gradients move binds before each step.  No buffer may be bound twice (the same address is refused), but two gradients may be one. */
 stripe_status_t stripe_adamw_bind(stripe_adamw_t* adamw, const stripe_adamw_tensor_t* tensors);
 stripe_status_t stripe_adamw_run(stripe_adamw_t* adamw, const stripe_adamw_step_t* step, void* hip_stream);
 

@@ -182,7 +182,7 @@ struct AdamWParams {
   uint32_t through[kAdamWTensors];           // chunks of the tensors up to and with it
   int32_t count;
   float b1, c1, b2, c2, eps;
-  float lr, rate, spread, factor;            // lr; lr / (1 - b1^t); 1 / sqrt(1 - b2^t); of the gradients
+  float rate, spread, factor;                // lr / (1 - b1^t); 1 / sqrt(1 - b2^t); of the gradients
   uint32_t seed;
   const float* control;                      // nullptr: the values above; else {lr, 1 / (1 - b1^t), 1 / sqrt(1 - b2^t), factor, seed's bits}
 };

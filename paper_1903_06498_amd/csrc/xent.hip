@@ -170,8 +170,8 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const XentJoinParams p) 
   store_loss(p, row, top, sum, p.target_z[row]);
 }
 
-// The same parts from logits in slices of the reduction, 1024 classes of a row a workgroup (one workgroup for a row: 15324 classes of 4 rows 27 us later);
-// lse and loss, where there are no more.
+// The same parts from logits in slices of the reduction, 1024 classes of a row a workgroup (one workgroup for a row: 4 rows, 1024 -> 15324 bf16 16.0 us in all, 11.3
+// here); lse and loss, where there are no more.
 constexpr int kSliceClasses = 1024;
 __global__ __launch_bounds__(256) void xent_slices_kernel(const XentJoinParams p) {
   constexpr int EACH = kSliceClasses / 256;
