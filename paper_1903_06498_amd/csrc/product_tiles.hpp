@@ -387,21 +387,23 @@ __device__ __forceinline__ bool place(const ProductParams& p, Tile* t) {
     if (t->slice >= t->slices) return false;
     number %= each;
   }
-  if (over_rows(KIND) && p.groups && spread(total, (unsigned)p.groups)) {
-    // An eighth of every group's tiles to each XCD: the groups' reductions are of very different lengths (8192 rows in 16 uneven groups, 1024 x 4096 features: 137 us
-    // where an XCD had whole groups, 100 here).
-    const unsigned x = blockIdx.x & 7u, i = blockIdx.x >> 3, first = total * x >> 3, own = (total * (x + 1) >> 3) - first;
-    if (i >= own * (unsigned)p.groups) return false;
-    t->group = (int)(i / own);
-    l = first + i % own;
-  } else {
-    if (over_rows(KIND) && p.groups) total *= (unsigned)p.groups;
-    if (!logical_number(number, total, &l)) return false;
-    if (over_rows(KIND) && p.groups) {
-      const unsigned each = row_tiles * (unsigned)p.tiles_n;
-      t->group = (int)(l / each);
-      l %= each;
+  if (over_rows(KIND) && p.groups) {
+    unsigned own = total, first = 0;
+    if (spread(total, (unsigned)p.groups)) {
+      // An eighth of every group's tiles to each XCD: the groups' reductions are of very different lengths (8192 rows in 16 uneven groups, 1024 x 4096 features: 137 us
+      // where an XCD had whole groups, 100 here).
+      const unsigned x = blockIdx.x & 7u;
+      first = total * x >> 3;
+      own = (total * (x + 1) >> 3) - first;
+      l = blockIdx.x >> 3;
+      if (l >= own * (unsigned)p.groups) return false;
+    } else if (!logical_number(number, total * (unsigned)p.groups, &l)) {
+      return false;
     }
+    t->group = (int)(l / own);
+    l = first + l % own;
+  } else if (!logical_number(number, total, &l)) {
+    return false;
   }
   const unsigned per = PATCH * (unsigned)p.tiles_n, patch = l / per, w = l % per;
   const unsigned high = row_tiles - patch * PATCH < PATCH ? row_tiles - patch * PATCH : PATCH;
