@@ -439,9 +439,11 @@ void stripe_gated_destroy(stripe_gated_t* gated);
  *   dz = exp(z - lse) (dloss + dlse) - [class = target] dloss,  dx = dz W,  dW = dz^T x.
  * x [rows][in_features], W [classes][in_features]; targets [rows]: int32 on the DEVICE; loss, lse, dloss, dlse [rows]: fp32.
  * A row whose target is not one of 0 .. classes - 1 does not count: loss, lse and dx are 0, dW has nothing of it, and whatever x holds there
- * (NaN, too) changes no bit of any result.  The backward pass computes z again, a piece of the vocabulary at a time (exp(z - lse) is at most 1, whatever the
- * two sums' roundings); a piece's dz is in the workspace, rounded to the operands' type.  In bf16 it is divided by the rows' largest |dloss| or |dloss + dlse| before and multiplied by it in dx and dW: of rows
- * whose weights are less than 2^-110 of that, digits may be lost.  dx is added up in fp32 over the pieces.
+ * (NaN, too) changes no bit of any result.  Logits may be of any finite size: exponentials are taken of distances, as the hardware's one of base 2 of the
+ * distance times log2 e, both in fp32 (f32 gradients: expf).  The backward pass computes z again, a piece of the vocabulary at a time (exp(z - lse) is
+ * at most 1, whatever the two sums' roundings); a piece's dz is in the workspace, rounded to the operands' type.  In bf16 it is divided by the rows'
+ * largest |dloss| or |dloss + dlse| before and multiplied by it in dx and dW: of rows whose weights are less than 2^-110 of that, digits may be
+ * lost.  dx is added up in fp32 over the pieces.
  */
 typedef struct {
   int64_t rows;             /* 0 .. 2^24 */
